@@ -71,7 +71,7 @@
  *                                 after n polls (n < 0: at once) and record
  *                                 the error that cavs_sync reports.
  *   - Errors found by kernels after a call has returned (a bounded wait that
- *     gave up) are kept by the context and returned by the next cavs_sync or
+ *     gave up, a word out of range) are kept by the context and returned by the next cavs_sync or
  *     cavs_timing_read.
  */
 #ifndef CAVS_H
@@ -317,6 +317,90 @@ cavs_status cavs_infer(cavs_ctx* ctx, const cavs_params* params, const cavs_sche
 cavs_status cavs_backward(cavs_ctx* ctx, const cavs_params* params, const cavs_sched* sched,
                           const cavs_inputs* inputs, void* ws, size_t ws_bytes,
                           const cavs_grads* grads);
+
+/* ---------------------------------------------------------------------------
+ * The two ends of a language model, outside F: the embedding makes the rows
+ * that vertices pull and turns their gradient into its table's; the vocabulary
+ * head scores pushed states over a large vocabulary.  With CAVS_LOSS_NONE and
+ * inputs.dH_ext a training step is
+ *   cavs_embed -> cavs_forward -> cavs_vocab_grad -> cavs_backward (dH_ext =
+ *   the head's dh) -> cavs_embed_grad (dX).
+ * Tables, rows and their gradients are fp32 or bf16 (CAVS_T_*), densely
+ * packed; sums and statistics are fp32, each output is rounded once.
+ *
+ * Words and labels are read on the device.  One that is out of range counts as
+ * -1 (no word, no label); the next cavs_sync or cavs_timing_read returns
+ * CAVS_ERR_RANGE.  Outputs must not overlap inputs or each other.  The calls
+ * allocate nothing, synchronise nothing and may be captured into a graph.
+ * ------------------------------------------------------------------------- */
+#define CAVS_T_F32 0
+#define CAVS_T_BF16 1
+
+typedef struct {
+  int32_t e_type, x_type;   /* CAVS_T_*: the table E (and dE); the rows X (and dX) */
+  int32_t n_words, D;       /* E [n_words, D], both > 0 */
+  const void* E;            /* cavs_embed: the table; cavs_embed_grad: unused */
+  float scale;
+} cavs_embedding;
+
+/* X[i] = scale * E[word[i]], i < n; word -1: a row of zeros. */
+cavs_status cavs_embed(cavs_ctx* ctx, const cavs_embedding* e, const int32_t* word, int32_t n,
+                       void* X);
+
+/* Bytes of device workspace cavs_embed_grad needs for n words.  0 on bad args. */
+size_t cavs_embed_grad_workspace_bytes(const cavs_embedding* e, int32_t n);
+
+/* dE[v] = scale * (sum of dX[i] over the i with word[i] = v), every row of dE
+   written.  The words are sorted and each row's terms added in a fixed order
+   (ascending i, in parts of 32 where a word occurs more often), so that the
+   result does not change from run to run. */
+cavs_status cavs_embed_grad(cavs_ctx* ctx, const cavs_embedding* e, const int32_t* word, int32_t n,
+                            const void* dX, void* dE, void* ws, size_t ws_bytes);
+
+/* Softmax cross entropy over C words, alone or mixed with distillation from a
+ * teacher's top logits (Section 3.5's lazily batched push, without the [n, C]
+ * logits).  Rows i with label[i] >= 0 are scored, z = h_i Ws + bs:
+ *   CE_i = ln sum_c exp(z_c) - z_label
+ *   KD_i = T^2 sum_j q_j (ln q_j - z_{t_j} / T + ln sum_c exp(z_c / T)),
+ *          q = softmax(top_logit / T) over the row's teacher's words t_j
+ *   L    = mean over the scored rows of (1 - alpha) CE_i + alpha KD_i
+ * Teacher's words may be listed in any order; -1 is no word, a word listed
+ * twice counts twice, and a row without a word whose logit is above -inf has
+ * KD_i = 0.  A bias of -inf takes a word out of the softmax.  With alpha = 1
+ * the labels' values do not matter and label may be NULL (every row scored).
+ * No scored row: L = 0, gradients 0.
+ * fp32 weights take the split products of CAVS_FP32 above; bf16 weights
+ * multiply with h rounded to bf16 and, in the gradients, dL/dz rounded to
+ * bf16 (the rounding points of CAVS_BF16), fp32 accumulation. */
+typedef struct {
+  int32_t h_type, w_type;   /* CAVS_T_*: h (and dh); Ws (and dWs) */
+  int32_t n, H, C;          /* rows, a multiple of 64 columns, words; at most 2^20, 2^15, 2^20 */
+  const void* h;            /* [n, H] */
+  const void* Ws;           /* [H, C] */
+  const float* bs;          /* [C] or NULL */
+  const int32_t* label;     /* [n] word of each row, or -1: not scored */
+  int32_t K;                /* teacher's words per row, 0 .. 256; 0: no teacher */
+  const int32_t* top_word;  /* [n, K] */
+  const float* top_logit;   /* [n, K] */
+  float alpha, temp;        /* weight of KD, in [0, 1]; T > 0 (read with K > 0) */
+} cavs_vocab;
+
+/* Bytes of device workspace cavs_vocab_loss (train = 0) or cavs_vocab_grad
+   (train = 1) needs: of n (H + C / 8) order for the loss, and for the gradient
+   one piece of dL/dz of about 256 MB, whatever C is.  0 on bad args. */
+size_t cavs_vocab_workspace_bytes(const cavs_vocab* v, int32_t train);
+
+/* loss [1] = L; row_loss [n] (or NULL) the terms of the mean, 0 for rows that
+   are not scored.  h, Ws and ws must be aligned to 16 bytes.  H % 64 != 0 and
+   sizes above those given are CAVS_ERR_UNSUPPORTED. */
+cavs_status cavs_vocab_loss(cavs_ctx* ctx, const cavs_vocab* v, float* loss, float* row_loss,
+                            void* ws, size_t ws_bytes);
+
+/* The same and the gradients of L, overwritten: dh [n, H] (0 for rows that are
+   not scored), dWs [H, C], dbs [C] (NULL exactly when bs is).  dh and dWs must
+   be aligned to 16 bytes. */
+cavs_status cavs_vocab_grad(cavs_ctx* ctx, const cavs_vocab* v, float* loss, float* row_loss,
+                            void* dh, void* dWs, float* dbs, void* ws, size_t ws_bytes);
 
 /* ---------------------------------------------------------------------------
  * Instrumentation (not part of the computation).  When enabled, every kernel

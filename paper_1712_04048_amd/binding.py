@@ -36,6 +36,8 @@ BF16 = 1
 LOSS_CE = 0
 LOSS_L2 = 1
 LOSS_NONE = 2
+T_F32 = 0
+T_BF16 = 1
 
 _i32 = ct.c_int32
 _vp = ct.c_void_p
@@ -74,10 +76,24 @@ class cavs_launch_time(ct.Structure):
     _fields_ = [("name", ct.c_char * 96), ("row0", _i32), ("rows", _i32), ("ms", ct.c_double)]
 
 
+class cavs_embedding(ct.Structure):
+    _fields_ = [("e_type", _i32), ("x_type", _i32), ("n_words", _i32), ("D", _i32), ("E", _vp),
+                ("scale", ct.c_float)]
+
+
+class cavs_vocab(ct.Structure):
+    _fields_ = [("h_type", _i32), ("w_type", _i32), ("n", _i32), ("H", _i32), ("C", _i32),
+                ("h", _vp), ("Ws", _vp), ("bs", _vp), ("label", _vp), ("K", _i32),
+                ("top_word", _vp), ("top_logit", _vp), ("alpha", ct.c_float),
+                ("temp", ct.c_float)]
+
+
 EXPORTS = ["cavs_create", "cavs_set_stream", "cavs_destroy", "cavs_last_error", "cavs_sync",
            "cavs_schedule_workspace_bytes", "cavs_schedule", "cavs_schedule_static",
            "cavs_workspace_bytes",
            "cavs_forward", "cavs_backward", "cavs_infer_workspace_bytes", "cavs_infer",
+           "cavs_embed", "cavs_embed_grad_workspace_bytes", "cavs_embed_grad",
+           "cavs_vocab_workspace_bytes", "cavs_vocab_loss", "cavs_vocab_grad",
            "cavs_timing_enable", "cavs_timing_read"]
 
 _lib = None
@@ -120,6 +136,19 @@ def lib():
         L.cavs_infer_workspace_bytes.argtypes = [ct.POINTER(cavs_params), ct.POINTER(cavs_sched)]
         L.cavs_infer.restype = _i32
         L.cavs_infer.argtypes = L.cavs_forward.argtypes
+        emb, voc = ct.POINTER(cavs_embedding), ct.POINTER(cavs_vocab)
+        L.cavs_embed.restype = _i32
+        L.cavs_embed.argtypes = [_vp, emb, _vp, _i32, _vp]
+        L.cavs_embed_grad_workspace_bytes.restype = ct.c_size_t
+        L.cavs_embed_grad_workspace_bytes.argtypes = [emb, _i32]
+        L.cavs_embed_grad.restype = _i32
+        L.cavs_embed_grad.argtypes = [_vp, emb, _vp, _i32, _vp, _vp, _vp, ct.c_size_t]
+        L.cavs_vocab_workspace_bytes.restype = ct.c_size_t
+        L.cavs_vocab_workspace_bytes.argtypes = [voc, _i32]
+        L.cavs_vocab_loss.restype = _i32
+        L.cavs_vocab_loss.argtypes = [_vp, voc, _vp, _vp, _vp, ct.c_size_t]
+        L.cavs_vocab_grad.restype = _i32
+        L.cavs_vocab_grad.argtypes = [_vp, voc, _vp, _vp, _vp, _vp, _vp, _vp, ct.c_size_t]
         L.cavs_timing_enable.restype = _i32
         L.cavs_timing_enable.argtypes = [_vp, _i32]
         L.cavs_timing_read.restype = _i32
@@ -347,3 +376,138 @@ def backward(ctx: Context, params: Params, sched: Schedule, X: Optional[torch.Te
     g = cavs_grads(*[_ptr(grads.get(k)) for k in ("dWx", "dU", "db", "dWs", "dbs", "dX")])
     ctx.check(lib().cavs_backward(ctx._h, ct.byref(p), ct.byref(sched.raw), ct.byref(inp),
                                   ws.data_ptr(), ws.numel(), ct.byref(g)))
+
+
+# --------------------------------------------------------------------------
+# The two ends of a language model (embedding, vocabulary head)
+# --------------------------------------------------------------------------
+
+_TYPES = {torch.float32: T_F32, torch.bfloat16: T_BF16}
+
+
+def _operand(name: str, t: Optional[torch.Tensor], shape, dtypes, device) -> Optional[int]:
+    """The address of a tensor after the checks that the C ABI cannot make."""
+    if not isinstance(t, torch.Tensor):
+        raise CavsError(ERR_ARG, "%s: a tensor is required" % name)
+    if t.dtype not in dtypes:
+        raise CavsError(ERR_ARG, "%s: %s, not %s" % (name, t.dtype, " or ".join(map(str, dtypes))))
+    if tuple(t.shape) != tuple(shape):
+        raise CavsError(ERR_ARG, "%s: shape %s, not %s" % (name, tuple(t.shape), tuple(shape)))
+    if device is not None and t.device != device:
+        raise CavsError(ERR_ARG, "%s is on %s, the context on %s" % (name, t.device, device))
+    if not t.is_contiguous():
+        raise CavsError(ERR_ARG, "%s is not contiguous" % name)
+    return t.data_ptr() if t.numel() else None
+
+
+def _workspace(ws: torch.Tensor, device):
+    _operand("ws", ws, (ws.numel(),), (torch.uint8,), device)
+    return ws.data_ptr(), ws.numel()
+
+
+@dataclass
+class Embedding:
+    """A table of word vectors: E [n_words, D] (float32 or bfloat16), scale."""
+    E: torch.Tensor
+    scale: float = 1.0
+
+    def raw(self, x_dtype, device=None) -> cavs_embedding:
+        if not isinstance(self.E, torch.Tensor) or self.E.dim() != 2:
+            raise CavsError(ERR_ARG, "E: a tensor [n_words, D] is required")
+        if x_dtype not in _TYPES:
+            raise CavsError(ERR_ARG, "X: %s is not supported" % x_dtype)
+        p = _operand("E", self.E, self.E.shape, _TYPES, device)
+        return cavs_embedding(_TYPES[self.E.dtype], _TYPES[x_dtype], int(self.E.shape[0]),
+                              int(self.E.shape[1]), p, float(self.scale))
+
+
+def embed(ctx: Context, emb: Embedding, word: torch.Tensor, X: torch.Tensor) -> None:
+    """cavs_embed: X [n, D] = scale * E[word] (asynchronous); int32 word -1: zeros."""
+    dev, n = ctx.torch_device, int(word.numel())
+    e = emb.raw(X.dtype, dev)
+    ctx.check(lib().cavs_embed(ctx._h, ct.byref(e), _operand("word", word, (n,), (torch.int32,), dev),
+                               n, _operand("X", X, (n, e.D), _TYPES, dev)))
+
+
+def embed_grad_workspace_bytes(emb: Embedding, n: int) -> int:
+    e = emb.raw(torch.float32)
+    return int(lib().cavs_embed_grad_workspace_bytes(ct.byref(e), int(n)))
+
+
+def embed_grad(ctx: Context, emb: Embedding, word: torch.Tensor, dX: torch.Tensor,
+               dE: torch.Tensor, ws: torch.Tensor) -> None:
+    """cavs_embed_grad: dE [n_words, D] of E's type, overwritten, from dX [n, D]
+    (asynchronous)."""
+    dev, n = ctx.torch_device, int(word.numel())
+    e = emb.raw(dX.dtype, dev)
+    ctx.check(lib().cavs_embed_grad(
+        ctx._h, ct.byref(e), _operand("word", word, (n,), (torch.int32,), dev), n,
+        _operand("dX", dX, (n, e.D), _TYPES, dev),
+        _operand("dE", dE, (e.n_words, e.D), (emb.E.dtype,), dev), *_workspace(ws, dev)))
+
+
+@dataclass
+class VocabHead:
+    """A softmax head over a large vocabulary: h [n, H], Ws [H, C] (float32 or
+    bfloat16), bs [C] float32, label [n] int32 (-1: not scored), and a
+    teacher's words and logits [n, K] (int32, float32) with their weight alpha
+    and temperature temp."""
+    h: torch.Tensor
+    Ws: torch.Tensor
+    bs: Optional[torch.Tensor] = None
+    label: Optional[torch.Tensor] = None
+    top_word: Optional[torch.Tensor] = None
+    top_logit: Optional[torch.Tensor] = None
+    alpha: float = 0.0
+    temp: float = 1.0
+
+    def raw(self, device=None) -> cavs_vocab:
+        for k, t in (("h", self.h), ("Ws", self.Ws)):
+            if not isinstance(t, torch.Tensor) or t.dim() != 2:
+                raise CavsError(ERR_ARG, "%s: a matrix is required" % k)
+        n, H, C = int(self.h.shape[0]), int(self.h.shape[1]), int(self.Ws.shape[1])
+        K = 0
+        if self.top_word is not None or self.top_logit is not None:
+            if self.top_word is None or self.top_logit is None or self.top_word.dim() != 2:
+                raise CavsError(ERR_ARG, "top_word and top_logit [n, K] go together")
+            K = int(self.top_word.shape[1])
+        f, i = (torch.float32,), (torch.int32,)
+        p = lambda name, t, shape, types: (None if t is None else
+                                           _operand(name, t, shape, types, device))
+        return cavs_vocab(
+            _TYPES.get(self.h.dtype, -1), _TYPES.get(self.Ws.dtype, -1), n, H, C,
+            p("h", self.h, (n, H), _TYPES), p("Ws", self.Ws, (H, C), _TYPES),
+            p("bs", self.bs, (C,), f), p("label", self.label, (n,), i), K,
+            p("top_word", self.top_word, (n, K), i), p("top_logit", self.top_logit, (n, K), f),
+            float(self.alpha), float(self.temp))
+
+
+def vocab_workspace_bytes(head: VocabHead, train: bool) -> int:
+    v = head.raw()
+    return int(lib().cavs_vocab_workspace_bytes(ct.byref(v), int(bool(train))))
+
+
+def vocab_loss(ctx: Context, head: VocabHead, loss: torch.Tensor,
+               row_loss: Optional[torch.Tensor], ws: torch.Tensor) -> None:
+    """cavs_vocab_loss (asynchronous): loss [1], row_loss [n] or None."""
+    dev, f = ctx.torch_device, (torch.float32,)
+    v = head.raw(dev)
+    ctx.check(lib().cavs_vocab_loss(
+        ctx._h, ct.byref(v), _operand("loss", loss, (1,), f, dev),
+        None if row_loss is None else _operand("row_loss", row_loss, (v.n,), f, dev),
+        *_workspace(ws, dev)))
+
+
+def vocab_grad(ctx: Context, head: VocabHead, loss: torch.Tensor,
+               row_loss: Optional[torch.Tensor], dh: torch.Tensor, dWs: torch.Tensor,
+               dbs: Optional[torch.Tensor], ws: torch.Tensor) -> None:
+    """cavs_vocab_grad (asynchronous): the loss and the gradients dh [n, H],
+    dWs [H, C] (of h's and Ws's types) and dbs [C], overwritten."""
+    dev, f = ctx.torch_device, (torch.float32,)
+    v = head.raw(dev)
+    ctx.check(lib().cavs_vocab_grad(
+        ctx._h, ct.byref(v), _operand("loss", loss, (1,), f, dev),
+        None if row_loss is None else _operand("row_loss", row_loss, (v.n,), f, dev),
+        _operand("dh", dh, (v.n, v.H), (head.h.dtype,), dev),
+        _operand("dWs", dWs, (v.H, v.C), (head.Ws.dtype,), dev),
+        None if dbs is None else _operand("dbs", dbs, (v.C,), f, dev), *_workspace(ws, dev)))

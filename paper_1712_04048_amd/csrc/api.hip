@@ -10,6 +10,7 @@
 #include <mutex>
 
 #include "kernels.h"
+#include "vocab.h"
 
 namespace cavs {
 
@@ -55,7 +56,13 @@ hipError_t zero_async(void* p, size_t bytes, hipStream_t s) {
 }
 
 cavs_status device_errors(cavs_ctx* ctx) {
-  if (!ctx->dev_err || !ctx->dev_err[0]) return CAVS_OK;
+  if (!ctx->dev_err) return CAVS_OK;
+  const bool range = ctx->dev_err[1] != 0;
+  ctx->dev_err[1] = 0;
+  if (!ctx->dev_err[0])
+    return range ? fail(ctx, CAVS_ERR_RANGE,
+                        "a word or label of an earlier call on this context was out of range")
+                 : CAVS_OK;
   ctx->dev_err[0] = 0;
   return fail(ctx, CAVS_ERR_HIP,
               "a persistent or XCD-local level loop's grid barrier gave up waiting in an "
@@ -445,7 +452,7 @@ cavs_status cavs_create(cavs_ctx** out, int32_t device, void* hip_stream) {
     delete ctx;
     return CAVS_ERR_HIP;
   }
-  ctx->dev_err[0] = 0;
+  ctx->dev_err[0] = ctx->dev_err[1] = 0;
   if (static_sched_scratch(ctx, device, &ctx->sched_scratch) != CAVS_OK) {
     (void)hipHostFree(ctx->host_stage);
     (void)hipHostFree(ctx->dev_err);
@@ -812,6 +819,50 @@ cavs_status cavs_backward(cavs_ctx* ctx, const cavs_params* p, const cavs_sched*
   }
   CAVS_LAUNCH_CHECK(ctx);
   return CAVS_OK;
+}
+
+size_t cavs_embed_grad_workspace_bytes(const cavs_embedding* e, int32_t n) {
+  return embed_grad_ws_bytes(e, n);
+}
+
+cavs_status cavs_embed(cavs_ctx* ctx, const cavs_embedding* e, const int32_t* word, int32_t n,
+                       void* X) {
+  if (!ctx) return CAVS_ERR_ARG;
+  ctx->err.clear();
+  CAVS_HIP_CHECK(ctx, hipSetDevice(ctx->device));
+  ActiveCtx active(ctx);
+  return embed_run(ctx, e, word, n, X);
+}
+
+cavs_status cavs_embed_grad(cavs_ctx* ctx, const cavs_embedding* e, const int32_t* word, int32_t n,
+                            const void* dX, void* dE, void* ws, size_t ws_bytes) {
+  if (!ctx) return CAVS_ERR_ARG;
+  ctx->err.clear();
+  CAVS_HIP_CHECK(ctx, hipSetDevice(ctx->device));
+  ActiveCtx active(ctx);
+  return embed_grad_run(ctx, e, word, n, dX, dE, ws, ws_bytes);
+}
+
+size_t cavs_vocab_workspace_bytes(const cavs_vocab* v, int32_t train) {
+  return vocab_ws_bytes(v, train != 0);
+}
+
+cavs_status cavs_vocab_loss(cavs_ctx* ctx, const cavs_vocab* v, float* loss, float* row_loss,
+                            void* ws, size_t ws_bytes) {
+  if (!ctx) return CAVS_ERR_ARG;
+  ctx->err.clear();
+  CAVS_HIP_CHECK(ctx, hipSetDevice(ctx->device));
+  ActiveCtx active(ctx);
+  return vocab_run(ctx, v, loss, row_loss, nullptr, nullptr, nullptr, ws, ws_bytes, false);
+}
+
+cavs_status cavs_vocab_grad(cavs_ctx* ctx, const cavs_vocab* v, float* loss, float* row_loss,
+                            void* dh, void* dWs, float* dbs, void* ws, size_t ws_bytes) {
+  if (!ctx) return CAVS_ERR_ARG;
+  ctx->err.clear();
+  CAVS_HIP_CHECK(ctx, hipSetDevice(ctx->device));
+  ActiveCtx active(ctx);
+  return vocab_run(ctx, v, loss, row_loss, dh, dWs, dbs, ws, ws_bytes, true);
 }
 
 }  // extern "C"
