@@ -16,57 +16,6 @@ constexpr int kEmbedMax = 1 << 28, kEmbedMaxD = 1 << 20;
 constexpr int kPart = 32;         // rows of a word that one wavefront adds
 constexpr int kSortWords = 512;   // most words of a sorting workgroup
 
-// V adjacent elements as floats, and back (rounded once)
-template <int V, class T>
-__device__ __forceinline__ void load_row(const T* p, float (&v)[V]) {
-  if constexpr (sizeof(T) == 4) {
-    if constexpr (V % 4 == 0) {
-#pragma unroll
-      for (int i = 0; i < V; i += 4) {
-        const float4 x = ldg4((const float*)p + i);
-        v[i] = x.x; v[i + 1] = x.y; v[i + 2] = x.z; v[i + 3] = x.w;
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < V; ++i) v[i] = p[i];
-    }
-  } else {
-    uint32_t w[(V + 1) / 2];
-    if constexpr (V == 8) {
-      const uint4 x = *reinterpret_cast<const uint4*>(p);
-      w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
-    } else if constexpr (V == 4) {
-      const uint2 x = *reinterpret_cast<const uint2*>(p);
-      w[0] = x.x; w[1] = x.y;
-    } else {
-      w[0] = *p;
-    }
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-      v[i] = __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
-  }
-}
-template <int V, class T>
-__device__ __forceinline__ void store_row(T* p, const float (&v)[V]) {
-  if constexpr (sizeof(T) == 4) {
-    if constexpr (V % 4 == 0) {
-#pragma unroll
-      for (int i = 0; i < V; i += 4) st4((float*)p + i, make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]));
-    } else {
-#pragma unroll
-      for (int i = 0; i < V; ++i) p[i] = v[i];
-    }
-  } else if constexpr (V == 8) {
-    *reinterpret_cast<uint4*>(p) =
-        make_uint4(f2bf2(v[0], v[1]), f2bf2(v[2], v[3]), f2bf2(v[4], v[5]), f2bf2(v[6], v[7]));
-  } else if constexpr (V == 4) {
-    st_bf4((u16*)p, make_float4(v[0], v[1], v[2], v[3]));
-  } else {
-#pragma unroll
-    for (int i = 0; i < V; ++i) p[i] = f2bf(v[i]);
-  }
-}
-
 // A thread per V elements of X.
 template <class E, class X, int V>
 __global__ void __launch_bounds__(256) k_embed(int n_words, int D, unsigned total, float scale,

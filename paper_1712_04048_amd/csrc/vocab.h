@@ -9,11 +9,14 @@
 // padded capacity; rows from the live ones to the end of their tile hold zeros.
 #pragma once
 
+#include <type_traits>
+
 #include "kernels.h"
 
 namespace cavs {
 
 constexpr int kVocabTile = 256;   // rows, and words of a piece, are padded to this
+constexpr int kVocabFew = 64;     // most rows of the kernels for few rows
 constexpr int kVocabMaxK = 256;   // most teacher's words per row
 
 struct VocabNet {
@@ -21,6 +24,7 @@ struct VocabNet {
   int rows;                // n padded to kVocabTile
   int bf;                  // products in bf16 (h and W_s rounded), else split fp32
   int hbf, wbf;            // element types of h / dh and of W_s / dW_s
+  int few, pad, keep;      // at most kVocabFew rows; Ws is a padded copy; z is kept
   int two;                 // a second softmax, at a temperature other than 1
   float alpha, temp;
   // dz is kept in units of `unit` = 1 - alpha (alpha = 1: T), so that the label's
@@ -39,8 +43,11 @@ struct VocabNet {
   int* live;               // [0] live rows
   float* scal;             // [0] unit / max(1, live rows)
   int* label;              // [rows] -1: none
-  int* tword;              // [rows, K] distinct words of the row, -1: none
-  float* tq;               // [rows, K] the teacher's probability of tword
+  int* tword;              // [rows, K] the row's words, ascending (absent ones last)
+  float* tq;               // [rows, K] the teacher's probability of tword (a word that
+                           //   is there twice: all of it at its first place, else 0)
+  uint32_t* trange;        // [slots, rows] places in tword of the words of a slot: the
+                           //   first, and past the last in the upper half
   float2* tsum;            // [rows] sum of q ln q, 1 (a teacher's word is there) or 0
   void* hp;                // [rows, H] live rows of h in the products' type
   float* pm;               // [slots, rows] each slot of columns: its largest z,
@@ -55,7 +62,9 @@ struct VocabNet {
   float* zrow;             // a row of zeros (16 bytes and more)
   // gradient, one piece of words at a time
   int P;                   // words of a piece, a multiple of kVocabTile
-  void* dZ;                // [rows, P] products' type
+  void* dZ;                // [rows, P] products' type (bf16, several pieces: two of them)
+  size_t dz_half;          // bytes from one to the other
+  float* Z;                // [rows, P] z in one piece, where it is kept (in fp32 dZ itself), or null
   float* dbp;              // [rows / 64 or finer, P] sums of dz over groups of rows
   int db_rows;             // rows of a group
   float* hpart;            // [Sh, rows, H] dh's sums, added to by each piece
@@ -73,7 +82,9 @@ struct VocabEp {
   const int* label;
   const int* tword;
   const float* tq;
+  const uint32_t* trange;
   float *pm, *ps, *pt, *zlab, *ztop;
+  float* zkeep;            // LOSS: z goes here (or null), rows of ldz
   const float4* rowc;
   void* dz;
   long long ldz;
@@ -95,29 +106,110 @@ __device__ __forceinline__ void wave_lds_fence() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// LDS floats of a wavefront's slab: 16 rows of NC columns, four floats of
-// padding (a lane group's 16-byte writes to 16 rows then spread over the banks).
-template <int NC>
-constexpr int kSlabFloats = 16 * (NC + 4);
+// V adjacent elements as floats, and back (rounded once)
+template <int V, class T>
+__device__ __forceinline__ void load_row(const T* p, float (&v)[V]) {
+  if constexpr (sizeof(T) == 4) {
+    if constexpr (V % 4 == 0) {
+#pragma unroll
+      for (int i = 0; i < V; i += 4) {
+        const float4 x = ldg4((const float*)p + i);
+        v[i] = x.x; v[i + 1] = x.y; v[i + 2] = x.z; v[i + 3] = x.w;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] = p[i];
+    }
+  } else {
+    uint32_t w[(V + 1) / 2];
+    if constexpr (V == 8) {
+      const uint4 x = *reinterpret_cast<const uint4*>(p);
+      w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
+    } else if constexpr (V == 4) {
+      const uint2 x = *reinterpret_cast<const uint2*>(p);
+      w[0] = x.x; w[1] = x.y;
+    } else {
+      w[0] = *p;
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      v[i] = __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+  }
+}
+template <int V, class T>
+__device__ __forceinline__ void store_row(T* p, const float (&v)[V]) {
+  if constexpr (sizeof(T) == 4) {
+    if constexpr (V % 4 == 0) {
+#pragma unroll
+      for (int i = 0; i < V; i += 4) st4((float*)p + i, make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]));
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) p[i] = v[i];
+    }
+  } else if constexpr (V == 8) {
+    *reinterpret_cast<uint4*>(p) =
+        make_uint4(f2bf2(v[0], v[1]), f2bf2(v[2], v[3]), f2bf2(v[4], v[5]), f2bf2(v[6], v[7]));
+  } else if constexpr (V == 4) {
+    st_bf4((u16*)p, make_float4(v[0], v[1], v[2], v[3]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) p[i] = f2bf(v[i]);
+  }
+}
 
-// One group of 16 rows of a wavefront's tile: lane (g, r) holds NV = NC / 4 of
-// row `row` (its own r's; rr's row is row0 + step rr), z[i] the product of word
-// a0 + col(i, g).  LOSS: the slot's statistics and the z that the loss names.
-// Otherwise dz = w1 exp(z - m) + wT exp((z - m) / T) - [label] - teacher's q,
-// in 32 bits until it is stored, and its sum over the rows into db.
+// The sum over the sixteen lanes of a lane group, in every one of them.
+__device__ __forceinline__ float row16_sum(float v) {
+  auto ror = [](float x, auto n) {   // row_ror
+    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x120 + decltype(n)::value, 15, 15, true));
+  };
+  v += ror(v, std::integral_constant<int, 8>{});
+  v += ror(v, std::integral_constant<int, 4>{});
+  v += ror(v, std::integral_constant<int, 2>{});
+  v += ror(v, std::integral_constant<int, 1>{});
+  return v;
+}
+
+// One group of 16 rows of a wavefront's tile of NC words, which lie in slot
+// `slot` of words: lane (g, r) holds NV = NC / 4 of row `row` (r's), z[i] the score of word
+// a0 + col(i, g), four adjacent i adjacent words.  LOSS: the words' statistics
+// (to pm[stat] and on) and the z that the loss names.  Otherwise dz = w1 exp(z - m) + wT exp((z - m)
+// / T) - [label] - teacher's q, in 32 bits until it is stored, and added to db.
 //
 // The statistics need one pass: largest, then the sums relative to it, which
 // the row kernel joins over the slots.  A slot without a finite word (words
 // masked with -inf, columns past C) has largest -inf and sums 0.
+//
+// A row's label and its teacher's words fall into few slots, so what looks for
+// them is skipped where no row of the group has one: the labels by comparison,
+// the words (sorted by k_vocab_teacher) by their range in this slot.  The
+// values go out as the lanes hold them: passing them through LDS for whole
+// 128-byte stores made a tile of dz 20 us long, where a tile's product of
+// depth 1024 is 25.
 template <bool LOSS, bool TEACH, class OUT, int NC, class Col>
-__device__ __forceinline__ void vocab_rows16(const VocabEp& e, float (&z)[NC / 4], Col col, int row0,
-                                             int step, int a0, int slot, int live, float* slab,
-                                             float (&db)[NC / 64]) {
-  constexpr int NV = NC / 4, LD = NC + 4;
-  const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15, row = row0 + step * r;
+__device__ __forceinline__ void vocab_rows16(const VocabEp& e, float (&z)[NC / 4], Col col, int row,
+                                             int a0, int slot, size_t stat, int live,
+                                             float (&db)[NC / 4]) {
+  constexpr int NV = NC / 4;
+  const int g = (threadIdx.x & 63) >> 4;
   const bool here = row < live;
-  const int lab = here && e.label ? e.label[row] - a0 : -1;
+  const int lab = (here && e.label ? e.label[row] : -1) - a0;
+  const bool labelled = __any((unsigned)lab < (unsigned)NC);
+  uint32_t range = 0;
+  if constexpr (TEACH) range = here ? e.trange[(size_t)slot * e.rows + row] : 0u;
+  // f(word's place in the row's list, its column) for each of the row's words here
+  auto words = [&](auto&& f) {
+    const int hi = range >> 16;
+    for (int j = range & 0xffffu; __any(j < hi); ++j) {
+      const size_t at = (size_t)row * e.K + j;
+      f(at, j < hi ? e.tword[at] - a0 : -1);
+    }
+  };
   if constexpr (LOSS) {
+    if (e.zkeep) {
+      float* d = e.zkeep + (size_t)row * e.ldz + a0;
+#pragma unroll
+      for (int i = 0; i < NV; i += 4) st4(d + col(i, g), make_float4(z[i], z[i + 1], z[i + 2], z[i + 3]));
+    }
     float m = z[0];
 #pragma unroll
     for (int i = 1; i < NV; ++i) m = fmaxf(m, z[i]);
@@ -129,78 +221,78 @@ __device__ __forceinline__ void vocab_rows16(const VocabEp& e, float (&z)[NC / 4
     for (int i = 0; i < NV; ++i) s += __builtin_amdgcn_exp2f((z[i] - mm) * kLog2e);
     s += __shfl_xor(s, 16, kWave);
     s += __shfl_xor(s, 32, kWave);
-    if (e.two) {
+    if (TEACH && e.two) {
+      const float k = e.invT * kLog2e;
 #pragma unroll
-      for (int i = 0; i < NV; ++i) t += __builtin_amdgcn_exp2f((z[i] - mm) * e.invT * kLog2e);
+      for (int i = 0; i < NV; ++i) t += __builtin_amdgcn_exp2f((z[i] - mm) * k);
       t += __shfl_xor(t, 16, kWave);
       t += __shfl_xor(t, 32, kWave);
     }
     if (g == 0) {
-      const size_t at = (size_t)slot * e.rows + row;
-      e.pm[at] = m;
-      e.ps[at] = s;
-      if (e.two) e.pt[at] = t;
+      e.pm[stat] = m;
+      e.ps[stat] = s;
+      if (TEACH && e.two) e.pt[stat] = t;
     }
-    if ((unsigned)lab < (unsigned)NC) {
+    if (labelled) {
 #pragma unroll
       for (int i = 0; i < NV; ++i)
         if (col(i, g) == lab) e.zlab[row] = z[i];
     }
+    if constexpr (TEACH)
+      words([&](size_t at, int d) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+          if (col(i, g) == d) e.ztop[at] = z[i];
+      });
   } else {
-    float4 c = e.rowc[row];
+    const float4 c = e.rowc[row];
+    if (TEACH && e.two) {
+      const float k = e.invT * kLog2e;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      float v = c.y * __builtin_amdgcn_exp2f((z[i] - c.x) * kLog2e);
-      if (e.two) v += c.z * __builtin_amdgcn_exp2f((z[i] - c.x) * e.invT * kLog2e);
-      if (col(i, g) == lab) v -= c.w;
-      z[i] = here && a0 + col(i, g) < e.C ? v : 0.f;
-    }
-  }
-  if constexpr (!LOSS || TEACH) {
-    // four adjacent words of a lane at a time
-#pragma unroll
-    for (int i = 0; i < NV; i += 4)
-      st4(slab + r * LD + col(i, g), make_float4(z[i], z[i + 1], z[i + 2], z[i + 3]));
-    wave_lds_fence();
-  }
-  if constexpr (TEACH) {
-    // each teacher's word of a row is there once (k_vocab_teacher), so no two
-    // lanes change one place
-    for (int x = lane; x < 16 * e.K; x += 64) {
-      const int rr = (unsigned)x / (unsigned)e.K, rw = row0 + step * rr;
-      if (rw >= live) continue;
-      const size_t at = (size_t)rw * e.K + (x - rr * e.K);
-      const int d = e.tword[at] - a0;
-      if ((unsigned)d >= (unsigned)NC) continue;
-      if constexpr (LOSS) e.ztop[at] = slab[rr * LD + d];
-      else slab[rr * LD + d] -= e.distw * e.tq[at];
-    }
-    wave_lds_fence();
-  }
-  if constexpr (!LOSS) {
-#pragma unroll
-    for (int k = 0; k < NC / 64; ++k)
-#pragma unroll
-      for (int rr = 0; rr < 16; ++rr) db[k] += slab[rr * LD + lane + 64 * k];
-    constexpr int VEC = sizeof(OUT) == 2 ? 8 : 4, PER = NC / VEC, ROWS = 64 / PER;
-    const int rr0 = lane / PER, c0 = lane % PER * VEC;
-#pragma unroll
-    for (int k = 0; k < 16 / ROWS; ++k) {
-      const int rr = rr0 + k * ROWS;
-      OUT* d = (OUT*)e.dz + (size_t)(row0 + step * rr) * e.ldz + (a0 - e.col0) + c0;
-      const float4 x = *reinterpret_cast<const float4*>(slab + rr * LD + c0);
-      if constexpr (sizeof(OUT) == 2) {
-        const float4 y = *reinterpret_cast<const float4*>(slab + rr * LD + c0 + 4);
-        *reinterpret_cast<uint4*>(d) =
-            make_uint4(f2bf2(x.x, x.y), f2bf2(x.z, x.w), f2bf2(y.x, y.y), f2bf2(y.z, y.w));
-      } else {
-        *reinterpret_cast<float4*>(d) = x;
+      for (int i = 0; i < NV; ++i) {
+        const float x = z[i] - c.x;
+        z[i] = c.y * __builtin_amdgcn_exp2f(x * kLog2e) + c.z * __builtin_amdgcn_exp2f(x * k);
       }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) z[i] = c.y * __builtin_amdgcn_exp2f((z[i] - c.x) * kLog2e);
     }
-    wave_lds_fence();   // the next group's values overwrite the slab
-  } else if constexpr (TEACH) {
-    wave_lds_fence();
+    if (labelled) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) z[i] -= col(i, g) == lab ? c.w : 0.f;
+    }
+    if constexpr (TEACH)
+      words([&](size_t at, int d) {
+        const float q = d >= 0 ? e.distw * e.tq[at] : 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) z[i] -= col(i, g) == d ? q : 0.f;
+      });
+    if (a0 + NC > e.C) {   // words past C (a row whose sums are NaN has NaN there too)
+#pragma unroll
+      for (int i = 0; i < NV; ++i) z[i] = a0 + col(i, g) < e.C ? z[i] : 0.f;
+    }
+    OUT* d = (OUT*)e.dz + (size_t)row * e.ldz + (a0 - e.col0);
+#pragma unroll
+    for (int i = 0; i < NV; i += 4) {
+      const float4 v = make_float4(z[i], z[i + 1], z[i + 2], z[i + 3]);
+      if constexpr (sizeof(OUT) == 2) st_bf4((u16*)d + col(i, g), v);
+      else st4((float*)d + col(i, g), v);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) db[i] += z[i];
   }
+}
+
+// A wavefront's sums of dz over its rows, as group `group` of the piece's.
+template <int NC, class Col>
+__device__ __forceinline__ void vocab_db(const VocabEp& e, float (&db)[NC / 4], Col col, int a0, int group) {
+  const int lane = threadIdx.x & 63, g = lane >> 4;
+  float* d = e.dbp + (size_t)group * e.ldz + (a0 - e.col0);
+#pragma unroll
+  for (int i = 0; i < NC / 4; ++i) db[i] = row16_sum(db[i]);
+#pragma unroll
+  for (int i = 0; i < NC / 4; i += 4)
+    if ((lane & 15) == (i / 4) % 16) st4(d + col(i, g), make_float4(db[i], db[i + 1], db[i + 2], db[i + 3]));
 }
 
 // The bias of a lane's words (0 where there is none), for words past C -inf:
@@ -214,6 +306,63 @@ __device__ __forceinline__ void vocab_bias(const VocabEp& e, int a0, int g, Col 
   }
 }
 
+// A workgroup of the kernels for few rows: four wavefronts of 32 words each by 64
+// rows, z(i, f) lane (g, r)'s word col(i, g) of row 16 f + r.  The wavefronts'
+// statistics are joined into the slots of SW words.
+template <bool TEACH, int SW, class Z>
+__device__ __forceinline__ void vocab_few_end(const VocabEp& e, float (&stats)[3][4][kVocabFew], int a0, Z z) {
+  constexpr int NC = 32, PER = SW / NC;   // wavefronts of a slot
+  const int tid = threadIdx.x, w = tid >> 6, g = (tid & 63) >> 4, r = tid & 15, aw = a0 + NC * w;
+  VocabEp own = e;
+  own.pm = stats[0][w];
+  own.ps = stats[1][w];
+  own.pt = stats[2][w];
+  auto col = [](int i, int gg) { return 16 * (i >> 2) + 4 * gg + (i & 3); };
+  float bias[NC / 4], db[NC / 4];
+  vocab_bias(e, aw, g, col, bias);
+  const int live = *e.live;
+#pragma unroll
+  for (int f = 0; f < kVocabFew / 16; ++f) {
+    float x[NC / 4];
+#pragma unroll
+    for (int i = 0; i < NC / 4; ++i) x[i] = z(i, f) + bias[i];
+    vocab_rows16<true, TEACH, float, NC>(own, x, col, 16 * f + r, aw, aw / SW, 16 * f + r, live, db);
+  }
+  __syncthreads();
+  const int row = tid & 63;
+  if (w >= 4 / PER) return;
+  float m = -INFINITY, s = 0.f, t = 0.f;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) m = fmaxf(m, stats[0][PER * w + k][row]);
+  const float mm = m == -INFINITY ? 0.f : m;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const float d = (stats[0][PER * w + k][row] - mm) * kLog2e;
+    s += stats[1][PER * w + k][row] * __builtin_amdgcn_exp2f(d);
+    if (TEACH && e.two) t += stats[2][PER * w + k][row] * __builtin_amdgcn_exp2f(d * e.invT);
+  }
+  const size_t at = (size_t)(a0 / SW + w) * e.rows + row;
+  e.pm[at] = m;
+  e.ps[at] = s;
+  if (TEACH && e.two) e.pt[at] = t;
+}
+
+// Eight (bf16) or two (float) adjacent values from element o on of a matrix of
+// `end` elements (at least 64): where it ends among them, or before, what there
+// is and zeros.
+__device__ __forceinline__ uint4 vocab_load8(const u16* W, size_t o, size_t end) {
+  uint4 x;
+  if (o + 8 <= end) {
+    __builtin_memcpy(&x, W + o, 16);
+  } else {
+    unsigned __int128 t;
+    __builtin_memcpy(&t, W + (end - 8), 16);
+    t = o < end ? t >> (16 * (int)(o - (end - 8))) : 0;
+    __builtin_memcpy(&x, &t, 16);
+  }
+  return x;
+}
+
 // four adjacent values of one row of an output, times w
 __device__ __forceinline__ void vocab_store4(const VocabOut& o, float w, int z, int row, int c, float4 v) {
   if (row >= o.rows || c >= o.cols) return;
@@ -222,8 +371,11 @@ __device__ __forceinline__ void vocab_store4(const VocabOut& o, float w, int z, 
   const float x[4] = {v.x, v.y, v.z, v.w};
   if (o.bf) {
     u16* d = (u16*)o.out + at;
-    if ((o.ld & 3) == 0 && c + 4 <= o.cols) {
-      st_bf4(d, v);
+    // at the alignment of an element, whatever C is: dW_s of 50 001 columns and few
+    // rows took 106 us in 2-byte stores, 53 so
+    if (c + 4 <= o.cols) {
+      const uint2 q = make_uint2(f2bf2(v.x, v.y), f2bf2(v.z, v.w));
+      __builtin_memcpy(d, &q, 8);
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -231,8 +383,9 @@ __device__ __forceinline__ void vocab_store4(const VocabOut& o, float w, int z, 
     }
   } else {
     float* d = (float*)o.out + at;
-    if ((o.ld & 3) == 0 && c + 4 <= o.cols) {
-      st4(d, o.acc ? add4(ldg4(d), v) : v);
+    if (c + 4 <= o.cols) {
+      if (o.acc) v = add4(ldg4(d), v);   // sums of the library's own, aligned
+      __builtin_memcpy(d, &v, 16);
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -243,16 +396,21 @@ __device__ __forceinline__ void vocab_store4(const VocabOut& o, float w, int z, 
 
 VocabEp vocab_ep(const VocabNet& v, int col0);
 
-// The products, by type.  loss: statistics of every word; dz: one piece's dZ
-// and dbp; dh: the piece's share of hpart; dW: the piece's columns of dW.
-void vocab_x3_loss(const VocabNet& v, hipStream_t s);
+// The piece of dZ that begins with word col0: the two halves in turn.
+inline char* vocab_dz_at(const VocabNet& v, int col0) {
+  return (char*)v.dZ + (col0 / v.P % 2) * v.dz_half;
+}
+
+// The products, by type.  loss: statistics of every word (few rows: from the
+// caller's W, without a padded copy); dz: one piece's dZ and dbp; dh: the
+// piece's share of hpart; dw: the piece's columns of dW_s; grads: both.
+void vocab_x3_loss(const VocabNet& v, const void* W, hipStream_t s);
 void vocab_x3_dz(const VocabNet& v, int col0, int cols, hipStream_t s);
 void vocab_x3_dh(const VocabNet& v, int col0, int cols, hipStream_t s);
 void vocab_x3_dw(const VocabNet& v, int col0, int cols, const VocabOut& o, hipStream_t s);
-void vocab_bf_loss(const VocabNet& v, hipStream_t s);
+void vocab_bf_loss(const VocabNet& v, const void* W, hipStream_t s);
 void vocab_bf_dz(const VocabNet& v, int col0, int cols, hipStream_t s);
-void vocab_bf_dh(const VocabNet& v, int col0, int cols, hipStream_t s);
-void vocab_bf_dw(const VocabNet& v, int col0, int cols, const VocabOut& o, hipStream_t s);
+void vocab_bf_grads(const VocabNet& v, int col0, int cols, int next, const VocabOut& o, hipStream_t s);
 
 // embed.hip
 size_t embed_grad_ws_bytes(const cavs_embedding* e, int n);

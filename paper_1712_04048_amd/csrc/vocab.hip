@@ -19,223 +19,251 @@ namespace cavs {
 namespace {
 
 // Sizes whose tiles and offsets the kernels count in 32 bits.
+constexpr size_t kKeepBytes = (size_t)128 << 20;
 constexpr int kVocabMaxRows = 1 << 20, kVocabMaxWords = 1 << 20, kVocabMaxH = 1 << 15;
 
-// Live rows in ascending order, their labels, unit / their number.  One
-// workgroup: 8192 rows are eight rounds.
-__global__ void __launch_bounds__(1024) k_vocab_rows(int n, int C, const int* __restrict__ label,
-                                                     int* rows, int* place, int* clabel, int* live, float unit,
-                                                     float* scal,
-                                                     float* row_loss, float* zrow, int* err) {
-  __shared__ int wsum[16];
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  if (tid < 64) zrow[tid] = 0.f;
-  int done = 0;
+// The live rows: their list and numbering, their labels, their rows of h in the
+// products' type (zeros to the end of their last tile), and unit / their number.
+// A workgroup takes R of the caller's rows and counts the labels before them
+// itself, so that nothing waits for a list: R is at least 16 and at least n /
+// 512, which bounds what all of them read to 512 n labels.
+template <class IN, class OUT>
+__global__ void __launch_bounds__(256) k_vocab_rows(VocabNet v, int R, const int* __restrict__ label,
+                                                    float* row_loss, int* err) {
+  __shared__ int wsum[4], src_of[64], found;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, n = v.n, C = v.C, H = v.H;
+  const int lo = blockIdx.x * R, hi = min(lo + R, n);
+  auto scored = [&](int i) {
+    const int y = label ? label[i] : 0;
+    return y >= 0 && y < C;
+  };
+  int before = 0;
+#pragma unroll 4
+  for (int i = tid; i < lo; i += 256) before += scored(i);
+  before = wave_sum_int(before);
+  if (lane == 0) wsum[w] = before;
+  __syncthreads();
+  before = wsum[0] + wsum[1] + wsum[2] + wsum[3];
   bool bad = false;
-  for (int base = 0; base < n; base += 1024) {
-    const int i = base + tid;
-    const int y = i < n ? (label ? label[i] : 0) : -1;
-    bad |= y < -1 || y >= C;
-    const bool on = y >= 0 && y < C;
-    const unsigned long long m = __ballot(on);
-    if (lane == 0) wsum[w] = __popcll(m);
+  // 64 rows at a time: the first wavefront numbers them, then all copy
+  for (int i0 = lo; i0 < hi; i0 += 64) {
+    if (w == 0) {
+      const int i = i0 + lane;
+      const int y = i < hi ? (label ? label[i] : 0) : -1;
+      const bool on = y >= 0 && y < C;
+      bad |= y < -1 || y >= C;
+      const unsigned long long m = __ballot(on);
+      const int k = __popcll(m & ((1ull << lane) - 1)), at = before + k;
+      if (i < hi) v.place[i] = on ? at : -1;
+      if (on) {
+        src_of[k] = i;
+        v.rows_list[at] = i;
+        v.label[at] = label ? y : -1;
+      } else if (i < hi && row_loss) {
+        row_loss[i] = 0.f;
+      }
+      if (lane == 0) found = __popcll(m);
+    }
     __syncthreads();
-    int before = done, total = 0;
-#pragma unroll
-    for (int k = 0; k < 16; ++k) {
-      if (k < w) before += wsum[k];
-      total += wsum[k];
+    const int nf = found;
+    constexpr int VEC = 8;
+    const int q = H / VEC, items = nf * q;   // H is a multiple of 64
+#pragma unroll 4
+    for (int x = tid; x < items; x += 256) {
+      const int k = (unsigned)x / (unsigned)q, c = (x - k * q) * VEC;
+      float val[VEC];
+      load_row<VEC>((const IN*)v.h + (size_t)src_of[k] * H + c, val);
+      store_row<VEC>((OUT*)v.hp + (size_t)(before + k) * H + c, val);
     }
-    if (on) {
-      const int at = before + __popcll(m & ((1ull << lane) - 1));
-      rows[at] = i;
-      clabel[at] = label ? y : -1;
-      place[i] = at;
-    } else if (i < n) {
-      place[i] = -1;
-      if (row_loss) row_loss[i] = 0.f;
-    }
-    done += total;
+    before += nf;
     __syncthreads();
   }
   if (bad) err[1] = 1;
+  if (hi < n) return;
+  if (tid < 64) v.zrow[tid] = 0.f;
   if (tid == 0) {
-    *live = done;
-    scal[0] = unit / (float)max(done, 1);
+    *v.live = before;
+    *v.scal = v.unit / (float)max(before, 1);
   }
+  // H is a multiple of 64: whole 16 bytes
+  const size_t from = (size_t)before * H * sizeof(OUT);
+  const int tile = v.few ? kVocabFew : kVocabTile;
+  const size_t to = (size_t)cdiv_dev(before, tile) * tile * H * sizeof(OUT);
+  for (size_t o = from + 16 * tid; o < to; o += 256 * 16) st4((float*)((char*)v.hp + o), f4zero());
 }
 
-// The live rows of h in the products' type, zeros to the end of their tile.
-template <class IN, class OUT>
-__global__ void __launch_bounds__(256) k_vocab_pack(int H, const IN* __restrict__ h,
-                                                    const int* __restrict__ rows,
-                                                    const int* __restrict__ live, OUT* hp) {
-  const int nl = *live, end = (nl + kVocabTile - 1) / kVocabTile * kVocabTile;
-  const int q = H / 4;   // H is a multiple of 64
-  for (int row = blockIdx.x * 4 + (threadIdx.x >> 6); row < end; row += gridDim.x * 4) {
-    const IN* src = row < nl ? h + (size_t)rows[row] * H : nullptr;
-    OUT* dst = hp + (size_t)row * H;
-    for (int c = threadIdx.x & 63; c < q; c += 64) {
-      float4 v = f4zero();
-      if (src) {
-        if constexpr (sizeof(IN) == 4) {
-          v = ldg4((const float*)src + 4 * c);
-        } else {
-          const uint2 x = *reinterpret_cast<const uint2*>(src + 4 * c);
-          v = make_float4(__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xffff0000u),
-                          __uint_as_float(x.y << 16), __uint_as_float(x.y & 0xffff0000u));
-        }
-      }
-      if constexpr (sizeof(OUT) == 4) st4((float*)dst + 4 * c, v);
-      else st_bf4((u16*)dst + 4 * c, v);
-    }
-  }
-}
-
-// W_s with its rows padded to whole 16 bytes (zeros), for a C that is not.
+// W_s with its rows padded to whole 16 bytes (zeros), for a C that is not: 16
+// bytes a thread, read at the alignment of their elements.
 template <class T>
-__global__ void __launch_bounds__(256) k_vocab_pad(int C, int Cq, const T* __restrict__ W, T* out) {
-  const size_t row = blockIdx.y;
-  for (int c = blockIdx.x * 256 + threadIdx.x; c < Cq; c += gridDim.x * 256)
-    out[row * Cq + c] = c < C ? W[row * C + c] : T(0);
+__global__ void __launch_bounds__(256) k_vocab_pad(int H, int C, int Cq, const T* __restrict__ W, T* out) {
+  constexpr int VEC = 16 / sizeof(T);
+  const int c = (blockIdx.x * 256 + threadIdx.x) * VEC, left = C - c;
+  if (left <= 0) return;
+  for (int row = blockIdx.y; row < H; row += gridDim.y) {
+    const T* src = W + (size_t)row * C + c;
+    uint4 x;
+    if (left >= VEC) {
+      __builtin_memcpy(&x, src, 16);
+    } else {
+      T t[VEC];
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) t[i] = i < left ? src[i] : T(0);
+      __builtin_memcpy(&x, t, 16);
+    }
+    *reinterpret_cast<uint4*>(out + (size_t)row * Cq + c) = x;
+  }
 }
 
-// The teacher's distribution over its words of a live row: q = softmax(t / T)
-// over the words that are there and have a logit above -inf.  A word that is
-// listed twice counts as the sum of its entries, at its first place, so that
-// the products' epilogues change each word once; the loss's sum of q ln q is
-// over the entries.  A wavefront per row; K at most kVocabMaxK.
-__global__ void __launch_bounds__(256) k_vocab_teacher(int C, int K, float invT,
-                                                       const int* __restrict__ rows,
-                                                       const int* __restrict__ live,
-                                                       const int* __restrict__ top_word,
-                                                       const float* __restrict__ top_logit,
-                                                       int* tword, float* tq, float2* tsum, int* err) {
-  constexpr int PER = kVocabMaxK / 64;
-  __shared__ int words[4][kVocabMaxK];
+// The teacher's distribution over its words of a live row, q = softmax(t / T)
+// over the words that are there and have a logit above -inf, the words in
+// ascending order and their ranges in the products' slots of words.  A word that
+// is listed twice counts as the sum of its entries, at its first place; the
+// loss's sum of q ln q is over the entries.  A wavefront per row; an entry's
+// place is the number of smaller ones (K at most kVocabMaxK).
+__global__ void __launch_bounds__(256) k_vocab_teacher(VocabNet v, const int* __restrict__ top_word,
+                                                       const float* __restrict__ top_logit, int* err) {
+  constexpr int PER = kVocabMaxK / 64, kNone = 0x7fffffff;
+  __shared__ int words[4][kVocabMaxK], sorted[4][kVocabMaxK];
   __shared__ float qs[4][kVocabMaxK];
-  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, row = blockIdx.x * 4 + w;
-  const int nl = *live;
-  if (row < nl) {
-    const size_t src = (size_t)rows[row] * K;
-    int id[PER];
-    float t[PER], m = -INFINITY;
-    bool bad = false;
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, row = blockIdx.x * 4 + w, K = v.K;
+  if (row >= *v.live) return;
+  const size_t src = (size_t)v.rows_list[row] * K, dst = (size_t)row * K;
+  const float invT = 1.f / v.temp;
+  int id[PER];
+  float t[PER], m = -INFINITY;
+  bool bad = false, nan = false;
 #pragma unroll
-    for (int k = 0; k < PER; ++k) {
-      const int j = lane + 64 * k;
-      id[k] = j < K ? top_word[src + j] : -1;
-      bad |= id[k] < -1 || id[k] >= C;
-      if (id[k] >= C) id[k] = -1;
-      t[k] = id[k] >= 0 ? top_logit[src + j] * invT : -INFINITY;
-      m = fmaxf(m, t[k]);
+  for (int k = 0; k < PER; ++k) {
+    const int j = lane + 64 * k;
+    const int x = j < K ? top_word[src + j] : -1;
+    bad |= x < -1 || x >= v.C;
+    id[k] = x >= 0 && x < v.C ? x : kNone;
+    t[k] = id[k] != kNone ? top_logit[src + j] * invT : -INFINITY;
+    nan |= t[k] != t[k];
+    m = fmaxf(m, t[k]);
+  }
+  if (bad) err[1] = 1;
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, kWave));
+  const bool some = m > -INFINITY || __any(nan);   // a NaN is not nothing
+  float sum = 0.f, q[PER], s = 0.f;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    q[k] = t[k] == -INFINITY ? 0.f : expf(t[k] - m);
+    sum += q[k];
+  }
+  sum = wave_sum(sum);
+  const float ls = logf(sum);
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    q[k] = some ? q[k] / sum : 0.f;
+    if (some && !(q[k] == 0.f)) s += q[k] * (t[k] - m - ls);
+    words[w][lane + 64 * k] = id[k];
+    qs[w][lane + 64 * k] = q[k];
+  }
+  s = wave_sum(s);
+  if (lane == 0) v.tsum[row] = make_float2(s, some ? 1.f : 0.f);
+  wave_lds_fence();
+  const int reach = (K + 63) / 64;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    if (k >= reach) break;
+    const int j = lane + 64 * k;
+    if (j >= K) continue;
+    int place = 0;
+    bool first = true;
+    float total = 0.f;
+    for (int i = 0; i < K; ++i) {
+      const int x = words[w][i];
+      const bool same = x == id[k], before = same && i < j;
+      place += x < id[k] || before;
+      first = first && !before;
+      total += same ? qs[w][i] : 0.f;
     }
-    if (bad) err[1] = 1;
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, kWave));
-    // nothing there: all -inf (a NaN among them is not nothing)
-    bool nan = false;
-#pragma unroll
-    for (int k = 0; k < PER; ++k) nan |= t[k] != t[k];
-    const bool some = m > -INFINITY || __any(nan);
-    float sum = 0.f, q[PER], s = 0.f;
-#pragma unroll
-    for (int k = 0; k < PER; ++k) {
-      q[k] = t[k] == -INFINITY ? 0.f : expf(t[k] - m);
-      sum += q[k];
+    sorted[w][place] = id[k];
+    v.tword[dst + place] = id[k];
+    v.tq[dst + place] = first && id[k] != kNone ? total : 0.f;
+  }
+  wave_lds_fence();
+  auto below = [&](long long word) {   // the row's words below this one
+    int lo = 0, hi = K;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (sorted[w][mid] < word) lo = mid + 1;
+      else hi = mid;
     }
-    sum = wave_sum(sum);
-    const float ls = logf(sum);
-#pragma unroll
-    for (int k = 0; k < PER; ++k) {
-      q[k] = some ? q[k] / sum : 0.f;
-      if (some && !(q[k] == 0.f)) s += q[k] * (t[k] - m - ls);
-      words[w][lane + 64 * k] = id[k];
-      qs[w][lane + 64 * k] = q[k];
-    }
-    s = wave_sum(s);
-    if (lane == 0) tsum[row] = make_float2(s, some ? 1.f : 0.f);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-#pragma unroll
-    for (int k = 0; k < PER; ++k) {
-      const int j = lane + 64 * k;
-      if (j >= K) continue;
-      bool first = true;
-      float total = 0.f;
-      for (int i = 0; i < K; ++i) {
-        const bool same = words[w][i] == id[k];
-        first = first && !(same && i < j);
-        total += same ? qs[w][i] : 0.f;
-      }
-      const size_t at = (size_t)row * K + j;
-      tword[at] = first ? id[k] : -1;
-      tq[at] = total;
-    }
+    return lo;
+  };
+  // the last tile's slots past C as well
+  const int slots = cdiv_dev(v.C, kVocabTile) * (kVocabTile / v.slot_words);
+  for (int k = lane; k < slots; k += 64) {
+    const long long a = (long long)k * v.slot_words;
+    v.trange[(size_t)k * v.rows + row] = below(a) | (uint32_t)below(a + v.slot_words) << 16;
   }
 }
 
 // A row's statistics joined over the slots, its loss, and what its dz is made
-// from.  64 rows a workgroup, sixteen wavefronts on every sixteenth slot each,
-// their sums added in their order.
+// from.  16 rows a workgroup, 64 lanes on every 64th slot (or teacher's word)
+// of each, their sums added in their order.
 //   CE = ln(sum exp(z - m)) + m - z_label
 //   KD = T^2 (sum q ln q + ln(sum exp((z - m) / T)) + sum q (m - z) / T)
 __global__ void __launch_bounds__(1024) k_vocab_join(VocabNet v, float* row_loss) {
-  __shared__ float sm[16][64], ss[16][64], st[16][64];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, row = blockIdx.x * 64 + lane;
+  __shared__ float sm[64][16], ss[64][16], st[64][16], sd[64][16];
+  const int i = threadIdx.x & 15, k0 = threadIdx.x >> 4, row = blockIdx.x * 16 + i;
   const int nl = *v.live;
-  if ((int)blockIdx.x * 64 >= nl) {
+  const float4 none = make_float4(INFINITY, 0.f, 0.f, 0.f);   // exp(z - inf): no dz
+  if ((int)blockIdx.x * 16 >= nl) {
     // the rest of the last tile of 256 rows
-    if (w == 0 && (int)blockIdx.x * 64 < cdiv_dev(nl, kVocabTile) * kVocabTile)
-      v.rowc[row] = f4zero();
+    if (k0 == 0 && (int)blockIdx.x * 16 < cdiv_dev(nl, kVocabTile) * kVocabTile) v.rowc[row] = none;
     return;
   }
   float m = -INFINITY;
-  for (int k = w; k < v.slots; k += 16) m = fmaxf(m, v.pm[(size_t)k * v.rows + row]);
-  sm[w][lane] = m;
+#pragma unroll 4
+  for (int k = k0; k < v.slots; k += 64) m = fmaxf(m, v.pm[(size_t)k * v.rows + row]);
+  sm[k0][i] = m;
   __syncthreads();
 #pragma unroll
-  for (int k = 0; k < 16; ++k) m = fmaxf(m, sm[k][lane]);
+  for (int k = 0; k < 64; ++k) m = fmaxf(m, sm[k][i]);
   const float mm = m == -INFINITY ? 0.f : m;
-  float s = 0.f, t = 0.f;
-  for (int k = w; k < v.slots; k += 16) {
+  float s = 0.f, t = 0.f, dot = 0.f;
+#pragma unroll 4
+  for (int k = k0; k < v.slots; k += 64) {
     const size_t at = (size_t)k * v.rows + row;
     const float d = (v.pm[at] - mm) * kLog2e;
     s += v.ps[at] * __builtin_amdgcn_exp2f(d);
     if (v.two) t += v.pt[at] * __builtin_amdgcn_exp2f(d / v.temp);
   }
-  ss[w][lane] = s;
-  st[w][lane] = t;
+  if (row < nl)
+    for (int j = k0; j < v.K; j += 64) {
+      const size_t at = (size_t)row * v.K + j;
+      const float q = v.tq[at];
+      if (q != 0.f) dot += q * (m - v.ztop[at]);   // a word that is not there has none
+    }
+  ss[k0][i] = s;
+  st[k0][i] = t;
+  sd[k0][i] = dot;
   __syncthreads();
-  if (w > 0) return;
-  s = 0.f;
-  t = 0.f;
-#pragma unroll
-  for (int k = 0; k < 16; ++k) {
-    s += ss[k][lane];
-    t += st[k][lane];
+  if (k0 > 0) return;
+  s = t = dot = 0.f;
+#pragma unroll 16
+  for (int k = 0; k < 64; ++k) {
+    s += ss[k][i];
+    t += st[k][i];
+    dot += sd[k][i];
   }
   if (!v.two) t = s;
   if (row >= nl) {
-    v.rowc[row] = f4zero();
+    v.rowc[row] = none;
     return;
   }
   float val = 0.f, has = 0.f;
-  const float a = v.K > 0 ? v.alpha : 0.f;
+  const float a = v.alpha;
   const int y = v.label[row];
   if (y >= 0 && a < 1.f) val = (1.f - a) * (logf(s) + (m - v.zlab[row]));
   if (v.K > 0) {
     const float2 q = v.tsum[row];
     has = q.y;
-    if (has != 0.f && a > 0.f) {
-      float dot = 0.f;
-      for (int j = 0; j < v.K; ++j) {
-        const size_t at = (size_t)row * v.K + j;
-        const float p = v.tq[at];
-        if (v.tword[at] >= 0 && p != 0.f) dot += p * (m - v.ztop[at]);
-      }
-      val += a * v.temp * v.temp * (q.x + logf(t) + dot / v.temp);
-    }
+    if (has != 0.f && a > 0.f) val += a * v.temp * v.temp * (q.x + logf(t) + dot / v.temp);
   }
   v.val[row] = val;
   if (row_loss) row_loss[v.rows_list[row]] = val;
@@ -263,16 +291,77 @@ __global__ void __launch_bounds__(1024) k_vocab_mean(const float* __restrict__ v
   }
 }
 
-// db_s of a piece: the groups' sums in order.
-__global__ void __launch_bounds__(256) k_vocab_db(int cols, int P, int group,
-                                                  const int* __restrict__ live,
-                                                  const float* __restrict__ dbp,
-                                                  const float* __restrict__ scal, float* db) {
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= cols) return;
+// dz from the z that the loss kept (in place in fp32), as vocab_rows16 forms it,
+// and its sums over 64 rows: 256 words x 64 rows a workgroup, a wavefront on
+// whole rows of 1 KB.
+template <class OUT>
+__global__ void __launch_bounds__(256) k_vocab_dz(VocabNet v) {
+  __shared__ float4 sums[4][64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, nl = *v.live;
+  const int c0 = blockIdx.x * 256, c = c0 + 4 * lane, r0 = blockIdx.y * 64;
+  if (r0 >= cdiv_dev(nl, kVocabTile) * kVocabTile) return;
+  const float invT = 1.f / v.temp;
+  float4 db = f4zero();
+#pragma unroll 4
+  for (int rr = 0; rr < 16; ++rr) {
+    const int row = __builtin_amdgcn_readfirstlane(r0 + 16 * w + rr);
+    const size_t at = (size_t)row * v.P + c;
+    float d[4] = {0.f, 0.f, 0.f, 0.f};
+    if (row < nl) {
+      const float4 z = ldg4(v.Z + at), k = v.rowc[row];
+      const float x[4] = {z.x - k.x, z.y - k.x, z.z - k.x, z.w - k.x};
+      const int lab = v.label[row];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        d[i] = k.y * __builtin_amdgcn_exp2f(x[i] * kLog2e);
+        if (v.two) d[i] += k.z * __builtin_amdgcn_exp2f(x[i] * (invT * kLog2e));
+        if (c + i == lab) d[i] -= k.w;
+      }
+      if (v.K > 0) {
+        const int s0 = c0 / v.slot_words, s1 = s0 + 256 / v.slot_words - 1;
+        const int lo = v.trange[(size_t)s0 * v.rows + row] & 0xffffu;
+        const int hi = v.trange[(size_t)s1 * v.rows + row] >> 16;
+        for (int j = lo; j < hi; ++j) {
+          const size_t t = (size_t)row * v.K + j;
+          const int word = v.tword[t];
+          const float q = v.distw * v.tq[t];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) d[i] -= c + i == word ? q : 0.f;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) d[i] = c + i < v.C ? d[i] : 0.f;
+    }
+    const float4 o = make_float4(d[0], d[1], d[2], d[3]);
+    if constexpr (sizeof(OUT) == 2) st_bf4((u16*)v.dZ + at, o);
+    else st4((float*)v.dZ + at, o);
+    db = add4(db, o);
+  }
+  sums[w][lane] = db;
+  __syncthreads();
+  if (w == 0)
+    st4(v.dbp + (size_t)blockIdx.y * v.P + c,
+        add4(add4(sums[0][lane], sums[1][lane]), add4(sums[2][lane], sums[3][lane])));
+}
+
+// db_s of a piece: 64 columns a workgroup, its wavefronts every sixteenth group,
+// their sums in order.
+__global__ void __launch_bounds__(1024) k_vocab_db(int cols, int P, int group,
+                                                   const int* __restrict__ live,
+                                                   const float* __restrict__ dbp,
+                                                   const float* __restrict__ scal, float* db) {
+  __shared__ float sums[16][64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
   const int G = cdiv_dev(*live, group);
   float s = 0.f;
-  for (int k = 0; k < G; ++k) s += dbp[(size_t)k * P + c];
+#pragma unroll 4
+  for (int k = w; k < G; k += 16) s += dbp[(size_t)k * P + c];   // P is a multiple of 256
+  sums[w][lane] = s;
+  __syncthreads();
+  if (w > 0 || c >= cols) return;
+  s = 0.f;
+#pragma unroll
+  for (int k = 0; k < 16; ++k) s += sums[k][lane];
   db[c] = s * *scal;
 }
 
@@ -287,25 +376,36 @@ __global__ void __launch_bounds__(256) k_vocab_dw(int H, int P, int cols, int S,
   vocab_store4(o, *o.scale, 0, row, c, s);
 }
 
-// dL/dh: live rows from the sums over parts of the vocabulary, the others 0.
-template <class OUT>
+// dL/dh: live rows from the sums over parts of the vocabulary, the others 0.  A
+// workgroup's four wavefronts take a row each, or a quarter of one row's parts
+// (WIDE: many parts, few rows), added in their order.
+template <class OUT, bool WIDE>
 __global__ void __launch_bounds__(256) k_vocab_dh(int n, int H, size_t part, int S,
                                                   const int* __restrict__ place,
                                                   const float* __restrict__ sums,
                                                   const float* __restrict__ scal, OUT* dh) {
-  const int q = H / 4, lane = threadIdx.x & 63;
-  const float w = *scal;
-  for (int i = blockIdx.x * 4 + (threadIdx.x >> 6); i < n; i += gridDim.x * 4) {
-    const int k = place[i];
-    for (int c = lane; c < q; c += 64) {
-      float4 v = f4zero();
-      if (k >= 0)
-        for (int z = 0; z < S; ++z) v = add4(v, ldg4(sums + z * part + (size_t)k * H + 4 * c));
-      v = make_float4(v.x * w, v.y * w, v.z * w, v.w * w);
-      if constexpr (sizeof(OUT) == 4) st4((float*)dh + (size_t)i * H + 4 * c, v);
-      else st_bf4((u16*)dh + (size_t)i * H + 4 * c, v);
-    }
+  __shared__ float4 quarter[WIDE ? 4 : 1][64];
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int i = WIDE ? blockIdx.y : blockIdx.y * 4 + w, c = (blockIdx.x * 64 + lane) * 4;
+  const int per = cdiv_dev(S, 4), z0 = WIDE ? min(w * per, S) : 0, z1 = WIDE ? min(z0 + per, S) : S;
+  if (!WIDE && i >= n) return;
+  const int k = place[i];
+  float4 v = f4zero();
+  if (k >= 0 && c < H) {
+    const float* p = sums + (size_t)k * H + c;
+#pragma unroll 8
+    for (int z = z0; z < z1; ++z) v = add4(v, ldg4(p + z * part));
   }
+  if constexpr (WIDE) {
+    quarter[w][lane] = v;
+    __syncthreads();
+    if (w > 0) return;
+    v = add4(add4(quarter[0][lane], quarter[1][lane]), add4(quarter[2][lane], quarter[3][lane]));
+  }
+  if (c >= H) return;
+  const float x = *scal;
+  const float o[4] = {v.x * x, v.y * x, v.z * x, v.w * x};
+  store_row<4>(dh + (size_t)i * H + c, o);
 }
 
 // Workspace: VocabNet with offsets as its pointers from base.
@@ -315,9 +415,12 @@ size_t vocab_net(const cavs_vocab* p, bool train, char* base, VocabNet& v) {
   v.H = p->H;
   v.C = p->C;
   v.K = p->K;
-  v.rows = (p->n + kVocabTile - 1) / kVocabTile * kVocabTile;
   v.hbf = p->h_type == CAVS_T_BF16;
   v.wbf = v.bf = p->w_type == CAVS_T_BF16;
+  // few rows have kernels that read no more of them than there can be
+  v.few = p->n <= kVocabFew;
+  const int tile = v.few ? kVocabFew : kVocabTile;
+  v.rows = (p->n + tile - 1) / tile * tile;
   v.alpha = p->K > 0 ? p->alpha : 0.f;
   v.temp = p->K > 0 ? p->temp : 1.f;
   v.two = p->K > 0 && p->temp != 1.f;
@@ -346,42 +449,87 @@ size_t vocab_net(const cavs_vocab* p, bool train, char* base, VocabNet& v) {
   v.tq = (float*)take(rows * K * 4);
   v.ztop = (float*)take(rows * K * 4);
   v.tsum = (float2*)take(K ? rows * 8 : 0);
+  v.slot_words = v.bf ? 128 : 64;
+  v.slots = (v.C + v.slot_words - 1) / v.slot_words;
+  // the last tile's wavefronts past C have slots too
+  const size_t slots = (size_t)((v.C + kVocabTile - 1) / kVocabTile) * (kVocabTile / v.slot_words);
+  v.trange = (uint32_t*)take(K ? slots * rows * 4 : 0);
   v.hp = take(rows * H * es);
   v.Cq = (v.C + vec - 1) / vec * vec;
-  const bool pad = v.Cq != v.C;
+  // the loss of few rows reads W_s as it is, the gradients do not
+  const bool pad = v.Cq != v.C && (train || !v.few);
+  v.pad = pad;
   char* wq = take(pad ? H * (size_t)v.Cq * es : 0);
   v.Ws = pad ? wq : p->Ws;
   v.ldw = v.Cq;
-  v.slot_words = v.bf ? 128 : 64;
-  v.slots = (v.C + v.slot_words - 1) / v.slot_words;
-  // a slot more than joined: the last tile's wavefronts past C write theirs
-  const size_t stat = (size_t)((v.C + kVocabTile - 1) / kVocabTile) * (kVocabTile / v.slot_words) * rows * 4;
+  const size_t stat = slots * rows * 4;
   v.pm = (float*)take(stat);
   v.ps = (float*)take(stat);
   v.pt = (float*)take(v.two ? stat : 0);
   if (!train) return o;
   // Pieces: dZ of about 256 MB, of equal width, at least 2048 words.  The last
-  // ones' tiles are then as full as the first ones'.
+  // ones' tiles are then as full as the first ones'.  In bf16 two of them: the
+  // next piece's dz is formed while one is multiplied.
   const size_t words = std::max<size_t>(((size_t)256 << 20) / (rows * es), 2048);
   const size_t pieces = ((size_t)v.C + words - 1) / words;
   v.P = (int)(((v.C + pieces - 1) / pieces + kVocabTile - 1) / kVocabTile * kVocabTile);
-  v.dZ = take(rows * v.P * es);
+  v.dz_half = v.bf && v.P < v.C ? rows * v.P * es : 0;
+  v.dZ = take(rows * v.P * es + v.dz_half);
+  // z is kept, and not formed twice, where it is one piece: in fp32 always (3 ps a
+  // value there and back, its product 6 at H = 512); in bf16 up to half the
+  // Infinity Cache, and from H = 1024 on, where the product takes longer (4096
+  // rows, 31 000 words: 755 us without and 788 with at H = 512, 1288 and 1214 at
+  // 1024, 2325 and 2058 at 2048).
+  const bool keep = v.P >= v.C && (!v.bf || v.H >= 1024 || rows * v.P * 4 <= kKeepBytes);
+  v.Z = keep ? (float*)(v.bf ? take(rows * v.P * 4) : (char*)v.dZ) : nullptr;
+  v.keep = keep;
   v.db_rows = 64;
   v.dbp = (float*)take(rows / v.db_rows * v.P * 4);
-  // The gradient products are split over their contraction until a workgroup
-  // per CU is there, each part at least four stages deep and the parts of dh
-  // at most 64 MB (dW's: 128).
-  const int tile = v.bf ? 256 : 128, depth = v.bf ? 64 : 32, want = v.bf ? 256 : 512;
-  auto parts = [&](int tiles, int stages, size_t bytes, size_t cap) {
-    int S = std::max(1, std::min({want / std::max(tiles, 1), stages / 4,
-                                  (int)std::min<size_t>(cap / std::max<size_t>(bytes, 1), 64)}));
-    return (stages + (stages + S - 1) / S - 1) / ((stages + S - 1) / S);   // no part without a stage
-  };
-  auto tiles = [&](int x) { return (x + tile - 1) / tile; };
-  const int width = std::min(v.P, v.C);
-  v.Sh = parts(tiles(v.H) * tiles(v.n), (width + depth - 1) / depth, rows * H * 4, (size_t)64 << 20);
+  // The gradient products split their contraction (Sw, Sh parts, summed
+  // afterwards) as far as it shortens the launch; each part costs its way to
+  // memory and back.  Times in stages of a tile that has a CU for itself, 1.6 us
+  // of either type, or 6.4 MB of traffic.
+  const int side = v.bf ? 256 : 128, depth = v.bf ? 64 : 32;
+  auto tiles = [&](int x) { return (x + side - 1) / side; };
+  auto whole = [](int stages, int S) { return (stages + S - 1) / S; };   // stages of a part
+  const int width = std::min(v.P, v.C), tw = tiles(v.H) * tiles(width), th = tiles(v.H) * tiles(v.n);
+  const int kw = whole(v.n, depth), kh = whole(width, depth);
+  const double wmb = H * (double)v.P * 4e-6, hmb = rows * (double)H * 4e-6;
+  auto w_ok = [&](int S) { return S == 1 || (whole(kw, S) >= 4 && S * wmb <= 128); };
+  auto h_ok = [&](int S) { return S == 1 || (whole(kh, S) >= 4 && S * hmb <= 64); };
+  auto w_cost = [&](int S) { return S > 1 ? 2 * S * wmb / 6.4 + 3 : 0; };
+  auto h_cost = [&](int S) { return 2 * S * hmb / 6.4; };
+  int bw = 1, bh = 1;
+  if (v.bf && !v.few) {
+    // One launch, longer items first: it ends about a shorter item after the
+    // CUs' mean load.  With pieces the next one's dz follows, in short items.
+    const double dz = v.H / 64 + 8., more = v.P < v.C ? dz * tiles(v.n) * tiles(width) : 0.;
+    const double load = ((double)tw * kw + (double)th * kh + more) / 256;
+    double best = 1e30;
+    for (int sw : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64})
+      for (int sh : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+        if (!w_ok(sw) || !h_ok(sh)) break;
+        const double iw = whole(kw, sw), ih = whole(kh, sh), last = more > 0. ? dz : std::min(iw, ih);
+        const double t = std::max({load + last, iw, ih}) + w_cost(sw) + h_cost(sh);
+        if (t < best) best = t, bw = sw, bh = sh;
+      }
+  } else {
+    // One after the other, two workgroups a CU: rounds of 512, the last one
+    // faster if it leaves each its CU.
+    auto time = [&](int items, int stages) {
+      const int rest = items % 512;
+      return stages * (2. * (items / 512) + (rest == 0 ? 0. : rest <= 256 ? 1.1 : 2.));
+    };
+    double best_w = 1e30, best_h = 1e30;
+    for (int S = 1; S <= 64; ++S) {
+      const double w = time(tw * S, whole(kw, S)) + w_cost(S), h = time(th * S, whole(kh, S)) + h_cost(S);
+      if (w_ok(S) && w < best_w) best_w = w, bw = S;
+      if (h_ok(S) && h < best_h) best_h = h, bh = S;
+    }
+  }
+  v.Sw = whole(kw, whole(kw, bw));   // no part without a stage
+  v.Sh = whole(kh, whole(kh, bh));
   v.hpart = (float*)take((size_t)v.Sh * rows * H * 4);
-  v.Sw = parts(tiles(v.H) * tiles(width), v.rows / depth, H * v.P * 4, (size_t)128 << 20);
   v.wpart = (float*)take(v.Sw > 1 ? (size_t)v.Sw * H * v.P * 4 : 0);
   return o;
 }
@@ -415,17 +563,30 @@ cavs_status vocab_args(cavs_ctx* ctx, const cavs_vocab* p) {
 }
 
 template <class IN, class OUT>
-void pack(const VocabNet& v, hipStream_t s) {
-  CAVS_LAUNCH("k_vocab_pack", (k_vocab_pack<IN, OUT>), dim3(std::min(v.rows / 4, 8192)), dim3(256), 0, s,
-              v.H, (const IN*)v.h, v.rows_list, v.live, (OUT*)v.hp);
+void rows(const VocabNet& v, const cavs_vocab* p, float* row_loss, int* err, hipStream_t s) {
+  const int R = std::max(16, cdiv(v.n, 512));
+  CAVS_LAUNCH("k_vocab_rows", (k_vocab_rows<IN, OUT>), dim3(cdiv(v.n, R)), dim3(256), 0, s, v, R, p->label,
+              row_loss, err);
+}
+
+template <class OUT>
+void dh_sum(const VocabNet& v, OUT* dh, hipStream_t s) {
+  const size_t part = (size_t)v.rows * v.H;
+  const int gx = cdiv(v.H, 256);
+  if (v.Sh >= 8)
+    CAVS_LAUNCH("k_vocab_dh", (k_vocab_dh<OUT, true>), dim3(gx, v.n), dim3(256), 0, s, v.n, v.H, part, v.Sh,
+                v.place, v.hpart, v.scal, dh);
+  else
+    CAVS_LAUNCH("k_vocab_dh", (k_vocab_dh<OUT, false>), dim3(gx, cdiv(v.n, 4)), dim3(256), 0, s, v.n, v.H, part,
+                v.Sh, v.place, v.hpart, v.scal, dh);
 }
 
 }  // namespace
 
 VocabEp vocab_ep(const VocabNet& v, int col0) {
   return VocabEp{v.C,   col0,   v.K,  v.rows, v.two,  1.f / v.temp, v.distw, v.live,
-                 v.bs,  v.label, v.tword, v.tq, v.pm, v.ps, v.pt, v.zlab, v.ztop, v.rowc,
-                 v.dZ,  v.P,  v.dbp};
+                 v.bs,  v.label, v.tword, v.tq, v.trange, v.pm, v.ps, v.pt, v.zlab, v.ztop, v.Z, v.rowc,
+                 v.P > 0 ? vocab_dz_at(v, col0) : nullptr, v.P, v.dbp};
 }
 
 size_t vocab_ws_bytes(const cavs_vocab* p, bool train) {
@@ -457,56 +618,64 @@ cavs_status vocab_run(cavs_ctx* ctx, const cavs_vocab* p, float* loss, float* ro
     return CAVS_OK;
   }
   VocabNet v;
-  const size_t need = vocab_net(p, train, nullptr, v);
+  const size_t need = vocab_net(p, train, (char*)ws, v);
   if (!ws || ws_bytes < need)
     return fail(ctx, CAVS_ERR_WORKSPACE, "workspace too small: %zu < %zu", ws_bytes, need);
   if (!aligned16(ws)) return fail(ctx, CAVS_ERR_ARG, "ws must be aligned to 16 bytes");
-  vocab_net(p, train, (char*)ws, v);
 
-  CAVS_LAUNCH("k_vocab_rows", k_vocab_rows, dim3(1), dim3(1024), 0, s, v.n, v.C, p->label, v.rows_list,
-              v.place, v.label, v.live, v.unit, v.scal, row_loss, v.zrow, ctx->dev_err_dev);
-  if (v.hbf) v.bf ? pack<u16, u16>(v, s) : pack<u16, float>(v, s);
-  else v.bf ? pack<float, u16>(v, s) : pack<float, float>(v, s);
-  if (v.Cq != v.C) {
-    const dim3 grid(std::min(cdiv(v.Cq, 256), 64), v.H);
+  int* err = ctx->dev_err_dev;
+  if (v.hbf) v.bf ? rows<u16, u16>(v, p, row_loss, err, s) : rows<u16, float>(v, p, row_loss, err, s);
+  else v.bf ? rows<float, u16>(v, p, row_loss, err, s) : rows<float, float>(v, p, row_loss, err, s);
+  if (v.pad) {
+    const dim3 grid(cdiv(v.Cq, 256 * (v.bf ? 8 : 4)), v.H);
     if (v.bf)
-      CAVS_LAUNCH("k_vocab_pad", k_vocab_pad<u16>, grid, dim3(256), 0, s, v.C, v.Cq, (const u16*)p->Ws,
+      CAVS_LAUNCH("k_vocab_pad", k_vocab_pad<u16>, grid, dim3(256), 0, s, v.H, v.C, v.Cq, (const u16*)p->Ws,
                   (u16*)v.Ws);
     else
-      CAVS_LAUNCH("k_vocab_pad", k_vocab_pad<float>, grid, dim3(256), 0, s, v.C, v.Cq,
+      CAVS_LAUNCH("k_vocab_pad", k_vocab_pad<float>, grid, dim3(256), 0, s, v.H, v.C, v.Cq,
                   (const float*)p->Ws, (float*)v.Ws);
   }
   if (v.K > 0)
-    CAVS_LAUNCH("k_vocab_teacher", k_vocab_teacher, dim3(v.rows / 4), dim3(256), 0, s, v.C, v.K,
-                1.f / v.temp, v.rows_list, v.live, p->top_word, p->top_logit, v.tword, v.tq, v.tsum,
-                ctx->dev_err_dev);
-  v.bf ? vocab_bf_loss(v, s) : vocab_x3_loss(v, s);
-  CAVS_LAUNCH("k_vocab_join", k_vocab_join, dim3(v.rows / 64), dim3(1024), 0, s, v, row_loss);
+    CAVS_LAUNCH("k_vocab_teacher", k_vocab_teacher, dim3(v.rows / 4), dim3(256), 0, s, v, p->top_word,
+                p->top_logit, err);
+  v.bf ? vocab_bf_loss(v, p->Ws, s) : vocab_x3_loss(v, p->Ws, s);
+  CAVS_LAUNCH("k_vocab_join", k_vocab_join, dim3(v.rows / 16), dim3(1024), 0, s, v, row_loss);
   CAVS_LAUNCH("k_vocab_mean", k_vocab_mean, dim3(1), dim3(1024), 0, s, v.val, v.live, loss);
   if (train) {
-    for (int col0 = 0; col0 < v.C; col0 += v.P) {
-      const int cols = std::min(v.P, v.C - col0);
-      v.bf ? vocab_bf_dz(v, col0, cols, s) : vocab_x3_dz(v, col0, cols, s);
+    auto width = [&](int col0) { return std::max(0, std::min(v.P, v.C - col0)); };
+    auto db = [&](int col0) {
       if (dbs)
-        CAVS_LAUNCH("k_vocab_db", k_vocab_db, dim3(cdiv(cols, 256)), dim3(256), 0, s, cols, v.P,
+        CAVS_LAUNCH("k_vocab_db", k_vocab_db, dim3(cdiv(width(col0), 64)), dim3(1024), 0, s, width(col0), v.P,
                     v.db_rows, v.live, v.dbp, v.scal, dbs + col0);
+    };
+    for (int col0 = 0; col0 < v.C; col0 += v.P) {
+      const int cols = width(col0), next = width(col0 + v.P);
+      if (v.keep) {
+        const dim3 grid(v.P / 256, v.rows / 64);
+        if (v.bf) CAVS_LAUNCH("k_vocab_dz", k_vocab_dz<u16>, grid, dim3(256), 0, s, v);
+        else CAVS_LAUNCH("k_vocab_dz", k_vocab_dz<float>, grid, dim3(256), 0, s, v);
+      } else if (!v.bf) {
+        vocab_x3_dz(v, col0, cols, s);
+      } else if (col0 == 0) {
+        vocab_bf_dz(v, col0, cols, s);
+      }
+      if (!v.bf || col0 == 0) db(col0);
       char* at = (char*)dWs + (size_t)col0 * (v.wbf ? 2 : 4);
       const VocabOut out{at, v.C, 0, v.H, cols, v.wbf, 0, v.scal};
       const VocabOut sums{v.wpart, v.P, (size_t)v.H * v.P, v.H, cols, 0, 0, nullptr};
       const VocabOut& o = v.Sw > 1 ? sums : out;
-      v.bf ? vocab_bf_dw(v, col0, cols, o, s) : vocab_x3_dw(v, col0, cols, o, s);
+      if (v.bf) {
+        vocab_bf_grads(v, col0, cols, next, o, s);
+        if (next > 0) db(col0 + v.P);
+      } else {
+        vocab_x3_dw(v, col0, cols, o, s);
+        vocab_x3_dh(v, col0, cols, s);
+      }
       if (v.Sw > 1)
         CAVS_LAUNCH("k_vocab_dw", k_vocab_dw, dim3(cdiv(cols, 1024), v.H), dim3(256), 0, s, v.H, v.P, cols,
                     v.Sw, v.wpart, out);
-      v.bf ? vocab_bf_dh(v, col0, cols, s) : vocab_x3_dh(v, col0, cols, s);
     }
-    const dim3 grid(std::min(cdiv(v.n, 4), 8192));
-    if (v.hbf)
-      CAVS_LAUNCH("k_vocab_dh", k_vocab_dh<u16>, grid, dim3(256), 0, s, v.n, v.H, (size_t)v.rows * v.H, v.Sh,
-                  v.place, v.hpart, v.scal, (u16*)dh);
-    else
-      CAVS_LAUNCH("k_vocab_dh", k_vocab_dh<float>, grid, dim3(256), 0, s, v.n, v.H, (size_t)v.rows * v.H,
-                  v.Sh, v.place, v.hpart, v.scal, (float*)dh);
+    v.hbf ? dh_sum(v, (u16*)dh, s) : dh_sum(v, (float*)dh, s);
   }
   CAVS_LAUNCH_CHECK(ctx);
   return CAVS_OK;

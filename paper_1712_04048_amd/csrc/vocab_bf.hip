@@ -120,6 +120,8 @@ struct ColsOp {
 struct Live {
   const int* live;
   int what;
+  // uniform, which the compiler does not see past another product's copies
+  __device__ int tiles(int of) const { return cdiv_dev(__builtin_amdgcn_readfirstlane(*live), of); }
 };
 
 // A workgroup of WA x WB wavefronts: A rows 16 FA WA, B rows 16 FB WB, each
@@ -133,75 +135,106 @@ struct Shape {
 };
 
 constexpr int kBand = 8;
-template <class SH, class OA, class OB, class EP>
-__global__ void __launch_bounds__(SH::T, 2) k_vocab_bf(OA oa, OB ob, EP ep, Live lv, int ta, int tb,
-                                                       int K, int kchunk, int slices) {
-  constexpr int FA = SH::FA, FB = SH::FB, S = SH::S;
-  __shared__ __attribute__((aligned(16))) char lds[SH::kBytes];
-  if (lv.what == 1) tb = cdiv_dev(*lv.live, SH::BB);
-  if (lv.what == 2) K = min(K, cdiv_dev(*lv.live, kKB) * kKB);
-  // bands of eight B tiles, a band's A tiles one after the other, a contiguous
-  // eighth to each XCD
-  const int item = xcd_item(blockIdx.x, ta * tb * slices);
-  if (item < 0) return;
-  const int zi = item / (ta * tb), it = item % (ta * tb);
-  const int band = it / (kBand * ta), in = it % (kBand * ta), bw = min(kBand, tb - band * kBand);
-  const int a0 = in / bw * SH::BA, b0 = (band * kBand + in % bw) * SH::BB;
-  const int klo = zi * kchunk, nst = max(0, (min(K, klo + kchunk) - klo + kKB - 1) / kKB);
 
-  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, r = lane & 15;
-  const int w = __builtin_amdgcn_readfirstlane(tid >> 6), wa = w % SH::WA, wb = w / SH::WA;
-  typename OA::template Tile<SH::BA, SH::T> la;
-  typename OB::template Tile<SH::BB, SH::T> lb;
-  typename OA::template Frag<SH::BA> fa;
-  typename OB::template Frag<SH::BB> fb;
-  la.init(oa, a0, tid);
-  lb.init(ob, b0, tid);
-  fa.init(wa * 16 * FA, g, r);
-  fb.init(wb * 16 * FB, g, r);
-  v4f acc[FA][FB];
-  zero_acc(acc);
-  constexpr int kCopies = decltype(la)::kCopies + decltype(lb)::kCopies;
-  const uint32_t dst = __builtin_amdgcn_readfirstlane(
-      lds_addr_of(reinterpret_cast<const float*>(lds)) + 1024u * w);
-  auto issue = [&](int st) {
-    const uint32_t d = dst + (st % S) * SH::kStage;
-    la.issue(klo + st * kKB, d);
-    lb.issue(klo + st * kKB, d + SH::BA * 128);
-  };
-#pragma unroll
-  for (int st = 0; st < S - 1; ++st)
-    if (st < nst) issue(st);
-  for (int st = 0; st < nst; ++st) {
-    // this stage has landed and the one before it has been read, everywhere
-    if (st + S - 2 < nst) wait_vmcnt_lgkm0<(S - 2) * kCopies>();
-    else wait_vmcnt_lgkm0<0>();
-    barrier_nofence();
-    if (st + S - 1 < nst) issue(st + S - 1);
-    const char* A = lds + (st % S) * SH::kStage;
-    const char* B = A + SH::BA * 128;
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      bf16x8 a[FA], b[FB];
-#pragma unroll
-      for (int f = 0; f < FB; ++f) b[f] = fb.read(B, kk, f);
-#pragma unroll
-      for (int f = 0; f < FA; ++f) a[f] = fa.read(A, kk, f);
-#pragma unroll
-      for (int i = 0; i < FA; ++i)
-#pragma unroll
-        for (int j = 0; j < FB; ++j) acc[i][j] = mfma_bf16_16x16x32(a[i], b[j], acc[i][j]);
+// One product: A rows ta tiles, B rows tb tiles, the contraction in `slices`
+// parts of kchunk.
+template <class SH, class OA, class OB, class EP>
+struct Product {
+  OA oa;
+  OB ob;
+  EP ep;
+  Live lv;
+  int ta, tb, K, kchunk, slices;
+
+  Product(OA a, OB b, EP e, Live l, int ma, int mb, int K_, int kchunk_)
+      : oa(a), ob(b), ep(e), lv(l), ta(cdiv(ma, SH::BA)), tb(cdiv(mb, SH::BB)), K(K_), kchunk(kchunk_),
+        slices(cdiv(K_, kchunk_)) {}
+  int grid() const { return xcd_grid(ta * tb * slices); }
+
+  // Workgroup `at` of XCD x among this product's, or at less their number and
+  // false.  A contiguous eighth of the items to each XCD, in bands of eight B
+  // tiles, a band's A tiles one after the other.
+  __device__ __forceinline__ bool take(int x, int& at, char* lds) const {
+    at = __builtin_amdgcn_readfirstlane(at);   // uniform, as in Live
+    const int tb_ = lv.what == 1 ? lv.tiles(SH::BB) : tb;
+    const int items = ta * tb_ * slices, per = (items + 7) / 8, item = x * per + at;
+    if (at >= per) {
+      at -= per;
+      return false;
     }
+    if (item < items) {
+      const int zi = item / (ta * tb_), it = item % (ta * tb_);
+      const int band = it / (kBand * ta), in = it % (kBand * ta), bw = min(kBand, tb_ - band * kBand);
+      run(lds, zi, in / bw * SH::BA, (band * kBand + in % bw) * SH::BB);
+    }
+    return true;
   }
-  ep.template operator()<SH>(lds, zi, a0 + wa * 16 * FA, b0 + wb * 16 * FB, w, g, r, acc);
+
+  __device__ __forceinline__ void run(char* lds, int zi, int a0, int b0) const {
+    constexpr int FA = SH::FA, FB = SH::FB, S = SH::S;
+    const int end = lv.what == 2 ? min(K, lv.tiles(kKB) * kKB) : K;
+    const int klo = __builtin_amdgcn_readfirstlane(zi * kchunk);
+    const int nst = __builtin_amdgcn_readfirstlane(max(0, (min(end, klo + kchunk) - klo + kKB - 1) / kKB));
+    const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, r = lane & 15;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6), wa = w % SH::WA, wb = w / SH::WA;
+    typename OA::template Tile<SH::BA, SH::T> la;
+    typename OB::template Tile<SH::BB, SH::T> lb;
+    typename OA::template Frag<SH::BA> fa;
+    typename OB::template Frag<SH::BB> fb;
+    la.init(oa, a0, tid);
+    lb.init(ob, b0, tid);
+    fa.init(wa * 16 * FA, g, r);
+    fb.init(wb * 16 * FB, g, r);
+    v4f acc[FA][FB];
+    zero_acc(acc);
+    constexpr int kCopies = decltype(la)::kCopies + decltype(lb)::kCopies;
+    const uint32_t dst = __builtin_amdgcn_readfirstlane(
+        lds_addr_of(reinterpret_cast<const float*>(lds)) + 1024u * w);
+    auto issue = [&](int st) {
+      const uint32_t d = __builtin_amdgcn_readfirstlane(dst + (st % S) * SH::kStage);
+      la.issue(klo + st * kKB, d);
+      lb.issue(klo + st * kKB, d + SH::BA * 128);
+    };
+#pragma unroll
+    for (int st = 0; st < S - 1; ++st)
+      if (st < nst) issue(st);
+    for (int st = 0; st < nst; ++st) {
+      // this stage has landed and the one before it has been read, everywhere
+      if (st + S - 2 < nst) wait_vmcnt_lgkm0<(S - 2) * kCopies>();
+      else wait_vmcnt_lgkm0<0>();
+      barrier_nofence();
+      if (st + S - 1 < nst) issue(st + S - 1);
+      const char* A = lds + (st % S) * SH::kStage;
+      const char* B = A + SH::BA * 128;
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        bf16x8 a[FA], b[FB];
+#pragma unroll
+        for (int f = 0; f < FB; ++f) b[f] = fb.read(B, kk, f);
+#pragma unroll
+        for (int f = 0; f < FA; ++f) a[f] = fa.read(A, kk, f);
+#pragma unroll
+        for (int i = 0; i < FA; ++i)
+#pragma unroll
+          for (int j = 0; j < FB; ++j) acc[i][j] = mfma_bf16_16x16x32(a[i], b[j], acc[i][j]);
+      }
+    }
+    ep.template operator()<SH>(zi, a0 + wa * 16 * FA, b0 + wb * 16 * FB, g, r, acc);
+  }
+};
+
+// One or more independent products, the workgroups of the first ones first.
+template <class SH, class... P>
+__global__ void __launch_bounds__(SH::T, 2) k_vocab_bf(P... p) {
+  __shared__ __attribute__((aligned(16))) char lds[SH::kBytes];
+  const int x = blockIdx.x & 7;
+  int at = blockIdx.x >> 3;
+  (void)(p.take(x, at, lds) || ...);
 }
 
-template <class SH, class OA, class OB, class EP>
-void product(const char* name, OA oa, OB ob, EP ep, Live lv, int ma, int mb, int K, int kchunk,
-             hipStream_t s) {
-  const int ta = cdiv(ma, SH::BA), tb = cdiv(mb, SH::BB), slices = cdiv(K, kchunk);
-  CAVS_LAUNCH(name, (k_vocab_bf<SH, OA, OB, EP>), dim3(xcd_grid(ta * tb * slices)), dim3(SH::T), 0, s,
-              oa, ob, ep, lv, ta, tb, K, kchunk, slices);
+template <class SH, class... P>
+void launch(const char* name, hipStream_t s, P... p) {
+  CAVS_LAUNCH(name, (k_vocab_bf<SH, P...>), dim3((p.grid() + ...)), dim3(SH::T), 0, s, p...);
 }
 
 // Words are the tile's A rows: lane (g, r) holds words 16 f + 4 g .. + 3 of its
@@ -210,30 +243,23 @@ template <bool LOSS, bool TEACH>
 struct BfVocab {
   VocabEp e;
   template <class SH>
-  __device__ void operator()(char* lds, int, int a, int b, int w, int g, int r,
-                             const v4f (&acc)[SH::FA][SH::FB]) const {
+  __device__ void operator()(int, int a, int b, int g, int r, const v4f (&acc)[SH::FA][SH::FB]) const {
     constexpr int NC = 16 * SH::FA, NV = NC / 4;
-    static_assert(SH::T / 64 * kSlabFloats<NC> * 4 <= SH::kBytes, "slabs fit the stages' LDS");
-    static_assert(LOSS || NC % 64 == 0, "whole lanes of column sums");
     const int a0 = e.col0 + a;
     auto col = [](int i, int gg) { return 16 * (i >> 2) + 4 * gg + (i & 3); };
-    float bias[NV], db[NC / 64] = {};
+    float bias[NV], db[NV] = {};
     vocab_bias(e, a0, g, col, bias);
-    if (!LOSS || TEACH) __syncthreads();   // the slabs take the stages' place
-    float* slab = reinterpret_cast<float*>(lds) + w * kSlabFloats<NC>;
     const int live = *e.live;
 #pragma unroll
     for (int f = 0; f < SH::FB; ++f) {
       float z[NV];
 #pragma unroll
       for (int i = 0; i < NV; ++i) z[i] = acc[i >> 2][f][i & 3] + bias[i];
-      vocab_rows16<LOSS, TEACH, u16, NC>(e, z, col, b + 16 * f, 1, a0, a0 / NC, live, slab, db);
+      const int row = b + 16 * f + r;
+      vocab_rows16<LOSS, TEACH, u16, NC>(e, z, col, row, a0, a0 / NC, (size_t)(a0 / NC) * e.rows + row,
+                                         live, db);
     }
-    if (!LOSS) {
-#pragma unroll
-      for (int k = 0; k < NC / 64; ++k)
-        e.dbp[(size_t)(b / (16 * SH::FB)) * e.ldz + a + (threadIdx.x & 63) + 64 * k] = db[k];
-    }
+    if (!LOSS) vocab_db<NC>(e, db, col, a0, b / (16 * SH::FB));
   }
 };
 
@@ -241,8 +267,7 @@ struct BfVocab {
 struct BfOut {
   VocabOut o;
   template <class SH>
-  __device__ void operator()(char*, int z, int a, int b, int, int g, int r,
-                             const v4f (&acc)[SH::FA][SH::FB]) const {
+  __device__ void operator()(int z, int a, int b, int g, int r, const v4f (&acc)[SH::FA][SH::FB]) const {
     const float w = o.scale ? *o.scale : 1.f;
 #pragma unroll
     for (int j = 0; j < SH::FB; ++j)
@@ -253,41 +278,148 @@ struct BfOut {
   }
 };
 
-using Big = Shape<2, 4, 8, 4, 2>;    // 256 x 256, eight wavefronts, 128 KB
+// The loss over at most 64 rows: bound by reading W_s, so a workgroup takes
+// every row of 128 words (four wavefronts of 32 x 64) and keeps two stages of
+// its columns in flight in registers.  They come from W_s as it is, whatever C
+// is: a 16-byte load needs no more than the alignment of its elements, where
+// the copies to LDS want four bytes (padding 50 001 columns took 53 of 140 us).
+constexpr int kFewRows = kVocabFew, kFewWords = 128;
+template <bool TEACH>
+__global__ void __launch_bounds__(256, 2) k_vocab_few(VocabEp e, const u16* __restrict__ W,
+                                                      const u16* __restrict__ hp, int H) {
+  constexpr int FA = 2, FB = 4, kA = kFewWords * 128, kB = kFewRows * 128;
+  __shared__ __attribute__((aligned(16))) char lds[2][kA + kB];
+  __shared__ float stats[3][4][kFewRows];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g = lane >> 4, r = lane & 15;
+  const int a0 = blockIdx.x * kFewWords, C = e.C;
+  const size_t end = (size_t)H * C;   // at least 64 values
+  // LDS as ColsOp and RowsOp have it
+  int ka[4], ca[4];
+  const u16* hb[2];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int at = i * 256 + tid, q = at & 15, k = at >> 4, s = (k & 3) | ((k >> 3) & 1) << 2;
+    ka[i] = k;
+    ca[i] = a0 + 16 * ((q >> 1) ^ s) + 8 * (q & 1);
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int row = (i * 256 + tid) >> 3;
+    hb[i] = hp + (size_t)row * H + 8 * ((tid & 7) ^ (row & 7));
+  }
+  struct Stage {
+    uint4 a[4], b[2];
+  } st[2];
+  auto load = [&](Stage& x, int k0) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x.a[i] = vocab_load8(W, (size_t)(k0 + ka[i]) * C + ca[i], end);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) x.b[i] = *reinterpret_cast<const uint4*>(hb[i] + k0);
+  };
+  ColsOp::Frag<kFewWords> fa;
+  RowsOp::Frag<kFewRows> fb;
+  fa.init(32 * w, g, r);
+  fb.init(0, g, r);
+  v4f acc[FA][FB];
+  zero_acc(acc);
+  load(st[0], 0);
+  load(st[1], min(kKB, H - kKB));
+  for (int k0 = 0; k0 < H; k0 += 2 * kKB) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      if (k0 + s * kKB >= H) break;
+      char* L = lds[s];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(L + 16 * (i * 256 + tid)) = st[s].a[i];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) *reinterpret_cast<uint4*>(L + kA + 16 * (i * 256 + tid)) = st[s].b[i];
+      __syncthreads();   // the other buffer's readers are past this one's barrier
+      load(st[s], min(k0 + (s + 2) * kKB, H - kKB));   // past the end: the last stage, unused
+      __builtin_amdgcn_sched_barrier(0);   // the loads go out before these products
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        bf16x8 a[FA], b[FB];
+#pragma unroll
+        for (int f = 0; f < FA; ++f) a[f] = fa.read(L, kk, f);
+#pragma unroll
+        for (int f = 0; f < FB; ++f) b[f] = fb.read(L + kA, kk, f);
+#pragma unroll
+        for (int i = 0; i < FA; ++i)
+#pragma unroll
+          for (int j = 0; j < FB; ++j) acc[i][j] = mfma_bf16_16x16x32(a[i], b[j], acc[i][j]);
+      }
+    }
+  }
+  vocab_few_end<TEACH, kFewWords>(e, stats, a0, [&](int i, int f) { return acc[i >> 2][f][i & 3]; });
+}
 
-template <bool LOSS>
-void logits(const char* name, const VocabNet& v, int col0, int cols, hipStream_t s) {
-  const ColsOp w{(const u16*)v.Ws + col0, v.ldw, v.Cq - col0};
-  const RowsOp h{(const u16*)v.hp, v.H, v.rows, v.H};
-  const VocabEp e = vocab_ep(v, col0);
-  const Live lv{v.live, 1};
-  if (v.K > 0) product<Big>(name, w, h, BfVocab<LOSS, true>{e}, lv, cols, v.rows, v.H, v.H, s);
-  else product<Big>(name, w, h, BfVocab<LOSS, false>{e}, lv, cols, v.rows, v.H, v.H, s);
+using Big = Shape<2, 4, 8, 4, 2>;    // 256 x 256, eight wavefronts, 128 KB
+using Few = Shape<4, 1, 4, 4, 2>;    // 256 x 64, four wavefronts, 80 KB: two share a CU
+
+template <bool LOSS, bool TEACH>
+using Logits = Product<Big, ColsOp, RowsOp, BfVocab<LOSS, TEACH>>;
+template <bool LOSS, bool TEACH>
+Logits<LOSS, TEACH> logits(const VocabNet& v, int col0, int cols) {
+  return {ColsOp{(const u16*)v.Ws + col0, v.ldw, v.Cq - col0}, RowsOp{(const u16*)v.hp, v.H, v.rows, v.H},
+          BfVocab<LOSS, TEACH>{vocab_ep(v, col0)}, Live{v.live, 1}, cols, v.rows, v.H, v.H};
+}
+
+template <class SH>
+Product<SH, RowsOp, RowsOp, BfOut> dh(const VocabNet& v, int col0, int cols) {
+  const int K = cdiv(cols, kKB) * kKB, kchunk = cdiv(K / kKB, v.Sh) * kKB;
+  const VocabOut o{v.hpart, v.H, (size_t)v.rows * v.H, v.rows, v.H, 0, col0 > 0, nullptr};
+  return {RowsOp{(const u16*)v.Ws + col0, v.ldw, v.H, v.Cq - col0},
+          RowsOp{(const u16*)vocab_dz_at(v, col0), v.P, v.rows, v.P}, BfOut{o}, Live{v.live, 1}, v.H, v.rows, K, kchunk};
+}
+
+Product<Big, ColsOp, ColsOp, BfOut> dw(const VocabNet& v, int col0, int cols, const VocabOut& o) {
+  return {ColsOp{(const u16*)vocab_dz_at(v, col0), v.P, v.P}, ColsOp{(const u16*)v.hp, v.H, v.H}, BfOut{o},
+          Live{v.live, 2}, cols, v.H, cdiv(v.n, kKB) * kKB, cdiv(cdiv(v.n, kKB), v.Sw) * kKB};
 }
 
 }  // namespace
 
-void vocab_bf_loss(const VocabNet& v, hipStream_t s) {
-  logits<true>("k_vocab_bf<loss>", v, 0, v.C, s);
+void vocab_bf_loss(const VocabNet& v, const void* W, hipStream_t s) {
+  if (v.few) {
+    const dim3 grid(cdiv(v.C, kFewWords));
+    const VocabEp e = vocab_ep(v, 0);
+    if (v.K > 0)
+      CAVS_LAUNCH("k_vocab_few", k_vocab_few<true>, grid, dim3(256), 0, s, e, (const u16*)W, (const u16*)v.hp,
+                  v.H);
+    else
+      CAVS_LAUNCH("k_vocab_few", k_vocab_few<false>, grid, dim3(256), 0, s, e, (const u16*)W,
+                  (const u16*)v.hp, v.H);
+    return;
+  }
+  if (v.K > 0) launch<Big>("k_vocab_bf<loss>", s, logits<true, true>(v, 0, v.C));
+  else launch<Big>("k_vocab_bf<loss>", s, logits<true, false>(v, 0, v.C));
 }
 
 void vocab_bf_dz(const VocabNet& v, int col0, int cols, hipStream_t s) {
-  logits<false>("k_vocab_bf<dz>", v, col0, cols, s);
+  if (v.K > 0) launch<Big>("k_vocab_bf<dz>", s, logits<false, true>(v, col0, cols));
+  else launch<Big>("k_vocab_bf<dz>", s, logits<false, false>(v, col0, cols));
 }
 
-void vocab_bf_dh(const VocabNet& v, int col0, int cols, hipStream_t s) {
-  const int K = cdiv(std::min(cols, v.C - col0), kKB) * kKB, kchunk = cdiv(K / kKB, v.Sh) * kKB;
-  const VocabOut o{v.hpart, v.H, (size_t)v.rows * v.H, v.rows, v.H, 0, col0 > 0, nullptr};
-  product<Big>("k_vocab_bf<dh>", RowsOp{(const u16*)v.Ws + col0, v.ldw, v.H, v.Cq - col0},
-               RowsOp{(const u16*)v.dZ, v.P, v.rows, v.P}, BfOut{o}, Live{v.live, 1}, v.H, v.rows, K,
-               kchunk, s);
-}
-
-void vocab_bf_dw(const VocabNet& v, int col0, int cols, const VocabOut& o, hipStream_t s) {
-  const int kchunk = cdiv(v.rows / kKB, v.Sw) * kKB;
-  product<Big>("k_vocab_bf<dw>", ColsOp{(const u16*)v.dZ, v.P, v.P},
-               ColsOp{(const u16*)v.hp, v.H, v.H}, BfOut{o}, Live{v.live, 2}, cols, v.H, v.rows,
-               kchunk, s);
+// next > 0: the columns of the next piece, whose dz is formed beside this one's
+// products (it fills the CUs that they leave: 196 tiles of dW_s and 112 of dL/dh
+// take turns on 256 CUs badly by themselves).
+void vocab_bf_grads(const VocabNet& v, int col0, int cols, int next, const VocabOut& o, hipStream_t s) {
+  const auto w = dw(v, col0, cols, o);
+  if (v.few) {
+    launch<Big>("k_vocab_bf<dw>", s, w);
+    launch<Few>("k_vocab_bf<dh, few>", s, dh<Few>(v, col0, cols));
+  } else {
+    // the longer items first, the next piece's short ones last
+    const auto h = dh<Big>(v, col0, cols);
+    auto with = [&](auto first, auto second) {
+      if (next == 0) launch<Big>("k_vocab_bf<dw, dh>", s, first, second);
+      else if (v.K > 0)
+        launch<Big>("k_vocab_bf<dw, dh, dz>", s, first, second, logits<false, true>(v, col0 + cols, next));
+      else launch<Big>("k_vocab_bf<dw, dh, dz>", s, first, second, logits<false, false>(v, col0 + cols, next));
+    };
+    if (w.kchunk >= h.kchunk) with(w, h);
+    else with(h, w);
+  }
 }
 
 }  // namespace cavs

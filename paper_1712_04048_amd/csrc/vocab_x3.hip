@@ -32,16 +32,13 @@ struct LiveK {
 // rows 64 wn + 4 r + c.
 template <bool LOSS, bool TEACH>
 struct X3Vocab {
-  using UsesLds = void;
   VocabEp e;
-  __device__ void operator()(char* lds, int, int m0, int n0, int wm, int wn, int g, int r,
+  __device__ void operator()(const Net&, int, int m0, int n0, int wm, int wn, int g, int r,
                              const v4f (&acc)[4][4]) const {
-    const int w = threadIdx.x >> 6, a0 = e.col0 + m0 + 64 * wm, row0 = n0 + 64 * wn;
+    const int a0 = e.col0 + m0 + 64 * wm, row0 = n0 + 64 * wn;
     auto col = [](int i, int gg) { return 16 * gg + i; };
-    float b[16], db[1] = {0.f};
+    float b[16], db[16] = {};
     vocab_bias(e, a0, g, col, b);
-    if (!LOSS || TEACH) __syncthreads();   // the slabs take the operands' place
-    float* slab = reinterpret_cast<float*>(lds) + w * kSlabFloats<64>;
     const int live = *e.live;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
@@ -50,12 +47,13 @@ struct X3Vocab {
       for (int q = 0; q < 4; ++q)
 #pragma unroll
         for (int j = 0; j < 4; ++j) z[4 * q + j] = acc[j][c][q] + b[4 * q + j];
-      vocab_rows16<LOSS, TEACH, float, 64>(e, z, col, row0 + c, 4, a0, a0 / 64, live, slab, db);
+      const int row = row0 + c + 4 * r;
+      vocab_rows16<LOSS, TEACH, float, 64>(e, z, col, row, a0, a0 / 64,
+                                           (size_t)(a0 / 64) * e.rows + row, live, db);
     }
-    if (!LOSS) e.dbp[(size_t)(row0 / 64) * e.ldz + (a0 - e.col0) + (threadIdx.x & 63)] = db[0];
+    if (!LOSS) vocab_db<64>(e, db, col, a0, row0 / 64);
   }
 };
-static_assert(4 * kSlabFloats<64> * sizeof(float) <= 2 * kX3Bytes, "slabs fit the operands' LDS");
 
 struct X3VocabOut {
   VocabOut o;
@@ -90,9 +88,121 @@ void logits(const char* name, const VocabNet& v, int col0, int cols, hipStream_t
     x3_gemm<3, 15, 2>(name, zero_net(v), w, h, X3Vocab<LOSS, false>{e}, cols, v.rows, v.H, v.H, s, lv);
 }
 
+// The loss over at most 64 rows: a workgroup takes every row of 128 words, four
+// wavefronts of 32 x 64, two stages of 32 k in flight in registers, split on
+// their way to LDS (split3.h's parts, a plane of 64-byte rows each).  W_s is read
+// as it is, at the alignment of its elements.  The 128 x 128 tiles, one chunk in
+// flight and twice the work, took 83 us for 9 rows, 8 043 words, H = 1152.
+constexpr int kFewWords = 128;
+template <bool TEACH>
+__global__ void __launch_bounds__(256, 2) k_vocab_few_x3(VocabEp e, const float* __restrict__ W,
+                                                         const float* __restrict__ hp, int H) {
+  constexpr int FA = 2, FB = 4, kA = kFewWords * 64, kB = kVocabFew * 64, kPlanes = 3 * (kA + kB);
+  __shared__ __attribute__((aligned(16))) char lds[2][kPlanes];
+  __shared__ float stats[3][4][kVocabFew];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g = lane >> 4, r = lane & 15;
+  const int a0 = blockIdx.x * kFewWords, C = e.C;
+  const size_t end = (size_t)H * C;   // at least 64 values
+  // A: words 2 lane, 2 lane + 1, k octet w; B: row tid / 4, octet tid % 4
+  const float* hb = hp + (size_t)(tid >> 2) * H + 8 * (tid & 3);
+  struct Stage {
+    float2 a[8];
+    float4 b[2];
+  } st[2];
+  auto load = [&](Stage& x, int k0) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const size_t o = (size_t)(k0 + 8 * w + k) * C + a0 + 2 * lane;
+      if (o + 2 <= end) __builtin_memcpy(&x.a[k], W + o, 8);
+      else x.a[k] = make_float2(o < end ? W[o] : 0.f, 0.f);
+    }
+    x.b[0] = ldg4(hb + k0);
+    x.b[1] = ldg4(hb + k0 + 4);
+  };
+  auto put = [&](char* base, int plane, int row, int octet, const float (&v)[8]) {
+    const Split8 p = split8(v);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(base + k * plane + x3_addr(row, octet)) = p.p[k];
+  };
+  v4f acc[FA][FB];
+  zero_acc(acc);
+  load(st[0], 0);
+  load(st[1], min(kBK, H - kBK));
+  for (int k0 = 0; k0 < H; k0 += 2 * kBK) {   // H is a multiple of 64
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      char* L = lds[s];
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = c ? st[s].a[k].y : st[s].a[k].x;
+        put(L, kA, 2 * lane + c, w, v);
+      }
+      const float4 b0 = st[s].b[0], b1 = st[s].b[1];
+      const float v[8] = {b0.x, b0.y, b0.z, b0.w, b1.x, b1.y, b1.z, b1.w};
+      put(L + 3 * kA, kB, tid >> 2, tid & 3, v);
+      __syncthreads();   // the other buffer's readers are past this one's barrier
+      load(st[s], min(k0 + (s + 2) * kBK, H - kBK));   // past the end: the last stage, unused
+      __builtin_amdgcn_sched_barrier(0);   // the loads go out before these products
+      bf16x8 b[3][FB];
+#pragma unroll
+      for (int p = 0; p < 3; ++p)
+#pragma unroll
+        for (int f = 0; f < FB; ++f)
+          b[p][f] = *reinterpret_cast<const bf16x8*>(L + 3 * kA + p * kB + x3_addr(16 * f + r, g));
+#pragma unroll
+      for (int i = 0; i < FA; ++i) {
+        bf16x8 a[3];
+#pragma unroll
+        for (int p = 0; p < 3; ++p)
+          a[p] = *reinterpret_cast<const bf16x8*>(L + p * kA + x3_addr(32 * w + 16 * i + r, g));
+#pragma unroll
+        for (int t = 0; t < kSplitTerms; ++t)
+#pragma unroll
+          for (int f = 0; f < FB; ++f)
+            acc[i][f] = mfma_bf16_16x16x32(a[kTermA[t]], b[kTermB[t]][f], acc[i][f]);
+      }
+    }
+  }
+  float nan = 0.f;
+#pragma unroll
+  for (int i = 0; i < FA; ++i)
+#pragma unroll
+    for (int f = 0; f < FB; ++f)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) nan += acc[i][f][q];
+  if (nan != nan) {   // NaN, or an operand without parts (split3.h): these words' sums in fp32
+#pragma unroll
+    for (int i = 0; i < FA; ++i)
+#pragma unroll
+      for (int f = 0; f < FB; ++f)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int c = a0 + 32 * w + 16 * i + 4 * g + q;
+          float s = 0.f;
+          if (c < C)
+            for (int k = 0; k < H; ++k) s = fmaf(W[(size_t)k * C + c], hp[(size_t)(16 * f + r) * H + k], s);
+          acc[i][f][q] = s;
+        }
+  }
+  vocab_few_end<TEACH, 64>(e, stats, a0, [&](int i, int f) { return acc[i >> 2][f][i & 3]; });
+}
+
 }  // namespace
 
-void vocab_x3_loss(const VocabNet& v, hipStream_t s) {
+void vocab_x3_loss(const VocabNet& v, const void* W, hipStream_t s) {
+  if (v.few) {
+    const dim3 grid(cdiv(v.C, kFewWords));
+    const VocabEp e = vocab_ep(v, 0);
+    if (v.K > 0)
+      CAVS_LAUNCH("k_vocab_few_x3", k_vocab_few_x3<true>, grid, dim3(256), 0, s, e, (const float*)W,
+                  (const float*)v.hp, v.H);
+    else
+      CAVS_LAUNCH("k_vocab_few_x3", k_vocab_few_x3<false>, grid, dim3(256), 0, s, e, (const float*)W,
+                  (const float*)v.hp, v.H);
+    return;
+  }
   logits<true>("k_x3_gemm<vocab loss>", v, 0, v.C, s);
 }
 
@@ -110,9 +220,9 @@ void vocab_x3_dh(const VocabNet& v, int col0, int cols, hipStream_t s) {
 }
 
 void vocab_x3_dw(const VocabNet& v, int col0, int cols, const VocabOut& o, hipStream_t s) {
-  const int nch = cdiv(v.rows, kBK), kchunk = cdiv(nch, v.Sw) * kBK;
+  const int nch = cdiv(v.n, kBK), kchunk = cdiv(nch, v.Sw) * kBK;
   x3_gemm<3, 15, 2>("k_x3_gemm<vocab dw>", zero_net(v), X3Cols{(const float*)v.hp, v.H, v.H},
-                    X3Cols{(const float*)v.dZ, v.P, v.P}, X3VocabOut{o}, v.H, cols, v.rows,
+                    X3Cols{(const float*)v.dZ, v.P, v.P}, X3VocabOut{o}, v.H, cols, nch * kBK,
                     kchunk, s, LiveK{v.live});
 }
 

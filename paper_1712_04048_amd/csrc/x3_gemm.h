@@ -121,11 +121,6 @@ struct X3Out {
 struct X3Sized {
   __device__ void operator()(int&, int&, int&, int&) const {}
 };
-// What a workgroup does with its tile names UsesLds where it wants the tiles' LDS.
-template <class EP, class = void>
-struct X3UsesLds : std::false_type {};
-template <class EP>
-struct X3UsesLds<EP, std::void_t<typename EP::UsesLds>> : std::true_type {};
 constexpr int kX3Band = 8;
 template <class LA, class LB, class EP, class LV, int PARTS, int BLOCKS, int WGS>
 __global__ void __launch_bounds__(256, WGS) k_x3_gemm(Net n, LA la, LB lb, EP ep, LV lv, int ty,
@@ -172,10 +167,7 @@ __global__ void __launch_bounds__(256, WGS) k_x3_gemm(Net n, LA la, LB lb, EP ep
     if (x3_nan(acc))   // NaN, or an operand without parts (split3.h)
       sum(std::integral_constant<int, 0>{}, x3_again(tid & 127),
           [&] { x3_mma_f32(lds, lds + OPB, wm, wn, acc); });
-  if constexpr (X3UsesLds<EP>::value)
-    ep(lds, z, m0, n0, wm, wn, g, r, acc);   // with the tiles' LDS for its own use
-  else
-    ep(n, z, m0, n0, wm, wn, g, r, acc);
+  ep(n, z, m0, n0, wm, wn, g, r, acc);
 }
 
 template <int PARTS, int BLOCKS, int WGS, class LA, class LB, class EP, class LV = X3Sized>
