@@ -38,6 +38,15 @@ __global__ void __launch_bounds__(256) k_embed(int n_words, int D, unsigned tota
   store_row<V>(out + (size_t)i * D + c, v);
 }
 
+// Words at i, i + 64, .. (-1 from `to` on), all asked for before the first is
+// used: one after the other the sort's second pass took 20 of 26 us of 32 768,
+// which are one such load a wavefront.
+constexpr int kAhead = 32;
+__device__ __forceinline__ void load_words(const int* __restrict__ word, int i, int to, int (&v)[kAhead]) {
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k) v[k] = i + 64 * k < to ? word[i + 64 * k] : -1;
+}
+
 // The places of each word in ascending order: order[start[v] .. start[v + 1]).
 // A workgroup takes R adjacent words and reads all n places twice, its sixteen
 // wavefronts a contiguous part each: first counting its own words and the places
@@ -49,22 +58,28 @@ __global__ void __launch_bounds__(1024) k_embed_sort(int n, int n_words, int R,
                                                      int* order, int* err) {
   __shared__ int cnt[16][kSortWords];
   __shared__ int wsum[16];
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lo = blockIdx.x * R, nr = min(R, n_words - lo);
   const int per = (cdiv_dev(n, 16) + 63) / 64 * 64, from = min(w * per, n), to = min(from + per, n);
-  for (int i = tid; i < 16 * R; i += 1024) cnt[i / R][i % R] = 0;
-  __syncthreads();
-  int below = 0;
+  for (int i = lane; i < R; i += 64) cnt[w][i] = 0;   // a wavefront's own counts
+  wave_lds_fence();
+  int below = 0, v[kAhead];
   bool bad = false;
-#pragma unroll 4
-  for (int i = from + lane; i < to; i += 64) {
-    const int v = word[i];
-    below += v >= 0 && v < lo;
-    bad |= v < -1 || v >= n_words;
-    if (v >= lo && v < lo + nr) atomicAdd(&cnt[w][v - lo], 1);
+  for (int i0 = from; i0 < to; i0 += 64 * kAhead) {
+    load_words(word, i0 + lane, to, v);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (i0 + 64 * k >= to) break;
+      // what most of the places are is not this workgroup's: a comparison and a
+      // count in the scalar unit for each 64 (told apart in lanes, the two passes
+      // took 19 us of 32 768 places)
+      below += __popcll(__ballot((unsigned)v[k] < (unsigned)lo));
+      if (blockIdx.x == 0) bad |= (unsigned)(v[k] + 1) > (unsigned)n_words;
+      const unsigned x = (unsigned)v[k] - (unsigned)lo;
+      if (__any(x < (unsigned)nr) && x < (unsigned)nr) atomicAdd(&cnt[w][x], 1);
+    }
   }
   if (bad) err[1] = 1;
-  below = wave_sum_int(below);
   if (lane == 0) wsum[w] = below;
   __syncthreads();
   int base = 0;
@@ -97,86 +112,113 @@ __global__ void __launch_bounds__(1024) k_embed_sort(int n, int n_words, int R,
     }
   }
   __syncthreads();
-  for (int i0 = from; i0 < to; i0 += 64) {
-    const int i = i0 + lane, v = i < to ? word[i] - lo : -1;
-    unsigned long long left = __ballot(v >= 0 && v < nr);
-    while (left) {
-      const int v0 = __shfl(v, __ffsll(left) - 1, kWave);
-      const unsigned long long same = __ballot(v == v0);
-      const int at = cnt[w][v0];
-      if (v == v0) order[at + __popcll(same & ((1ull << lane) - 1))] = i;
-      wave_lds_fence();
-      if (lane == 0) cnt[w][v0] = at + __popcll(same);
-      wave_lds_fence();
-      left &= ~same;
+  for (int i0 = from; i0 < to; i0 += 64 * kAhead) {
+    if (to - from > 64 * kAhead) load_words(word, i0 + lane, to, v);   // else still there
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (i0 + 64 * k >= to) break;
+      const unsigned x = (unsigned)v[k] - (unsigned)lo;
+      unsigned long long left = __ballot(x < (unsigned)nr), same = 0;
+      if (left == 0) continue;
+      const bool mine = x < (unsigned)nr;
+      while (left) {   // the lanes that share each lane's word
+        const int v0 = __builtin_amdgcn_readlane((int)x, __ffsll(left) - 1);
+        const unsigned long long m = __ballot(mine && (int)x == v0);
+        same = (int)x == v0 ? m : same;
+        left &= ~m;
+      }
+      // the first of them counts them all off and tells them where they begin
+      const int rank = __popcll(same & ((1ull << lane) - 1)), first = mine ? __ffsll(same) - 1 : lane;
+      int at = 0;
+      if (mine && rank == 0) at = atomicAdd(&cnt[w][x], __popcll(same));
+      at = __shfl(at, first, kWave);
+      if (mine) order[at + rank] = i0 + 64 * k + lane;
     }
   }
 }
 
-// The sum of rows order[from .. to) of dX, columns c ..
+// The sum of rows order[from .. to) of dX, at most kPart, columns c ..: their
+// places in one load, then eight rows in flight, one column block of 64 V to a
+// wavefront (20 074 rows of 247 floats: 7 us, 18 with four rows in flight and
+// every column to one; 32 768 rows of 2 KB into a table of 100 MB: 41, at 4.1
+// TB/s).
 template <class X, int V>
 __device__ __forceinline__ void add_rows(const X* __restrict__ dX, int D, const int* __restrict__ order,
                                          int from, int to, int c, float (&s)[V]) {
+  const int lane = threadIdx.x & 63, n = to - from;
+  const int at = lane < n ? order[from + lane] : 0;
 #pragma unroll
   for (int k = 0; k < V; ++k) s[k] = 0.f;
-#pragma unroll 4
-  for (int j = from; j < to; ++j) {
-    float v[V];
-    load_row<V>(dX + (size_t)order[j] * D + c, v);
+  for (int j = 0; j < n; j += 8) {
+    // as they are in memory: a conversion here would wait for each in turn
+    RawRow<V, X> x[8];
 #pragma unroll
-    for (int k = 0; k < V; ++k) s[k] += v[k];
+    for (int u = 0; u < 8; ++u)
+      if (j + u < n) x[u].load(dX + (size_t)__builtin_amdgcn_readlane(at, j + u) * D + c);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      if (j + u >= n) break;
+      float v[V];
+      x[u].floats(v);
+#pragma unroll
+      for (int k = 0; k < V; ++k) s[k] += v[k];
+    }
   }
 }
 
-// Wavefronts 0 .. n_words - 1: the row of dE of a word that occurs at most
-// kPart times (zeros for one that does not occur).  The further ones take kPart
-// sorted places each: a word that occurs more often has its share of them
-// summed into part[p][0] (the word of the first place) or part[p][1] (one that
-// begins later: at most one such word, as it must reach past the end), and
-// begins[p] names the word of that kind that begins here, for k_embed_join.
+// The first wavefronts take kPart sorted places each: a word that occurs more
+// often than kPart times has its share of them summed into part[p][0] (the word
+// of the first place) or part[p][1] (one that begins later: at most one such
+// word, as it must reach past the end), and begins[p] names the word of that kind
+// that begins here, for k_embed_join.  The others take `each` adjacent words and
+// write the rows of dE of those that occur at most kPart times (zeros for one
+// that does not occur, most of them as a rule).
 template <class E, class X, int V>
-__global__ void __launch_bounds__(256) k_embed_sum(int n, int n_words, int D, float scale,
+__global__ void __launch_bounds__(256) k_embed_sum(int n, int n_words, int D, int each, float scale,
                                                    const int* __restrict__ word,
                                                    const int* __restrict__ start,
                                                    const int* __restrict__ order,
                                                    const X* __restrict__ dX, E* dE, float* part,
                                                    int* begins) {
   const int lane = threadIdx.x & 63;
-  const int item = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
+  const int at_ = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
+  // a row's column blocks are neighbours; past the last column a lane adds its
+  // block's first ones and stores nothing
+  const int cols = cdiv_dev(D, 64 * V), item = at_ / cols, cb = at_ - item * cols;
+  const int c0 = (cb * 64 + lane) * V, c = c0 < D ? c0 : cb * 64 * V;
   float s[V];
-  if (item < n_words) {
-    const int from = start[item], to = start[item + 1];
-    if (to - from > kPart) return;
-    for (int c = lane * V; c < D; c += 64 * V) {
+  const int parts = cdiv_dev(n, kPart);
+  if (item >= parts) {
+    const int w0 = (item - parts) * each;   // each is at most 8
+    const int at = start[min(w0 + min(lane, each), n_words)];
+    for (int k = 0; k < each && w0 + k < n_words; ++k) {
+      const int from = __builtin_amdgcn_readlane(at, k), to = __builtin_amdgcn_readlane(at, k + 1);
+      if (to - from > kPart) continue;
       add_rows<X, V>(dX, D, order, from, to, c, s);
 #pragma unroll
-      for (int k = 0; k < V; ++k) s[k] *= scale;
-      store_row<V>(dE + (size_t)item * D + c, s);
+      for (int i = 0; i < V; ++i) s[i] *= scale;
+      if (c0 < D) store_row<V>(dE + (size_t)(w0 + k) * D + c, s);
     }
     return;
   }
-  const int p = item - n_words, all = start[n_words], lo = p * kPart, hi = min(lo + kPart, all);
-  if (lo >= n) return;
+  const int p = item, all = start[n_words], lo = p * kPart, hi = min(lo + kPart, all);
   int first = -1;
   if (lo < hi) {
-    const int a = word[order[lo]], b = word[order[hi - 1]];
+    const int a = __builtin_amdgcn_readfirstlane(word[order[lo]]);
+    const int b = __builtin_amdgcn_readfirstlane(word[order[hi - 1]]);
     const int a0 = start[a], a1 = start[a + 1], b0 = start[b], b1 = start[b + 1];
     if (a1 - a0 > kPart) {
       if (a0 == lo) first = a;
-      for (int c = lane * V; c < D; c += 64 * V) {
-        add_rows<X, V>(dX, D, order, lo, min(a1, hi), c, s);
-        store_row<V>(part + (size_t)p * 2 * D + c, s);
-      }
+      add_rows<X, V>(dX, D, order, lo, min(a1, hi), c, s);
+      if (c0 < D) store_row<V>(part + (size_t)p * 2 * D + c, s);
     }
     if (b != a && b1 - b0 > kPart) {
       first = b;
-      for (int c = lane * V; c < D; c += 64 * V) {
-        add_rows<X, V>(dX, D, order, b0, hi, c, s);
-        store_row<V>(part + (size_t)(p * 2 + 1) * D + c, s);
-      }
+      add_rows<X, V>(dX, D, order, b0, hi, c, s);
+      if (c0 < D) store_row<V>(part + (size_t)(p * 2 + 1) * D + c, s);
     }
   }
-  if (lane == 0) begins[p] = first;
+  if (lane == 0 && cb == 0) begins[p] = first;
 }
 
 // dE of the words of more than kPart places: their parts in order, a contiguous
@@ -280,9 +322,12 @@ template <class E, class X, int V>
 void embed_grad_launch(cavs_ctx* ctx, const cavs_embedding* e, const int* word, int n, const void* dX,
                        void* dE, const EmbedWs& w) {
   const int parts = cdiv(n, kPart);
-  CAVS_LAUNCH("k_embed_sum", (k_embed_sum<E, X, V>), dim3(cdiv((long)e->n_words + parts, 4)), dim3(256), 0,
-              ctx->stream, n, e->n_words, e->D, e->scale, word, w.start, w.order, (const X*)dX, (E*)dE,
-              w.part, w.begins);
+  const int cols = cdiv(e->D, 64 * V);
+  // some 8192 wavefronts, eight words each at most
+  const int each = std::min(8, std::max(1, (int)((size_t)e->n_words * cols / 8192)));
+  CAVS_LAUNCH("k_embed_sum", (k_embed_sum<E, X, V>), dim3(cdiv(((long)parts + cdiv(e->n_words, each)) * cols, 4)),
+              dim3(256), 0, ctx->stream, n, e->n_words, e->D, each, e->scale, word, w.start, w.order,
+              (const X*)dX, (E*)dE, w.part, w.begins);
   if (n > kPart)
     CAVS_LAUNCH("k_embed_join", (k_embed_join<E, V>), dim3(std::min(parts, 256), cdiv(e->D, 64 * V)),
                 dim3(1024), 0, ctx->stream, parts, e->D, e->scale, w.start, w.begins, w.part, (E*)dE);

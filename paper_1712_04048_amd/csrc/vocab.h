@@ -106,35 +106,38 @@ __device__ __forceinline__ void wave_lds_fence() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// V adjacent elements as floats, and back (rounded once)
+// V adjacent elements as they are in memory, as floats, and back (rounded once)
 template <int V, class T>
-__device__ __forceinline__ void load_row(const T* p, float (&v)[V]) {
-  if constexpr (sizeof(T) == 4) {
-    if constexpr (V % 4 == 0) {
+struct RawRow {
+  static constexpr int kBytes = V * (int)sizeof(T);
+  uint32_t w[(kBytes + 3) / 4];
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (kBytes % 16 == 0) {
 #pragma unroll
-      for (int i = 0; i < V; i += 4) {
-        const float4 x = ldg4((const float*)p + i);
-        v[i] = x.x; v[i + 1] = x.y; v[i + 2] = x.z; v[i + 3] = x.w;
+      for (int i = 0; i < kBytes / 16; ++i) {
+        const uint4 x = reinterpret_cast<const uint4*>(p)[i];
+        w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < V; ++i) v[i] = p[i];
-    }
-  } else {
-    uint32_t w[(V + 1) / 2];
-    if constexpr (V == 8) {
-      const uint4 x = *reinterpret_cast<const uint4*>(p);
-      w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
-    } else if constexpr (V == 4) {
+    } else if constexpr (kBytes == 8) {
       const uint2 x = *reinterpret_cast<const uint2*>(p);
       w[0] = x.x; w[1] = x.y;
     } else {
-      w[0] = *p;
+      static_assert(V == 1, "16 or 8 bytes, or one element");
+      if constexpr (sizeof(T) == 4) w[0] = __float_as_uint(*p);
+      else w[0] = *p;
     }
+  }
+  __device__ __forceinline__ void floats(float (&v)[V]) const {
 #pragma unroll
     for (int i = 0; i < V; ++i)
-      v[i] = __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+      v[i] = __uint_as_float(sizeof(T) == 4 ? w[i] : i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
   }
+};
+template <int V, class T>
+__device__ __forceinline__ void load_row(const T* p, float (&v)[V]) {
+  RawRow<V, T> x;
+  x.load(p);
+  x.floats(v);
 }
 template <int V, class T>
 __device__ __forceinline__ void store_row(T* p, const float (&v)[V]) {
@@ -169,8 +172,24 @@ __device__ __forceinline__ float row16_sum(float v) {
   return v;
 }
 
-// One group of 16 rows of a wavefront's tile of NC words, which lie in slot
-// `slot` of words: lane (g, r) holds NV = NC / 4 of row `row` (r's), z[i] the score of word
+// What an epilogue needs of a row: its constants (rowc), its label (-1: none, or
+// no live row), its teacher's words in the slot.
+struct VocabRow {
+  float4 c;
+  int label;
+  uint32_t range;
+};
+template <bool LOSS, bool TEACH>
+__device__ __forceinline__ VocabRow vocab_row(const VocabEp& e, int row, int slot, int live) {
+  VocabRow v{};
+  if (!LOSS) v.c = e.rowc[row];
+  v.label = row < live && e.label ? e.label[row] : -1;
+  if (TEACH) v.range = row < live ? e.trange[(size_t)slot * e.rows + row] : 0u;
+  return v;
+}
+
+// One group of 16 rows of a wavefront's tile of NC words, which lie in one slot
+// of words: lane (g, r) holds NV = NC / 4 of row `row` (r's), z[i] the score of word
 // a0 + col(i, g), four adjacent i adjacent words.  LOSS: the words' statistics
 // (to pm[stat] and on) and the z that the loss names.  Otherwise dz = w1 exp(z - m) + wT exp((z - m)
 // / T) - [label] - teacher's q, in 32 bits until it is stored, and added to db.
@@ -187,15 +206,13 @@ __device__ __forceinline__ float row16_sum(float v) {
 // depth 1024 is 25.
 template <bool LOSS, bool TEACH, class OUT, int NC, class Col>
 __device__ __forceinline__ void vocab_rows16(const VocabEp& e, float (&z)[NC / 4], Col col, int row,
-                                             int a0, int slot, size_t stat, int live,
+                                             const VocabRow& info, int a0, size_t stat,
                                              float (&db)[NC / 4]) {
   constexpr int NV = NC / 4;
   const int g = (threadIdx.x & 63) >> 4;
-  const bool here = row < live;
-  const int lab = (here && e.label ? e.label[row] : -1) - a0;
+  const int lab = info.label - a0;   // -1 - a0 is no column either
   const bool labelled = __any((unsigned)lab < (unsigned)NC);
-  uint32_t range = 0;
-  if constexpr (TEACH) range = here ? e.trange[(size_t)slot * e.rows + row] : 0u;
+  const uint32_t range = info.range;
   // f(word's place in the row's list, its column) for each of the row's words here
   auto words = [&](auto&& f) {
     const int hi = range >> 16;
@@ -245,7 +262,7 @@ __device__ __forceinline__ void vocab_rows16(const VocabEp& e, float (&z)[NC / 4
           if (col(i, g) == d) e.ztop[at] = z[i];
       });
   } else {
-    const float4 c = e.rowc[row];
+    const float4 c = info.c;
     if (TEACH && e.two) {
       const float k = e.invT * kLog2e;
 #pragma unroll
@@ -326,7 +343,9 @@ __device__ __forceinline__ void vocab_few_end(const VocabEp& e, float (&stats)[3
     float x[NC / 4];
 #pragma unroll
     for (int i = 0; i < NC / 4; ++i) x[i] = z(i, f) + bias[i];
-    vocab_rows16<true, TEACH, float, NC>(own, x, col, 16 * f + r, aw, aw / SW, 16 * f + r, live, db);
+    const int row = 16 * f + r;
+    vocab_rows16<true, TEACH, float, NC>(own, x, col, row, vocab_row<true, TEACH>(e, row, aw / SW, live), aw,
+                                         row, db);
   }
   __syncthreads();
   const int row = tid & 63;

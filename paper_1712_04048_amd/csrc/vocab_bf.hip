@@ -140,6 +140,7 @@ constexpr int kBand = 8;
 // parts of kchunk.
 template <class SH, class OA, class OB, class EP>
 struct Product {
+  using Own = typename EP::template Own<SH>;
   OA oa;
   OB ob;
   EP ep;
@@ -198,6 +199,7 @@ struct Product {
 #pragma unroll
     for (int st = 0; st < S - 1; ++st)
       if (st < nst) issue(st);
+    ep.template prepare<SH>(lds + SH::kBytes, a0, b0);   // before the first stage's barrier
     for (int st = 0; st < nst; ++st) {
       // this stage has landed and the one before it has been read, everywhere
       if (st + S - 2 < nst) wait_vmcnt_lgkm0<(S - 2) * kCopies>();
@@ -219,14 +221,14 @@ struct Product {
           for (int j = 0; j < FB; ++j) acc[i][j] = mfma_bf16_16x16x32(a[i], b[j], acc[i][j]);
       }
     }
-    ep.template operator()<SH>(zi, a0 + wa * 16 * FA, b0 + wb * 16 * FB, g, r, acc);
+    ep.template operator()<SH>(lds + SH::kBytes, zi, a0, b0, wa, wb, g, r, acc);
   }
 };
 
 // One or more independent products, the workgroups of the first ones first.
 template <class SH, class... P>
 __global__ void __launch_bounds__(SH::T, 2) k_vocab_bf(P... p) {
-  __shared__ __attribute__((aligned(16))) char lds[SH::kBytes];
+  __shared__ __attribute__((aligned(16))) char lds[SH::kBytes + std::max({sizeof(typename P::Own)...})];
   const int x = blockIdx.x & 7;
   int at = blockIdx.x >> 3;
   (void)(p.take(x, at, lds) || ...);
@@ -242,22 +244,56 @@ void launch(const char* name, hipStream_t s, P... p) {
 template <bool LOSS, bool TEACH>
 struct BfVocab {
   VocabEp e;
+  // The tile's words' biases and rows' constants, in LDS beside the stages: asked
+  // for with the first stage's copies, they have come long before the epilogue,
+  // which one workgroup a CU leaves nothing else to run in.
   template <class SH>
-  __device__ void operator()(int, int a, int b, int g, int r, const v4f (&acc)[SH::FA][SH::FB]) const {
-    constexpr int NC = 16 * SH::FA, NV = NC / 4;
-    const int a0 = e.col0 + a;
-    auto col = [](int i, int gg) { return 16 * (i >> 2) + 4 * gg + (i & 3); };
-    float bias[NV], db[NV] = {};
-    vocab_bias(e, a0, g, col, bias);
+  struct Own {
+    float bias[SH::BA];
+    float4 c[LOSS ? 1 : SH::BB];
+    int label[SH::BB];
+    uint32_t range[TEACH ? SH::WA : 1][SH::BB];
+  };
+  template <class SH>
+  __device__ void prepare(char* own, int a, int b) const {
+    Own<SH>& o = *reinterpret_cast<Own<SH>*>(own);
+    constexpr int NC = 16 * SH::FA;
     const int live = *e.live;
+    for (int i = threadIdx.x; i < SH::BA; i += SH::T) {
+      const int c = e.col0 + a + i;
+      o.bias[i] = c < e.C ? (e.bs ? e.bs[c] : 0.f) : -INFINITY;
+    }
+    for (int i = threadIdx.x; i < SH::BB; i += SH::T) {
+      const VocabRow v = vocab_row<LOSS, false>(e, b + i, 0, live);
+      if (!LOSS) o.c[i] = v.c;
+      o.label[i] = v.label;
+      if (TEACH)
+        for (int k = 0; k < SH::WA; ++k)
+          o.range[k][i] = b + i < live ? e.trange[(size_t)((e.col0 + a) / NC + k) * e.rows + b + i] : 0u;
+    }
+  }
+  template <class SH>
+  __device__ void operator()(const char* own, int, int ta, int tb, int wa, int wb, int g, int r,
+                             const v4f (&acc)[SH::FA][SH::FB]) const {
+    const Own<SH>& o = *reinterpret_cast<const Own<SH>*>(own);
+    constexpr int NC = 16 * SH::FA, NV = NC / 4;
+    const int a = ta + wa * NC, b = tb + wb * 16 * SH::FB, a0 = e.col0 + a;
+    auto col = [](int i, int gg) { return 16 * (i >> 2) + 4 * gg + (i & 3); };
+    float db[NV] = {};
 #pragma unroll
     for (int f = 0; f < SH::FB; ++f) {
       float z[NV];
 #pragma unroll
-      for (int i = 0; i < NV; ++i) z[i] = acc[i >> 2][f][i & 3] + bias[i];
-      const int row = b + 16 * f + r;
-      vocab_rows16<LOSS, TEACH, u16, NC>(e, z, col, row, a0, a0 / NC, (size_t)(a0 / NC) * e.rows + row,
-                                         live, db);
+      for (int i = 0; i < NV; i += 4) {
+        const float4 x = *reinterpret_cast<const float4*>(o.bias + wa * NC + col(i, g));
+        z[i] = acc[i >> 2][f][0] + x.x;
+        z[i + 1] = acc[i >> 2][f][1] + x.y;
+        z[i + 2] = acc[i >> 2][f][2] + x.z;
+        z[i + 3] = acc[i >> 2][f][3] + x.w;
+      }
+      const int at = wb * 16 * SH::FB + 16 * f + r, row = tb + at;
+      const VocabRow v{LOSS ? f4zero() : o.c[LOSS ? 0 : at], o.label[at], TEACH ? o.range[TEACH ? wa : 0][at] : 0u};
+      vocab_rows16<LOSS, TEACH, u16, NC>(e, z, col, row, v, a0, (size_t)(a0 / NC) * e.rows + row, db);
     }
     if (!LOSS) vocab_db<NC>(e, db, col, a0, b / (16 * SH::FB));
   }
@@ -267,7 +303,13 @@ struct BfVocab {
 struct BfOut {
   VocabOut o;
   template <class SH>
-  __device__ void operator()(int z, int a, int b, int g, int r, const v4f (&acc)[SH::FA][SH::FB]) const {
+  struct Own {};
+  template <class SH>
+  __device__ void prepare(char*, int, int) const {}
+  template <class SH>
+  __device__ void operator()(const char*, int z, int ta, int tb, int wa, int wb, int g, int r,
+                             const v4f (&acc)[SH::FA][SH::FB]) const {
+    const int a = ta + wa * 16 * SH::FA, b = tb + wb * 16 * SH::FB;
     const float w = o.scale ? *o.scale : 1.f;
 #pragma unroll
     for (int j = 0; j < SH::FB; ++j)

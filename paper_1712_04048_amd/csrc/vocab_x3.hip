@@ -48,8 +48,8 @@ struct X3Vocab {
 #pragma unroll
         for (int j = 0; j < 4; ++j) z[4 * q + j] = acc[j][c][q] + b[4 * q + j];
       const int row = row0 + c + 4 * r;
-      vocab_rows16<LOSS, TEACH, float, 64>(e, z, col, row, a0, a0 / 64,
-                                           (size_t)(a0 / 64) * e.rows + row, live, db);
+      vocab_rows16<LOSS, TEACH, float, 64>(e, z, col, row, vocab_row<LOSS, TEACH>(e, row, a0 / 64, live), a0,
+                                           (size_t)(a0 / 64) * e.rows + row, db);
     }
     if (!LOSS) vocab_db<64>(e, db, col, a0, row0 / 64);
   }
