@@ -33,13 +33,18 @@ __global__ void __launch_bounds__(256) k_vocab_rows(VocabNet v, int R, const int
   __shared__ int wsum[4], src_of[64], found;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, n = v.n, C = v.C, H = v.H;
   const int lo = blockIdx.x * R, hi = min(lo + R, n);
-  auto scored = [&](int i) {
-    const int y = label ? label[i] : 0;
-    return y >= 0 && y < C;
-  };
   int before = 0;
+  if (label) {   // lo is a multiple of 4
 #pragma unroll 4
-  for (int i = tid; i < lo; i += 256) before += scored(i);
+    for (int i = 4 * tid; i < lo; i += 1024) {
+      int y[4];
+      __builtin_memcpy(y, label + i, 16);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) before += (unsigned)y[k] < (unsigned)C;
+    }
+  } else if (tid == 0) {
+    before = lo;
+  }
   before = wave_sum_int(before);
   if (lane == 0) wsum[w] = before;
   __syncthreads();
@@ -202,12 +207,33 @@ __global__ void __launch_bounds__(256) k_vocab_teacher(VocabNet v, const int* __
   }
 }
 
+// A live row's loss and what its dz is made from, from its joined statistics.
+__device__ float vocab_row_end(const VocabNet& v, int row, float m, float s, float t, float dot,
+                               float* row_loss) {
+  float val = 0.f, has = 0.f;
+  const float a = v.alpha;
+  const int y = v.label[row];
+  if (y >= 0 && a < 1.f) val = (1.f - a) * (logf(s) + (m - v.zlab[row]));
+  if (v.K > 0) {
+    const float2 q = v.tsum[row];
+    has = q.y;
+    if (has != 0.f && a > 0.f) val += a * v.temp * v.temp * (q.x + logf(t) + dot / v.temp);
+  }
+  v.val[row] = val;
+  if (row_loss) row_loss[v.rows_list[row]] = val;
+  // in units of v.unit
+  const float lab = a < 1.f ? 1.f : 0.f, c1 = lab != 0.f ? 1.f / s : 0.f;
+  const float cT = has != 0.f ? v.distw / t : 0.f;
+  v.rowc[row] = v.two ? make_float4(m, c1, cT, lab) : make_float4(m, c1 + cT, 0.f, lab);
+  return val;
+}
+
 // A row's statistics joined over the slots, its loss, and what its dz is made
 // from.  16 rows a workgroup, 64 lanes on every 64th slot (or teacher's word)
 // of each, their sums added in their order.
 //   CE = ln(sum exp(z - m)) + m - z_label
 //   KD = T^2 (sum q ln q + ln(sum exp((z - m) / T)) + sum q (m - z) / T)
-__global__ void __launch_bounds__(1024) k_vocab_join(VocabNet v, float* row_loss) {
+__global__ void __launch_bounds__(1024) k_vocab_join(VocabNet v, float* row_loss, float* loss) {
   __shared__ float sm[64][16], ss[64][16], st[64][16], sd[64][16];
   const int i = threadIdx.x & 15, k0 = threadIdx.x >> 4, row = blockIdx.x * 16 + i;
   const int nl = *v.live;
@@ -215,6 +241,7 @@ __global__ void __launch_bounds__(1024) k_vocab_join(VocabNet v, float* row_loss
   if ((int)blockIdx.x * 16 >= nl) {
     // the rest of the last tile of 256 rows
     if (k0 == 0 && (int)blockIdx.x * 16 < cdiv_dev(nl, kVocabTile) * kVocabTile) v.rowc[row] = none;
+    if (loss && threadIdx.x == 0) *loss = 0.f;
     return;
   }
   float m = -INFINITY;
@@ -252,54 +279,45 @@ __global__ void __launch_bounds__(1024) k_vocab_join(VocabNet v, float* row_loss
     dot += sd[k][i];
   }
   if (!v.two) t = s;
-  if (row >= nl) {
-    v.rowc[row] = none;
-    return;
-  }
-  float val = 0.f, has = 0.f;
-  const float a = v.alpha;
-  const int y = v.label[row];
-  if (y >= 0 && a < 1.f) val = (1.f - a) * (logf(s) + (m - v.zlab[row]));
-  if (v.K > 0) {
-    const float2 q = v.tsum[row];
-    has = q.y;
-    if (has != 0.f && a > 0.f) val += a * v.temp * v.temp * (q.x + logf(t) + dot / v.temp);
-  }
-  v.val[row] = val;
-  if (row_loss) row_loss[v.rows_list[row]] = val;
-  // in units of v.unit
-  const float lab = a < 1.f ? 1.f : 0.f, c1 = lab != 0.f ? 1.f / s : 0.f;
-  const float cT = has != 0.f ? v.distw / t : 0.f;
-  v.rowc[row] = v.two ? make_float4(m, c1, cT, lab) : make_float4(m, c1 + cT, 0.f, lab);
+  float val = 0.f;
+  if (row >= nl) v.rowc[row] = none;
+  else val = vocab_row_end(v, row, m, s, t, dot, row_loss);
+  if (!loss) return;
+  // at most 16 rows, this the only workgroup: their mean, as vocab_mean adds it
+  double sum = (double)val;
+#pragma unroll
+  for (int o = 8; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, kWave);
+  if (i == 0) *loss = (float)(sum / (double)max(nl, 1));
 }
 
-// The mean of the live rows' losses, in 64 bits and a fixed order.
-__global__ void __launch_bounds__(1024) k_vocab_mean(const float* __restrict__ val,
-                                                     const int* __restrict__ live, float* loss) {
-  __shared__ double part[16];
-  const int nl = *live;
+// The mean of the live rows' losses, in 64 bits and a fixed order, by 256 threads.
+__device__ void vocab_mean(const float* val, int nl, float* loss) {
+  __shared__ double part[4];
+  const int tid = threadIdx.x;
   double s = 0.0;
-  for (int i = threadIdx.x; i < nl; i += 1024) s += (double)val[i];
+#pragma unroll 4
+  for (int i = tid; i < nl; i += 256) s += (double)val[i];
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) s += __shfl_xor(s, o, kWave);
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
+  if ((tid & 63) == 0) part[tid >> 6] = s;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    s = 0.0;
-    for (int k = 0; k < 16; ++k) s += part[k];
-    *loss = (float)(s / (double)max(nl, 1));
-  }
+  if (tid == 0) *loss = (float)((part[0] + part[1] + part[2] + part[3]) / (double)max(nl, 1));
+}
+__global__ void __launch_bounds__(256) k_vocab_mean(const float* __restrict__ val,
+                                                    const int* __restrict__ live, float* loss) {
+  vocab_mean(val, *live, loss);
 }
 
 // dz from the z that the loss kept (in place in fp32), as vocab_rows16 forms it,
 // and its sums over 64 rows: 256 words x 64 rows a workgroup, a wavefront on
 // whole rows of 1 KB.
+// db: one group is all of db_s (else null, and the groups' sums go to dbp).
 template <class OUT>
-__global__ void __launch_bounds__(256) k_vocab_dz(VocabNet v) {
+__global__ void __launch_bounds__(256) k_vocab_dz(VocabNet v, float* db_out) {
   __shared__ float4 sums[4][64];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, nl = *v.live;
   const int c0 = blockIdx.x * 256, c = c0 + 4 * lane, r0 = blockIdx.y * 64;
-  if (r0 >= cdiv_dev(nl, kVocabTile) * kVocabTile) return;
+  if (!db_out && r0 >= cdiv_dev(nl, kVocabTile) * kVocabTile) return;
   const float invT = 1.f / v.temp;
   float4 db = f4zero();
 #pragma unroll 4
@@ -339,9 +357,16 @@ __global__ void __launch_bounds__(256) k_vocab_dz(VocabNet v) {
   }
   sums[w][lane] = db;
   __syncthreads();
-  if (w == 0)
-    st4(v.dbp + (size_t)blockIdx.y * v.P + c,
-        add4(add4(sums[0][lane], sums[1][lane]), add4(sums[2][lane], sums[3][lane])));
+  if (w > 0) return;
+  db = add4(add4(sums[0][lane], sums[1][lane]), add4(sums[2][lane], sums[3][lane]));
+  if (!db_out) {
+    st4(v.dbp + (size_t)blockIdx.y * v.P + c, db);
+    return;
+  }
+  const float x[4] = {db.x, db.y, db.z, db.w}, scale = *v.scal;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (c + i < v.C) db_out[c + i] = x[i] * scale;
 }
 
 // db_s of a piece: 64 columns a workgroup, its wavefronts every sixteenth group,
@@ -378,13 +403,17 @@ __global__ void __launch_bounds__(256) k_vocab_dw(int H, int P, int cols, int S,
 
 // dL/dh: live rows from the sums over parts of the vocabulary, the others 0.  A
 // workgroup's four wavefronts take a row each, or a quarter of one row's parts
-// (WIDE: many parts, few rows), added in their order.
+// (WIDE: many parts, few rows), added in their order.  The first workgroup also
+// forms the mean loss: a launch less.
 template <class OUT, bool WIDE>
 __global__ void __launch_bounds__(256) k_vocab_dh(int n, int H, size_t part, int S,
                                                   const int* __restrict__ place,
                                                   const float* __restrict__ sums,
-                                                  const float* __restrict__ scal, OUT* dh) {
+                                                  const float* __restrict__ scal, OUT* dh,
+                                                  const float* __restrict__ val,
+                                                  const int* __restrict__ live, float* loss) {
   __shared__ float4 quarter[WIDE ? 4 : 1][64];
+  if (blockIdx.x == 0 && blockIdx.y == 0) vocab_mean(val, *live, loss);
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int i = WIDE ? blockIdx.y : blockIdx.y * 4 + w, c = (blockIdx.x * 64 + lane) * 4;
   const int per = cdiv_dev(S, 4), z0 = WIDE ? min(w * per, S) : 0, z1 = WIDE ? min(z0 + per, S) : S;
@@ -564,21 +593,21 @@ cavs_status vocab_args(cavs_ctx* ctx, const cavs_vocab* p) {
 
 template <class IN, class OUT>
 void rows(const VocabNet& v, const cavs_vocab* p, float* row_loss, int* err, hipStream_t s) {
-  const int R = std::max(16, cdiv(v.n, 512));
+  const int R = std::max(16, cdiv(v.n, 4 * 512) * 4);
   CAVS_LAUNCH("k_vocab_rows", (k_vocab_rows<IN, OUT>), dim3(cdiv(v.n, R)), dim3(256), 0, s, v, R, p->label,
               row_loss, err);
 }
 
 template <class OUT>
-void dh_sum(const VocabNet& v, OUT* dh, hipStream_t s) {
+void dh_sum(const VocabNet& v, OUT* dh, float* loss, hipStream_t s) {
   const size_t part = (size_t)v.rows * v.H;
   const int gx = cdiv(v.H, 256);
   if (v.Sh >= 8)
     CAVS_LAUNCH("k_vocab_dh", (k_vocab_dh<OUT, true>), dim3(gx, v.n), dim3(256), 0, s, v.n, v.H, part, v.Sh,
-                v.place, v.hpart, v.scal, dh);
+                v.place, v.hpart, v.scal, dh, v.val, v.live, loss);
   else
     CAVS_LAUNCH("k_vocab_dh", (k_vocab_dh<OUT, false>), dim3(gx, cdiv(v.n, 4)), dim3(256), 0, s, v.n, v.H, part,
-                v.Sh, v.place, v.hpart, v.scal, dh);
+                v.Sh, v.place, v.hpart, v.scal, dh, v.val, v.live, loss);
 }
 
 }  // namespace
@@ -639,8 +668,12 @@ cavs_status vocab_run(cavs_ctx* ctx, const cavs_vocab* p, float* loss, float* ro
     CAVS_LAUNCH("k_vocab_teacher", k_vocab_teacher, dim3(v.rows / 4), dim3(256), 0, s, v, p->top_word,
                 p->top_logit, err);
   v.bf ? vocab_bf_loss(v, p->Ws, s) : vocab_x3_loss(v, p->Ws, s);
-  CAVS_LAUNCH("k_vocab_join", k_vocab_join, dim3(v.rows / 16), dim3(1024), 0, s, v, row_loss);
-  CAVS_LAUNCH("k_vocab_mean", k_vocab_mean, dim3(1), dim3(1024), 0, s, v.val, v.live, loss);
+  // the mean: with the gradients in their last kernel, else here or by itself
+  const bool one = !train && v.n <= 16;
+  CAVS_LAUNCH("k_vocab_join", k_vocab_join, dim3(one ? 1 : v.rows / 16), dim3(1024), 0, s, v, row_loss,
+              one ? loss : nullptr);
+  if (!train && !one)
+    CAVS_LAUNCH("k_vocab_mean", k_vocab_mean, dim3(1), dim3(256), 0, s, v.val, v.live, loss);
   if (train) {
     auto width = [&](int col0) { return std::max(0, std::min(v.P, v.C - col0)); };
     auto db = [&](int col0) {
@@ -652,14 +685,15 @@ cavs_status vocab_run(cavs_ctx* ctx, const cavs_vocab* p, float* loss, float* ro
       const int cols = width(col0), next = width(col0 + v.P);
       if (v.keep) {
         const dim3 grid(v.P / 256, v.rows / 64);
-        if (v.bf) CAVS_LAUNCH("k_vocab_dz", k_vocab_dz<u16>, grid, dim3(256), 0, s, v);
-        else CAVS_LAUNCH("k_vocab_dz", k_vocab_dz<float>, grid, dim3(256), 0, s, v);
+        float* const all = v.rows == v.db_rows ? dbs : nullptr;
+        if (v.bf) CAVS_LAUNCH("k_vocab_dz", k_vocab_dz<u16>, grid, dim3(256), 0, s, v, all);
+        else CAVS_LAUNCH("k_vocab_dz", k_vocab_dz<float>, grid, dim3(256), 0, s, v, all);
       } else if (!v.bf) {
         vocab_x3_dz(v, col0, cols, s);
       } else if (col0 == 0) {
         vocab_bf_dz(v, col0, cols, s);
       }
-      if (!v.bf || col0 == 0) db(col0);
+      if ((!v.bf || col0 == 0) && !(v.keep && v.rows == v.db_rows)) db(col0);
       char* at = (char*)dWs + (size_t)col0 * (v.wbf ? 2 : 4);
       const VocabOut out{at, v.C, 0, v.H, cols, v.wbf, 0, v.scal};
       const VocabOut sums{v.wpart, v.P, (size_t)v.H * v.P, v.H, cols, 0, 0, nullptr};
@@ -675,7 +709,7 @@ cavs_status vocab_run(cavs_ctx* ctx, const cavs_vocab* p, float* loss, float* ro
         CAVS_LAUNCH("k_vocab_dw", k_vocab_dw, dim3(cdiv(cols, 1024), v.H), dim3(256), 0, s, v.H, v.P, cols,
                     v.Sw, v.wpart, out);
     }
-    v.hbf ? dh_sum(v, (u16*)dh, s) : dh_sum(v, (float*)dh, s);
+    v.hbf ? dh_sum(v, (u16*)dh, loss, s) : dh_sum(v, (float*)dh, loss, s);
   }
   CAVS_LAUNCH_CHECK(ctx);
   return CAVS_OK;

@@ -10,34 +10,35 @@
 namespace cavs {
 namespace {
 
-constexpr int kKB = 64;   // contraction depth of a stage
+constexpr int kKB = 64;   // parts of a contraction are multiples of this,
+constexpr int kCK = 32;   // in chunks of this depth: one matrix instruction's
 
-// An operand's tile of ROWS rows, kKB deep, in LDS, and how it gets there.  A
+// An operand's tile of ROWS rows, kCK deep, in LDS, and how it gets there.  A
 // workgroup's copy instruction moves 16 bytes per thread, thread t of T to byte
 // 16 t, so the swizzles permute what a thread reads, not where it writes.
 //
-// Contiguous in the contraction: LDS rows of 128 bytes, their eight 16-byte
-// quads at quad ^ (row & 7); eight lanes that read one quad of eight rows then
+// Contiguous in the contraction: LDS rows of 64 bytes, their four 16-byte quads
+// at quad ^ (row >> 2 & 3); eight lanes that read one quad of eight rows then
 // cover the banks once.  The last quads may lie past the operand's end (kmax):
 // they read its last ones instead, which meet zeros of the other operand.
 struct RowsOp {
   const u16* p;
   long long ld;
   int rows, kmax;
+  static constexpr int kReads = 1;   // LDS reads of a fragment
+  static __device__ constexpr int quad(int row, int q) { return q ^ ((row >> 2) & 3); }
   template <int ROWS, int T>
   struct Tile {
-    static constexpr int kCopies = ROWS * 128 / (16 * T);
-    static_assert(kCopies * 16 * T == ROWS * 128, "whole copies");
+    static constexpr int kCopies = ROWS * 64 / (16 * T);
+    static_assert(kCopies * 16 * T == ROWS * 64, "whole copies");
     const u16* base[kCopies];
     int k, kmax;
     __device__ void init(const RowsOp& o, int r0, int tid) {
       kmax = o.kmax - 8;
 #pragma unroll
-      for (int i = 0; i < kCopies; ++i) {
-        const int at = i * T + tid, row = at >> 3;
-        base[i] = o.p + (size_t)min(r0 + row, o.rows - 1) * o.ld;
-      }
-      k = 8 * ((tid & 7) ^ ((tid >> 3) & 7));   // T is a multiple of 64: the same row & 7 for every i
+      for (int i = 0; i < kCopies; ++i)
+        base[i] = o.p + (size_t)min(r0 + ((i * T + tid) >> 2), o.rows - 1) * o.ld;
+      k = 8 * quad(tid >> 2, tid & 3);   // T is a multiple of 64: the same for every i
     }
     __device__ void issue(int k0, uint32_t lds) const {
       const int kk = min(k0 + k, kmax);
@@ -46,16 +47,13 @@ struct RowsOp {
         copy16_to_lds(reinterpret_cast<const float*>(base[i] + kk), lds + 16 * T * i);
     }
   };
-  // rows w0 + 16 f + r, k = 32 kk + 8 g ..
+  // rows w0 + 16 f + r, k = 8 g ..
   template <int ROWS>
   struct Frag {
-    uint32_t at[2];
-    __device__ void init(int w0, int g, int r) {
-#pragma unroll
-      for (int kk = 0; kk < 2; ++kk) at[kk] = (w0 + r) * 128 + (((4 * kk + g) ^ (r & 7)) << 4);
-    }
-    __device__ bf16x8 read(const char* lds, int kk, int f) const {
-      return *reinterpret_cast<const bf16x8*>(lds + at[kk] + f * 2048);
+    uint32_t at;
+    __device__ void init(int w0, int g, int r) { at = (w0 + r) * 64 + 16 * quad(r, g); }
+    __device__ bf16x8 read(const char* lds, int f) const {
+      return *reinterpret_cast<const bf16x8*>(lds + at + f * 1024);
     }
   };
 };
@@ -70,11 +68,13 @@ struct ColsOp {
   const u16* p;
   long long ld;
   int cols;   // columns there are (the last eight are read again past them)
+  static constexpr int kReads = 2;
+  static __device__ constexpr int swizzle(int k) { return (k & 3) | ((k >> 3) & 1) << 2; }
   template <int ROWS, int T>
   struct Tile {
     static_assert(ROWS >= 128, "eight segments to permute");
-    static constexpr int kCopies = ROWS * 128 / (16 * T);
-    static_assert(kCopies * 16 * T == ROWS * 128, "whole copies");
+    static constexpr int kCopies = ROWS * 64 / (16 * T);
+    static_assert(kCopies * 16 * T == ROWS * 64, "whole copies");
     const u16* base[kCopies];
     long long ld;
     __device__ void init(const ColsOp& o, int c0, int tid) {
@@ -82,8 +82,7 @@ struct ColsOp {
 #pragma unroll
       for (int i = 0; i < kCopies; ++i) {
         const int at = i * T + tid, k = at / (ROWS / 8), q = at % (ROWS / 8);
-        const int s = (k & 3) | ((k >> 3) & 1) << 2;
-        const int c = c0 + 16 * ((q >> 1) ^ s) + 8 * (q & 1);
+        const int c = c0 + 16 * ((q >> 1) ^ swizzle(k)) + 8 * (q & 1);
         base[i] = o.p + (size_t)k * o.ld + min(c, o.cols - 8);
       }
     }
@@ -102,11 +101,11 @@ struct ColsOp {
       s = (r >> 2) | (g & 1) << 2;
       at = (8 * g + (r >> 2)) * (2 * ROWS) + 8 * (r & 3);
     }
-    __device__ bf16x8 read(const char* lds, int kk, int f) const {
+    __device__ bf16x8 read(const char* lds, int f) const {
       typedef short s4 __attribute__((ext_vector_type(4)));
       typedef short s8 __attribute__((ext_vector_type(8)));
       typedef __attribute__((address_space(3))) s4 lds_s4;
-      const char* a = lds + at + (((seg0 + f) ^ s) << 5) + kk * 32 * (2 * ROWS);
+      const char* a = lds + at + (((seg0 + f) ^ s) << 5);
       const s4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)a);
       const s4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(a + 4 * (2 * ROWS)));
       const s8 v = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -125,13 +124,15 @@ struct Live {
 };
 
 // A workgroup of WA x WB wavefronts: A rows 16 FA WA, B rows 16 FB WB, each
-// wavefront 16 FA x 16 FB.  S stages of LDS: a stage's copies are S - 1 stages
-// ahead of its products, one barrier a stage.
-template <int WA_, int WB_, int FA_, int FB_, int S_>
+// wavefront 16 FA x 16 FB.  A ring of four chunks in LDS: a chunk's copies go out
+// four chunks ahead of its products, and its fragments are read from LDS while
+// the chunk before it is multiplied (the two sets of fragments and the sums take
+// the registers that two wavefronts a SIMD leave).  One barrier a chunk.
+template <int WA_, int WB_, int FA_, int FB_>
 struct Shape {
-  static constexpr int WA = WA_, WB = WB_, FA = FA_, FB = FB_, S = S_;
+  static constexpr int WA = WA_, WB = WB_, FA = FA_, FB = FB_, S = 4;
   static constexpr int T = 64 * WA * WB, BA = 16 * FA * WA, BB = 16 * FB * WB;
-  static constexpr int kStage = (BA + BB) * 128, kBytes = S * kStage;
+  static constexpr int kStage = (BA + BB) * 64, kBytes = S * kStage;
 };
 
 constexpr int kBand = 8;
@@ -175,7 +176,8 @@ struct Product {
     constexpr int FA = SH::FA, FB = SH::FB, S = SH::S;
     const int end = lv.what == 2 ? min(K, lv.tiles(kKB) * kKB) : K;
     const int klo = __builtin_amdgcn_readfirstlane(zi * kchunk);
-    const int nst = __builtin_amdgcn_readfirstlane(max(0, (min(end, klo + kchunk) - klo + kKB - 1) / kKB));
+    // an even number of chunks
+    const int nc = __builtin_amdgcn_readfirstlane(max(0, (min(end, klo + kchunk) - klo + kKB - 1) / kKB) * 2);
     const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, r = lane & 15;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6), wa = w % SH::WA, wb = w / SH::WA;
     typename OA::template Tile<SH::BA, SH::T> la;
@@ -191,34 +193,54 @@ struct Product {
     constexpr int kCopies = decltype(la)::kCopies + decltype(lb)::kCopies;
     const uint32_t dst = __builtin_amdgcn_readfirstlane(
         lds_addr_of(reinterpret_cast<const float*>(lds)) + 1024u * w);
-    auto issue = [&](int st) {
-      const uint32_t d = __builtin_amdgcn_readfirstlane(dst + (st % S) * SH::kStage);
-      la.issue(klo + st * kKB, d);
-      lb.issue(klo + st * kKB, d + SH::BA * 128);
+    auto issue = [&](int c) {
+      const uint32_t d = __builtin_amdgcn_readfirstlane(dst + (c % S) * SH::kStage);
+      la.issue(klo + c * kCK, d);
+      lb.issue(klo + c * kCK, d + SH::BA * 64);
+    };
+    struct Set {
+      bf16x8 a[FA], b[FB];
+    } set[2];
+    auto read = [&](Set& x, int c) {
+      const char* A = lds + (c % S) * SH::kStage;
+#pragma unroll
+      for (int f = 0; f < FB; ++f) x.b[f] = fb.read(A + SH::BA * 64, f);
+#pragma unroll
+      for (int f = 0; f < FA; ++f) x.a[f] = fa.read(A, f);
     };
 #pragma unroll
-    for (int st = 0; st < S - 1; ++st)
-      if (st < nst) issue(st);
-    ep.template prepare<SH>(lds + SH::kBytes, a0, b0);   // before the first stage's barrier
-    for (int st = 0; st < nst; ++st) {
-      // this stage has landed and the one before it has been read, everywhere
-      if (st + S - 2 < nst) wait_vmcnt_lgkm0<(S - 2) * kCopies>();
+    for (int c = 0; c < S; ++c)
+      if (c < nc) issue(c);
+    ep.template prepare<SH>(lds + SH::kBytes, a0, b0);   // before the first barrier
+    if (nc > 0) {
+      if (nc >= S) wait_vmcnt_lgkm0<(S - 1) * kCopies>();
       else wait_vmcnt_lgkm0<0>();
       barrier_nofence();
-      if (st + S - 1 < nst) issue(st + S - 1);
-      const char* A = lds + (st % S) * SH::kStage;
-      const char* B = A + SH::BA * 128;
+      read(set[0], 0);
+    }
+    for (int c0 = 0; c0 < nc; c0 += 2) {
 #pragma unroll
-      for (int kk = 0; kk < 2; ++kk) {
-        bf16x8 a[FA], b[FB];
-#pragma unroll
-        for (int f = 0; f < FB; ++f) b[f] = fb.read(B, kk, f);
-#pragma unroll
-        for (int f = 0; f < FA; ++f) a[f] = fa.read(A, kk, f);
+      for (int h = 0; h < 2; ++h) {
+        const int c = c0 + h;
+        // the next chunk has landed, and this one's fragments have been read,
+        // everywhere: its place is free
+        if (c + S - 1 < nc) wait_vmcnt_lgkm0<(S - 2) * kCopies>();
+        else wait_vmcnt_lgkm0<0>();
+        barrier_nofence();
+        if (c + S < nc) issue(c + S);
+        read(set[1 - h], c + 1);   // past the last chunk: a stale one, not used
+        const Set& x = set[h];
 #pragma unroll
         for (int i = 0; i < FA; ++i)
 #pragma unroll
-          for (int j = 0; j < FB; ++j) acc[i][j] = mfma_bf16_16x16x32(a[i], b[j], acc[i][j]);
+          for (int j = 0; j < FB; ++j) acc[i][j] = mfma_bf16_16x16x32(x.a[i], x.b[j], acc[i][j]);
+        constexpr int kReads = OA::kReads * FA + OB::kReads * FB, kPer = FA * FB / kReads > 0 ? FA * FB / kReads : 1;
+#pragma unroll
+        for (int i = 0; i < kReads; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);      // an LDS read
+          __builtin_amdgcn_sched_group_barrier(0x008, kPer, 0);   // products
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, FA * FB, 0);
       }
     }
     ep.template operator()<SH>(lds + SH::kBytes, zi, a0, b0, wa, wb, g, r, acc);
@@ -335,20 +357,15 @@ __global__ void __launch_bounds__(256, 2) k_vocab_few(VocabEp e, const u16* __re
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g = lane >> 4, r = lane & 15;
   const int a0 = blockIdx.x * kFewWords, C = e.C;
   const size_t end = (size_t)H * C;   // at least 64 values
-  // LDS as ColsOp and RowsOp have it
+  // a stage is two chunks, in LDS as ColsOp and RowsOp have them
   int ka[4], ca[4];
-  const u16* hb[2];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int at = i * 256 + tid, q = at & 15, k = at >> 4, s = (k & 3) | ((k >> 3) & 1) << 2;
-    ka[i] = k;
-    ca[i] = a0 + 16 * ((q >> 1) ^ s) + 8 * (q & 1);
+    const int at = (i & 1) * 256 + tid, q = at & 15, k = at >> 4;
+    ka[i] = kCK * (i >> 1) + k;
+    ca[i] = a0 + 16 * ((q >> 1) ^ ColsOp::swizzle(k)) + 8 * (q & 1);
   }
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int row = (i * 256 + tid) >> 3;
-    hb[i] = hp + (size_t)row * H + 8 * ((tid & 7) ^ (row & 7));
-  }
+  const u16* hb = hp + (size_t)(tid >> 2) * H + 8 * RowsOp::quad(tid >> 2, tid & 3);
   struct Stage {
     uint4 a[4], b[2];
   } st[2];
@@ -356,7 +373,7 @@ __global__ void __launch_bounds__(256, 2) k_vocab_few(VocabEp e, const u16* __re
 #pragma unroll
     for (int i = 0; i < 4; ++i) x.a[i] = vocab_load8(W, (size_t)(k0 + ka[i]) * C + ca[i], end);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) x.b[i] = *reinterpret_cast<const uint4*>(hb[i] + k0);
+    for (int i = 0; i < 2; ++i) x.b[i] = *reinterpret_cast<const uint4*>(hb + k0 + kCK * i);
   };
   ColsOp::Frag<kFewWords> fa;
   RowsOp::Frag<kFewRows> fb;
@@ -382,9 +399,9 @@ __global__ void __launch_bounds__(256, 2) k_vocab_few(VocabEp e, const u16* __re
       for (int kk = 0; kk < 2; ++kk) {
         bf16x8 a[FA], b[FB];
 #pragma unroll
-        for (int f = 0; f < FA; ++f) a[f] = fa.read(L, kk, f);
+        for (int f = 0; f < FA; ++f) a[f] = fa.read(L + kk * (kA / 2), f);
 #pragma unroll
-        for (int f = 0; f < FB; ++f) b[f] = fb.read(L + kA, kk, f);
+        for (int f = 0; f < FB; ++f) b[f] = fb.read(L + kA + kk * (kB / 2), f);
 #pragma unroll
         for (int i = 0; i < FA; ++i)
 #pragma unroll
@@ -395,8 +412,8 @@ __global__ void __launch_bounds__(256, 2) k_vocab_few(VocabEp e, const u16* __re
   vocab_few_end<TEACH, kFewWords>(e, stats, a0, [&](int i, int f) { return acc[i >> 2][f][i & 3]; });
 }
 
-using Big = Shape<2, 4, 8, 4, 2>;    // 256 x 256, eight wavefronts, 128 KB
-using Few = Shape<4, 1, 4, 4, 2>;    // 256 x 64, four wavefronts, 80 KB: two share a CU
+using Big = Shape<2, 4, 8, 4>;    // 256 x 256, eight wavefronts, 128 KB
+using Few = Shape<4, 1, 4, 4>;    // 256 x 64, four wavefronts, 80 KB: two share a CU
 
 template <bool LOSS, bool TEACH>
 using Logits = Product<Big, ColsOp, RowsOp, BfVocab<LOSS, TEACH>>;
