@@ -25,6 +25,7 @@ struct VocabNet {
   int bf;                  // products in bf16 (h and W_s rounded), else split fp32
   int hbf, wbf;            // element types of h / dh and of W_s / dW_s
   int few, pad, keep;      // at most kVocabFew rows; Ws is a padded copy; z is kept
+  int small;               // the loss on tiles of 128 words x 64 rows
   int two;                 // a second softmax, at a temperature other than 1
   float alpha, temp;
   // dz is kept in units of `unit` = 1 - alpha (alpha = 1: T), so that the label's
@@ -323,11 +324,12 @@ __device__ __forceinline__ void vocab_bias(const VocabEp& e, int a0, int g, Col 
   }
 }
 
-// A workgroup of the kernels for few rows: four wavefronts of 32 words each by 64
-// rows, z(i, f) lane (g, r)'s word col(i, g) of row 16 f + r.  The wavefronts'
-// statistics are joined into the slots of SW words.
+// A workgroup of the loss's small tiles: four wavefronts of 32 words each by 64
+// rows from row0 on, z(i, f) lane (g, r)'s word col(i, g) of row row0 + 16 f + r.
+// The wavefronts' statistics are joined into the slots of SW words.
 template <bool TEACH, int SW, class Z>
-__device__ __forceinline__ void vocab_few_end(const VocabEp& e, float (&stats)[3][4][kVocabFew], int a0, Z z) {
+__device__ __forceinline__ void vocab_few_end(const VocabEp& e, float (&stats)[3][4][kVocabFew], int a0,
+                                              int row0, Z z) {
   constexpr int NC = 32, PER = SW / NC;   // wavefronts of a slot
   const int tid = threadIdx.x, w = tid >> 6, g = (tid & 63) >> 4, r = tid & 15, aw = a0 + NC * w;
   VocabEp own = e;
@@ -343,9 +345,9 @@ __device__ __forceinline__ void vocab_few_end(const VocabEp& e, float (&stats)[3
     float x[NC / 4];
 #pragma unroll
     for (int i = 0; i < NC / 4; ++i) x[i] = z(i, f) + bias[i];
-    const int row = 16 * f + r;
+    const int row = row0 + 16 * f + r;
     vocab_rows16<true, TEACH, float, NC>(own, x, col, row, vocab_row<true, TEACH>(e, row, aw / SW, live), aw,
-                                         row, db);
+                                         16 * f + r, db);
   }
   __syncthreads();
   const int row = tid & 63;
@@ -360,7 +362,7 @@ __device__ __forceinline__ void vocab_few_end(const VocabEp& e, float (&stats)[3
     s += stats[1][PER * w + k][row] * __builtin_amdgcn_exp2f(d);
     if (TEACH && e.two) t += stats[2][PER * w + k][row] * __builtin_amdgcn_exp2f(d * e.invT);
   }
-  const size_t at = (size_t)(a0 / SW + w) * e.rows + row;
+  const size_t at = (size_t)(a0 / SW + w) * e.rows + row0 + row;
   e.pm[at] = m;
   e.ps[at] = s;
   if (TEACH && e.two) e.pt[at] = t;

@@ -485,8 +485,16 @@ size_t vocab_net(const cavs_vocab* p, bool train, char* base, VocabNet& v) {
   v.trange = (uint32_t*)take(K ? slots * rows * 4 : 0);
   v.hp = take(rows * H * es);
   v.Cq = (v.C + vec - 1) / vec * vec;
-  // the loss of few rows reads W_s as it is, the gradients do not
-  const bool pad = v.Cq != v.C && (train || !v.few);
+  // the loss on small tiles reads W_s as it is, the gradients do not
+  // Small tiles where the large ones would leave CUs without one (us, large and
+  // small; fp32, fewer than 256 tiles of 128 x 128: 172 x 5 176 x 832 76 and 51, 300
+  // x 10 000 x 512 58 and 52, 1000 x 5 000 x 512, 320 tiles, 57 and 66; bf16, fewer
+  // than 128 of 256 x 256: 172 x 5 176 x 832 37 and 26, 1000 x 5 000 x 512 31 and 28,
+  // 1000 x 10 000 x 1024, 160 tiles, 45 and 70).
+  const int big = v.bf ? 256 : 128;
+  const long large = (long)((v.n + big - 1) / big) * ((v.C + big - 1) / big);
+  v.small = v.few || large < (v.bf ? 128 : 256);
+  const bool pad = v.Cq != v.C && (train || !v.small);
   v.pad = pad;
   char* wq = take(pad ? H * (size_t)v.Cq * es : 0);
   v.Ws = pad ? wq : p->Ws;

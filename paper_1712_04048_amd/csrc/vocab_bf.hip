@@ -342,9 +342,9 @@ struct BfOut {
   }
 };
 
-// The loss over at most 64 rows: bound by reading W_s, so a workgroup takes
-// every row of 128 words (four wavefronts of 32 x 64) and keeps two stages of
-// its columns in flight in registers.  They come from W_s as it is, whatever C
+// The loss of few rows or words: 128 words x 64 rows to a workgroup (four
+// wavefronts of 32 x 64), two stages of W_s's columns in flight in registers; of
+// few rows it is bound by reading them (4 x 50 000 x 1024: 26 us, 3.9 TB/s).  They come from W_s as it is, whatever C
 // is: a 16-byte load needs no more than the alignment of its elements, where
 // the copies to LDS want four bytes (padding 50 001 columns took 53 of 140 us).
 constexpr int kFewRows = kVocabFew, kFewWords = 128;
@@ -355,7 +355,8 @@ __global__ void __launch_bounds__(256, 2) k_vocab_few(VocabEp e, const u16* __re
   __shared__ __attribute__((aligned(16))) char lds[2][kA + kB];
   __shared__ float stats[3][4][kFewRows];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g = lane >> 4, r = lane & 15;
-  const int a0 = blockIdx.x * kFewWords, C = e.C;
+  const int a0 = blockIdx.x * kFewWords, row0 = blockIdx.y * kVocabFew, C = e.C;
+  if (row0 >= *e.live) return;
   const size_t end = (size_t)H * C;   // at least 64 values
   // a stage is two chunks, in LDS as ColsOp and RowsOp have them
   int ka[4], ca[4];
@@ -365,7 +366,7 @@ __global__ void __launch_bounds__(256, 2) k_vocab_few(VocabEp e, const u16* __re
     ka[i] = kCK * (i >> 1) + k;
     ca[i] = a0 + 16 * ((q >> 1) ^ ColsOp::swizzle(k)) + 8 * (q & 1);
   }
-  const u16* hb = hp + (size_t)(tid >> 2) * H + 8 * RowsOp::quad(tid >> 2, tid & 3);
+  const u16* hb = hp + (size_t)(row0 + (tid >> 2)) * H + 8 * RowsOp::quad(tid >> 2, tid & 3);
   struct Stage {
     uint4 a[4], b[2];
   } st[2];
@@ -409,7 +410,7 @@ __global__ void __launch_bounds__(256, 2) k_vocab_few(VocabEp e, const u16* __re
       }
     }
   }
-  vocab_few_end<TEACH, kFewWords>(e, stats, a0, [&](int i, int f) { return acc[i >> 2][f][i & 3]; });
+  vocab_few_end<TEACH, kFewWords>(e, stats, a0, row0, [&](int i, int f) { return acc[i >> 2][f][i & 3]; });
 }
 
 using Big = Shape<2, 4, 8, 4>;    // 256 x 256, eight wavefronts, 128 KB
@@ -439,8 +440,8 @@ Product<Big, ColsOp, ColsOp, BfOut> dw(const VocabNet& v, int col0, int cols, co
 }  // namespace
 
 void vocab_bf_loss(const VocabNet& v, const void* W, hipStream_t s) {
-  if (v.few) {
-    const dim3 grid(cdiv(v.C, kFewWords));
+  if (v.small) {
+    const dim3 grid(cdiv(v.C, kFewWords), cdiv(v.n, kVocabFew));
     const VocabEp e = vocab_ep(v, 0);
     if (v.K > 0)
       CAVS_LAUNCH("k_vocab_few", k_vocab_few<true>, grid, dim3(256), 0, s, e, (const u16*)W, (const u16*)v.hp,

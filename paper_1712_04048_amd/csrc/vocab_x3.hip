@@ -88,7 +88,7 @@ void logits(const char* name, const VocabNet& v, int col0, int cols, hipStream_t
     x3_gemm<3, 15, 2>(name, zero_net(v), w, h, X3Vocab<LOSS, false>{e}, cols, v.rows, v.H, v.H, s, lv);
 }
 
-// The loss over at most 64 rows: a workgroup takes every row of 128 words, four
+// The loss of few rows or words: 128 words x 64 rows to a workgroup, four
 // wavefronts of 32 x 64, two stages of 32 k in flight in registers, split on
 // their way to LDS (split3.h's parts, a plane of 64-byte rows each).  W_s is read
 // as it is, at the alignment of its elements.  The 128 x 128 tiles, one chunk in
@@ -101,10 +101,11 @@ __global__ void __launch_bounds__(256, 2) k_vocab_few_x3(VocabEp e, const float*
   __shared__ __attribute__((aligned(16))) char lds[2][kPlanes];
   __shared__ float stats[3][4][kVocabFew];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g = lane >> 4, r = lane & 15;
-  const int a0 = blockIdx.x * kFewWords, C = e.C;
+  const int a0 = blockIdx.x * kFewWords, row0 = blockIdx.y * kVocabFew, C = e.C;
+  if (row0 >= *e.live) return;
   const size_t end = (size_t)H * C;   // at least 64 values
   // A: words 2 lane, 2 lane + 1, k octet w; B: row tid / 4, octet tid % 4
-  const float* hb = hp + (size_t)(tid >> 2) * H + 8 * (tid & 3);
+  const float* hb = hp + (size_t)(row0 + (tid >> 2)) * H + 8 * (tid & 3);
   struct Stage {
     float2 a[8];
     float4 b[2];
@@ -182,18 +183,18 @@ __global__ void __launch_bounds__(256, 2) k_vocab_few_x3(VocabEp e, const float*
           const int c = a0 + 32 * w + 16 * i + 4 * g + q;
           float s = 0.f;
           if (c < C)
-            for (int k = 0; k < H; ++k) s = fmaf(W[(size_t)k * C + c], hp[(size_t)(16 * f + r) * H + k], s);
+            for (int k = 0; k < H; ++k) s = fmaf(W[(size_t)k * C + c], hp[(size_t)(row0 + 16 * f + r) * H + k], s);
           acc[i][f][q] = s;
         }
   }
-  vocab_few_end<TEACH, 64>(e, stats, a0, [&](int i, int f) { return acc[i >> 2][f][i & 3]; });
+  vocab_few_end<TEACH, 64>(e, stats, a0, row0, [&](int i, int f) { return acc[i >> 2][f][i & 3]; });
 }
 
 }  // namespace
 
 void vocab_x3_loss(const VocabNet& v, const void* W, hipStream_t s) {
-  if (v.few) {
-    const dim3 grid(cdiv(v.C, kFewWords));
+  if (v.small) {
+    const dim3 grid(cdiv(v.C, kFewWords), cdiv(v.n, kVocabFew));
     const VocabEp e = vocab_ep(v, 0);
     if (v.K > 0)
       CAVS_LAUNCH("k_vocab_few_x3", k_vocab_few_x3<true>, grid, dim3(256), 0, s, e, (const float*)W,

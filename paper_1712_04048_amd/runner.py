@@ -128,3 +128,67 @@ class Batch:
             for k, v in self.grads.items():
                 r[k] = v.double().cpu().numpy()
         return r
+
+
+class LmBatch(Batch):
+    """A language model over one batch: the words that vertices pull come from a
+    table (``words[r]`` is the word of input row r), and every labelled vertex's
+    state is scored over the vocabulary by cavs_vocab_grad, which keeps no
+    logits.  The workload's X is not used; its Ws, bs and push_idx are the head
+    and the labels.  ``teacher``: (words [V, K], logits [V, K], alpha, temp) of a
+    model to learn from; ``head_dtype``: the type of the head's weights."""
+
+    def __init__(self, wl: Workload, table: torch.Tensor, words, ctx: Optional[B.Context] = None,
+                 device: int = 0, scale: float = 1.0, teacher=None,
+                 head_dtype: torch.dtype = torch.float32):
+        super().__init__(wl, ctx, device)
+        p, dev = self.params, self.dev
+        self.emb = B.Embedding(table, scale)
+        self.words = torch.as_tensor(np.ascontiguousarray(words, dtype=np.int32)).to(dev)
+        self.X = torch.empty(wl.n_x, wl.D, dtype=torch.float32, device=dev)
+        self.Ws, self.bs = p.Ws.to(head_dtype), p.bs
+        self.params = B.Params(p.cell, p.prec, B.LOSS_NONE, p.D, p.H, p.N, 0, p.Wx, p.U, p.b,
+                               None, None)
+        self.teacher = teacher
+        self.head: Optional[B.VocabHead] = None
+
+    def alloc(self):
+        super().alloc()
+        wl, dev = self.wl, self.dev
+        t = {}
+        if self.teacher is not None:
+            word, logit, alpha, temp = self.teacher
+            t = dict(top_word=torch.as_tensor(word, dtype=torch.int32).to(dev),
+                     top_logit=torch.as_tensor(logit, dtype=torch.float32).to(dev),
+                     alpha=alpha, temp=temp)
+        self.head = B.VocabHead(h=self.h, Ws=self.Ws, bs=self.bs, label=self.push_idx, **t)
+        self.dH_ext = torch.empty_like(self.h)
+        self.grads["dWs"] = torch.empty_like(self.Ws)
+        self.grads["dbs"] = torch.empty_like(self.bs)
+        self.grads["dE"] = torch.empty_like(self.emb.E)
+        self.row_loss = torch.empty(wl.V, dtype=torch.float32, device=dev)
+        u8 = dict(dtype=torch.uint8, device=dev)
+        self.ws_head = torch.empty(max(1, B.vocab_workspace_bytes(self.head, True)), **u8)
+        self.ws_emb = torch.empty(max(1, B.embed_grad_workspace_bytes(self.emb, wl.n_x)), **u8)
+
+    def forward(self):
+        B.embed(self.ctx, self.emb, self.words, self.X)
+        none = torch.empty(1, dtype=torch.float32, device=self.dev)   # CAVS_LOSS_NONE's 0
+        B.forward(self.ctx, self.params, self.sched, self.X, None, self.ws, self.h, self.c, none)
+        g = self.grads
+        B.vocab_grad(self.ctx, self.head, self.loss, self.row_loss, self.dH_ext, g["dWs"], g["dbs"],
+                     self.ws_head)
+
+    def backward(self):
+        super().backward()
+        B.embed_grad(self.ctx, self.emb, self.words, self.grads["dX"], self.grads["dE"], self.ws_emb)
+
+    def infer(self):
+        """The states and the loss alone (cavs_infer, cavs_vocab_loss)."""
+        B.embed(self.ctx, self.emb, self.words, self.X)
+        if self.ws_infer is None:
+            n = B.infer_workspace_bytes(self.params, self.sched)
+            self.ws_infer = torch.empty(max(n, 1), dtype=torch.uint8, device=self.dev)
+        none = torch.empty(1, dtype=torch.float32, device=self.dev)
+        B.infer(self.ctx, self.params, self.sched, self.X, None, self.ws_infer, self.h, self.c, none)
+        B.vocab_loss(self.ctx, self.head, self.loss, self.row_loss, self.ws_head)
