@@ -338,12 +338,12 @@ cavs_status cavs_backward(cavs_ctx* ctx, const cavs_params* params, const cavs_s
 
 typedef struct {
   int32_t e_type, x_type;   /* CAVS_T_*: the table E (and dE); the rows X (and dX) */
-  int32_t n_words, D;       /* E [n_words, D], both > 0 */
+  int32_t n_words, D;       /* E [n_words, D], both > 0; at most 2^28 and 2^14 */
   const void* E;            /* cavs_embed: the table; cavs_embed_grad: unused */
   float scale;
 } cavs_embedding;
 
-/* X[i] = scale * E[word[i]], i < n; word -1: a row of zeros. */
+/* X[i] = scale * E[word[i]], i < n <= 2^28; word -1: a row of zeros. */
 cavs_status cavs_embed(cavs_ctx* ctx, const cavs_embedding* e, const int32_t* word, int32_t n,
                        void* X);
 
@@ -353,7 +353,8 @@ size_t cavs_embed_grad_workspace_bytes(const cavs_embedding* e, int32_t n);
 /* dE[v] = scale * (sum of dX[i] over the i with word[i] = v), every row of dE
    written.  The words are sorted and each row's terms added in a fixed order
    (ascending i, in parts of 32 where a word occurs more often), so that the
-   result does not change from run to run. */
+   result does not change from run to run.  n and n_words are at most 2^22
+   here. */
 cavs_status cavs_embed_grad(cavs_ctx* ctx, const cavs_embedding* e, const int32_t* word, int32_t n,
                             const void* dX, void* dE, void* ws, size_t ws_bytes);
 
@@ -387,7 +388,8 @@ typedef struct {
 
 /* Bytes of device workspace cavs_vocab_loss (train = 0) or cavs_vocab_grad
    (train = 1) needs: of n (H + C / 8) order for the loss, and for the gradient
-   one piece of dL/dz of about 256 MB, whatever C is.  0 on bad args. */
+   pieces of dL/dz of about 256 MB (and, where a piece is all of it, z), whatever
+   C is.  The pointers are not read, but a NULL label is none.  0 on bad args. */
 size_t cavs_vocab_workspace_bytes(const cavs_vocab* v, int32_t train);
 
 /* loss [1] = L; row_loss [n] (or NULL) the terms of the mean, 0 for rows that

@@ -11,8 +11,9 @@
 namespace cavs {
 namespace {
 
-// Sizes whose indices the kernels count in 32 bits.
-constexpr int kEmbedMax = 1 << 28, kEmbedMaxD = 1 << 20;
+// Sizes whose indices the kernels count in 32 bits.  The gradient's sort reads
+// every place once for each 512 words of the table, which bounds both.
+constexpr int kEmbedMax = 1 << 28, kEmbedMaxD = 1 << 14, kGradMax = 1 << 22;
 constexpr int kPart = 32;         // rows of a word that one wavefront adds
 constexpr int kSortWords = 512;   // most words of a sorting workgroup
 
@@ -272,6 +273,15 @@ cavs_status embed_args(cavs_ctx* ctx, const cavs_embedding* e, int n) {
   return CAVS_OK;
 }
 
+cavs_status embed_grad_args(cavs_ctx* ctx, const cavs_embedding* e, int n) {
+  cavs_status st = embed_args(ctx, e, n);
+  if (st != CAVS_OK) return st;
+  if (n > kGradMax || e->n_words > kGradMax)
+    return fail(ctx, CAVS_ERR_UNSUPPORTED, "gradient of n=%d places, n_words=%d: at most %d each", n,
+                e->n_words, kGradMax);
+  return CAVS_OK;
+}
+
 bool element_aligned(const void* p, int type) {
   return ((uintptr_t)p & (type == CAVS_T_BF16 ? 1 : 3)) == 0;
 }
@@ -362,12 +372,12 @@ cavs_status embed_run(cavs_ctx* ctx, const cavs_embedding* e, const int* word, i
 
 size_t embed_grad_ws_bytes(const cavs_embedding* e, int n) {
   EmbedWs w;
-  return embed_args(nullptr, e, n) == CAVS_OK ? embed_ws(e, n, nullptr, w) : 0;
+  return embed_grad_args(nullptr, e, n) == CAVS_OK ? embed_ws(e, n, nullptr, w) : 0;
 }
 
 cavs_status embed_grad_run(cavs_ctx* ctx, const cavs_embedding* e, const int* word, int n, const void* dX,
                            void* dE, void* ws, size_t ws_bytes) {
-  cavs_status st = embed_args(ctx, e, n);
+  cavs_status st = embed_grad_args(ctx, e, n);
   if (st != CAVS_OK) return st;
   if (!dE || (n > 0 && (!word || !dX))) return fail(ctx, CAVS_ERR_ARG, "word, dX and dE are required");
   if (!element_aligned(dE, e->e_type) || !element_aligned(dX, e->x_type))

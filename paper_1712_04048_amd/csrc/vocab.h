@@ -5,8 +5,9 @@
 //
 // Rows without a label take no part: the live rows are listed first (rows[],
 // ascending) and everything below works on that compact numbering, whose
-// length only the device knows (live[0]).  Every buffer by row has kVocabRows-
-// padded capacity; rows from the live ones to the end of their tile hold zeros.
+// length only the device knows (live[0]).  Every buffer by row has kVocabTile-
+// padded capacity; the rows of hp and dZ that follow the live ones in the
+// gradients' contraction hold zeros.
 #pragma once
 
 #include <type_traits>

@@ -23,7 +23,7 @@ constexpr size_t kKeepBytes = (size_t)128 << 20;
 constexpr int kVocabMaxRows = 1 << 20, kVocabMaxWords = 1 << 20, kVocabMaxH = 1 << 15;
 
 // The live rows: their list and numbering, their labels, their rows of h in the
-// products' type (zeros to the end of their last tile), and unit / their number.
+// products' type (zeros behind the last), and unit / their number.
 // A workgroup takes R of the caller's rows and counts the labels before them
 // itself, so that nothing waits for a list: R is at least 16 and at least n /
 // 512, which bounds what all of them read to 512 n labels.
@@ -90,9 +90,11 @@ __global__ void __launch_bounds__(256) k_vocab_rows(VocabNet v, int R, const int
     *v.live = before;
     *v.scal = v.unit / (float)max(before, 1);
   }
-  // H is a multiple of 64: whole 16 bytes
+  // Zeros as far as they can meet a live row's: to the end of a chunk of dW_s's
+  // contraction, and in fp32 of a tile (a NaN in it would have it formed again).
+  // H is a multiple of 64: whole 16 bytes.
   const size_t from = (size_t)before * H * sizeof(OUT);
-  const int tile = v.few ? kVocabFew : kVocabTile;
+  const int tile = v.bf || v.few ? kVocabFew : 2 * kVocabFew;
   const size_t to = (size_t)cdiv_dev(before, tile) * tile * H * sizeof(OUT);
   for (size_t o = from + 16 * tid; o < to; o += 256 * 16) st4((float*)((char*)v.hp + o), f4zero());
 }
@@ -415,7 +417,7 @@ __global__ void __launch_bounds__(256) k_vocab_dh(int n, int H, size_t part, int
   __shared__ float4 quarter[WIDE ? 4 : 1][64];
   if (blockIdx.x == 0 && blockIdx.y == 0) vocab_mean(val, *live, loss);
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int i = WIDE ? blockIdx.y : blockIdx.y * 4 + w, c = (blockIdx.x * 64 + lane) * 4;
+  const int i = WIDE ? blockIdx.x : blockIdx.x * 4 + w, c = (blockIdx.y * 64 + lane) * 4;
   const int per = cdiv_dev(S, 4), z0 = WIDE ? min(w * per, S) : 0, z1 = WIDE ? min(z0 + per, S) : S;
   if (!WIDE && i >= n) return;
   const int k = place[i];
@@ -573,7 +575,7 @@ size_t vocab_net(const cavs_vocab* p, bool train, char* base, VocabNet& v) {
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
-cavs_status vocab_args(cavs_ctx* ctx, const cavs_vocab* p) {
+cavs_status vocab_sizes(cavs_ctx* ctx, const cavs_vocab* p) {
   if (!p) return fail(ctx, CAVS_ERR_ARG, "null vocabulary head");
   if ((p->h_type != CAVS_T_F32 && p->h_type != CAVS_T_BF16) ||
       (p->w_type != CAVS_T_F32 && p->w_type != CAVS_T_BF16))
@@ -585,17 +587,24 @@ cavs_status vocab_args(cavs_ctx* ctx, const cavs_vocab* p) {
                 kVocabMaxRows, kVocabMaxWords, kVocabMaxH);
   if (p->K > kVocabMaxK)
     return fail(ctx, CAVS_ERR_UNSUPPORTED, "K=%d teacher's words (max %d)", p->K, kVocabMaxK);
-  if (!p->Ws || (p->n > 0 && !p->h)) return fail(ctx, CAVS_ERR_ARG, "h and Ws are required");
-  if (!aligned16(p->h) || !aligned16(p->Ws))
-    return fail(ctx, CAVS_ERR_ARG, "h and Ws must be aligned to 16 bytes");
   if (p->K > 0) {
-    if (p->n > 0 && (!p->top_word || !p->top_logit))
-      return fail(ctx, CAVS_ERR_ARG, "top_word and top_logit are required with K=%d", p->K);
     if (!(p->alpha >= 0.f && p->alpha <= 1.f)) return fail(ctx, CAVS_ERR_ARG, "alpha outside [0, 1]");
-    if (!(p->temp > 0.f && p->temp < INFINITY)) return fail(ctx, CAVS_ERR_ARG, "temp must be positive");
+    if (!(p->temp > 0.f && p->temp < INFINITY && 1.f / p->temp < INFINITY))
+      return fail(ctx, CAVS_ERR_ARG, "temp must be positive, it and its inverse finite");
   }
   if (!p->label && p->n > 0 && !(p->K > 0 && p->alpha == 1.f))
     return fail(ctx, CAVS_ERR_ARG, "labels are required unless the teacher alone is learned from");
+  return CAVS_OK;
+}
+
+cavs_status vocab_args(cavs_ctx* ctx, const cavs_vocab* p) {
+  cavs_status st = vocab_sizes(ctx, p);
+  if (st != CAVS_OK) return st;
+  if (!p->Ws || (p->n > 0 && !p->h)) return fail(ctx, CAVS_ERR_ARG, "h and Ws are required");
+  if (!aligned16(p->h) || !aligned16(p->Ws))
+    return fail(ctx, CAVS_ERR_ARG, "h and Ws must be aligned to 16 bytes");
+  if (p->K > 0 && p->n > 0 && (!p->top_word || !p->top_logit))
+    return fail(ctx, CAVS_ERR_ARG, "top_word and top_logit are required with K=%d", p->K);
   return CAVS_OK;
 }
 
@@ -611,10 +620,10 @@ void dh_sum(const VocabNet& v, OUT* dh, float* loss, hipStream_t s) {
   const size_t part = (size_t)v.rows * v.H;
   const int gx = cdiv(v.H, 256);
   if (v.Sh >= 8)
-    CAVS_LAUNCH("k_vocab_dh", (k_vocab_dh<OUT, true>), dim3(gx, v.n), dim3(256), 0, s, v.n, v.H, part, v.Sh,
+    CAVS_LAUNCH("k_vocab_dh", (k_vocab_dh<OUT, true>), dim3(v.n, gx), dim3(256), 0, s, v.n, v.H, part, v.Sh,
                 v.place, v.hpart, v.scal, dh, v.val, v.live, loss);
   else
-    CAVS_LAUNCH("k_vocab_dh", (k_vocab_dh<OUT, false>), dim3(gx, cdiv(v.n, 4)), dim3(256), 0, s, v.n, v.H, part,
+    CAVS_LAUNCH("k_vocab_dh", (k_vocab_dh<OUT, false>), dim3(cdiv(v.n, 4), gx), dim3(256), 0, s, v.n, v.H, part,
                 v.Sh, v.place, v.hpart, v.scal, dh, v.val, v.live, loss);
 }
 
@@ -627,7 +636,7 @@ VocabEp vocab_ep(const VocabNet& v, int col0) {
 }
 
 size_t vocab_ws_bytes(const cavs_vocab* p, bool train) {
-  if (vocab_args(nullptr, p) != CAVS_OK) return 0;
+  if (vocab_sizes(nullptr, p) != CAVS_OK) return 0;
   VocabNet v;
   return p->n > 0 ? vocab_net(p, train, nullptr, v) : 0;
 }

@@ -94,8 +94,10 @@ def check(got, want, bound):
     assert all(v <= 1.0 for v in far.values()), far
 
 
+# one row and word to many; few rows, few words, tiles of either size, odd ends
 SHAPES = [(1, 1, 64), (1, 17, 64), (3, 100, 128), (64, 1000, 64), (65, 255, 320), (257, 513, 64),
-          (300, 2049, 192), (1000, 4100, 128), (17, 20001, 256), (640, 64, 512)]
+          (300, 2049, 192), (1000, 4100, 128), (17, 20001, 256), (640, 64, 512),
+          (40000, 33, 64), (130, 40003, 64), (64, 129, 1088), (2100, 4097, 64)]
 
 
 @pytest.mark.parametrize("types", [(F32, F32), (BF16, BF16), (F32, BF16), (BF16, F32)])
@@ -142,11 +144,17 @@ def test_teacher_alone_needs_no_labels(ctx, types):
         assert torch.equal(with_labels[k], without[k]), k
 
 
-@pytest.mark.parametrize("types", [(F32, F32), (BF16, BF16)])
-def test_pieces_of_the_vocabulary(ctx, types):
-    """More than 256 MB of dL/dz: two pieces and more, the last one narrower."""
-    n, C = (8300, 8801) if types[0] == F32 else (16500, 8801)
-    head = make(5, n, C, 64, types, pad=0.1)
+@pytest.mark.parametrize("types,n,C,H,K", [
+    # more than 256 MB of dL/dz: two pieces, the last one narrower
+    ((F32, F32), 8300, 8801, 64, 0), ((BF16, BF16), 16500, 8801, 64, 0),
+    ((F32, F32), 8300, 8801, 64, 3), ((BF16, BF16), 16500, 8801, 64, 3),
+    # three, with few rows live
+    ((BF16, BF16), 60000, 5800, 64, 0),
+    # one piece whose z is formed twice (bf16), and kept (H = 1024)
+    ((BF16, BF16), 5000, 7100, 64, 0), ((BF16, BF16), 5000, 7100, 64, 5),
+    ((BF16, BF16), 300, 5003, 1024, 5), ((BF16, BF16), 3000, 12000, 1024, 0)])
+def test_pieces_of_the_vocabulary(ctx, types, n, C, H, K):
+    head = make(5, n, C, H, types, pad=0.95 if n == 60000 else 0.1, K=K, alpha=0.4, temp=2.0)
     want, bound = reference(head)
     got = grad(ctx, head)
     ctx.sync()

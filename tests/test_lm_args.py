@@ -119,3 +119,31 @@ def test_embedding_tensors_are_checked():
             B.Embedding(bad).raw(torch.float32)
     with pytest.raises(B.CavsError):
         B.Embedding(E).raw(torch.float16)
+
+
+def test_sizes_past_the_kernels_are_refused():
+    """Through the C ABI, whose queries read no memory."""
+    _ensure_built()
+    L = B.lib()
+
+    def vocab(**kw):
+        d = dict(h_type=0, w_type=0, n=10, H=64, C=100, label=16)
+        d.update(kw)
+        return L.cavs_vocab_workspace_bytes(ct.byref(B.cavs_vocab(**d)), 1)
+
+    assert vocab() > 0 and vocab(n=1 << 20, C=1 << 20) > 0 and vocab(H=1 << 15) > 0
+    for kw in (dict(n=(1 << 20) + 1), dict(C=(1 << 20) + 1), dict(H=(1 << 15) + 64), dict(H=0), dict(C=0),
+               dict(n=-1), dict(K=-1), dict(h_type=2), dict(w_type=-1),
+               dict(K=3, alpha=0.5, temp=1e-40)):
+        assert vocab(**kw) == 0, kw
+
+    def grad(n=10, **kw):
+        d = dict(e_type=0, x_type=0, n_words=10, D=8)
+        d.update(kw)
+        return L.cavs_embed_grad_workspace_bytes(ct.byref(B.cavs_embedding(**d)), n)
+
+    assert grad() > 0 and grad(n=1 << 22, n_words=1 << 22) > 0 and grad(D=1 << 14) > 0
+    for kw in (dict(n=(1 << 22) + 1), dict(n_words=(1 << 22) + 1), dict(D=(1 << 14) + 1), dict(e_type=2),
+               dict(x_type=-1)):
+        assert grad(**kw) == 0, kw
+    assert L.cavs_vocab_workspace_bytes(None, 0) == 0 and L.cavs_embed_grad_workspace_bytes(None, 1) == 0
