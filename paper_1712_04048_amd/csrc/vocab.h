@@ -424,12 +424,11 @@ inline char* vocab_dz_at(const VocabNet& v, int col0) {
 }
 
 // The products, by type.  loss: statistics of every word (few rows: from the
-// caller's W, without a padded copy); dz: one piece's dZ and dbp; dh: the
-// piece's share of hpart; dw: the piece's columns of dW_s; grads: both.
+// caller's W, without a padded copy); dz: one piece's dZ and dbp; grads:
+// the piece's share of hpart (dL/dh) and its columns of dW_s.
 void vocab_x3_loss(const VocabNet& v, const void* W, hipStream_t s);
 void vocab_x3_dz(const VocabNet& v, int col0, int cols, hipStream_t s);
-void vocab_x3_dh(const VocabNet& v, int col0, int cols, hipStream_t s);
-void vocab_x3_dw(const VocabNet& v, int col0, int cols, const VocabOut& o, hipStream_t s);
+void vocab_x3_grads(const VocabNet& v, int col0, int cols, const VocabOut& o, hipStream_t s);
 void vocab_bf_loss(const VocabNet& v, const void* W, hipStream_t s);
 void vocab_bf_dz(const VocabNet& v, int col0, int cols, hipStream_t s);
 void vocab_bf_grads(const VocabNet& v, int col0, int cols, int next, const VocabOut& o, hipStream_t s);

@@ -538,34 +538,26 @@ size_t vocab_net(const cavs_vocab* p, bool train, char* base, VocabNet& v) {
   auto h_ok = [&](int S) { return S == 1 || (whole(kh, S) >= 4 && S * hmb <= 64); };
   auto w_cost = [&](int S) { return S > 1 ? 2 * S * wmb / 6.4 + 3 : 0; };
   auto h_cost = [&](int S) { return 2 * S * hmb / 6.4; };
+  // One launch, longer items first: it ends about a shorter item after the CUs'
+  // mean load, and not before a longer one.  Two fp32 workgroups share a CU: an
+  // item takes twice as long beside another, the last ones half of that.  In bf16
+  // with pieces the next one's dz follows, in short items; of few rows dL/dh is a
+  // launch of its own on small tiles, two a CU.
+  const double dz = v.H / 64 + 8., more = v.bf && v.P < v.C ? dz * tiles(v.n) * tiles(width) : 0.;
+  const bool apart = v.bf && v.few;
+  const double lw = (double)tw * kw / 256, lh = (double)th * kh / 256;
+  const double shared = v.bf ? 1. : 2., after = 1. / shared;
   int bw = 1, bh = 1;
-  if (v.bf && !v.few) {
-    // One launch, longer items first: it ends about a shorter item after the
-    // CUs' mean load.  With pieces the next one's dz follows, in short items.
-    const double dz = v.H / 64 + 8., more = v.P < v.C ? dz * tiles(v.n) * tiles(width) : 0.;
-    const double load = ((double)tw * kw + (double)th * kh + more) / 256;
-    double best = 1e30;
-    for (int sw : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64})
-      for (int sh : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
-        if (!w_ok(sw) || !h_ok(sh)) break;
-        const double iw = whole(kw, sw), ih = whole(kh, sh), last = more > 0. ? dz : std::min(iw, ih);
-        const double t = std::max({load + last, iw, ih}) + w_cost(sw) + h_cost(sh);
-        if (t < best) best = t, bw = sw, bh = sh;
-      }
-  } else {
-    // One after the other, two workgroups a CU: rounds of 512, the last one
-    // faster if it leaves each its CU.
-    auto time = [&](int items, int stages) {
-      const int rest = items % 512;
-      return stages * (2. * (items / 512) + (rest == 0 ? 0. : rest <= 256 ? 1.1 : 2.));
-    };
-    double best_w = 1e30, best_h = 1e30;
-    for (int S = 1; S <= 64; ++S) {
-      const double w = time(tw * S, whole(kw, S)) + w_cost(S), h = time(th * S, whole(kh, S)) + h_cost(S);
-      if (w_ok(S) && w < best_w) best_w = w, bw = S;
-      if (h_ok(S) && h < best_h) best_h = h, bh = S;
+  double best = 1e30;
+  for (int sw : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64})
+    for (int sh : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+      if (!w_ok(sw) || !h_ok(sh)) break;
+      const double iw = whole(kw, sw), ih = whole(kh, sh), last = more > 0. ? dz : std::min(iw, ih);
+      double t = apart ? std::max(lw, iw) + lh + ih
+                       : std::max({lw + lh + more / 256 + after * last, shared * iw, shared * ih});
+      t += w_cost(sw) + h_cost(sh);
+      if (t < best) best = t, bw = sw, bh = sh;
     }
-  }
   v.Sw = whole(kw, whole(kw, bw));   // no part without a stage
   v.Sh = whole(kh, whole(kh, bh));
   v.hpart = (float*)take((size_t)v.Sh * rows * H * 4);
@@ -719,8 +711,7 @@ cavs_status vocab_run(cavs_ctx* ctx, const cavs_vocab* p, float* loss, float* ro
         vocab_bf_grads(v, col0, cols, next, o, s);
         if (next > 0) db(col0 + v.P);
       } else {
-        vocab_x3_dw(v, col0, cols, o, s);
-        vocab_x3_dh(v, col0, cols, s);
+        vocab_x3_grads(v, col0, cols, o, s);
       }
       if (v.Sw > 1)
         CAVS_LAUNCH("k_vocab_dw", k_vocab_dw, dim3(cdiv(cols, 1024), v.H), dim3(256), 0, s, v.H, v.P, cols,

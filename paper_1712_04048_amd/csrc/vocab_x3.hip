@@ -211,20 +211,17 @@ void vocab_x3_dz(const VocabNet& v, int col0, int cols, hipStream_t s) {
   logits<false>("k_x3_gemm<vocab dz>", v, col0, cols, s);
 }
 
-void vocab_x3_dh(const VocabNet& v, int col0, int cols, hipStream_t s) {
+void vocab_x3_grads(const VocabNet& v, int col0, int cols, const VocabOut& o, hipStream_t s) {
   // a quad past C is the padded copy's zeros (X3Rows reads whole quads)
-  const int K = cols, kchunk = cdiv(cdiv(K, kBK), v.Sh) * kBK;
-  const VocabOut o{v.hpart, v.H, (size_t)v.rows * v.H, v.rows, v.H, 0, col0 > 0, nullptr};
-  x3_gemm<3, 15, 2>("k_x3_gemm<vocab dh>", zero_net(v), X3Rows{(const float*)v.dZ, v.P, v.rows},
-                    X3Rows{(const float*)v.Ws + col0, v.ldw, v.H}, X3VocabOut{o}, v.rows, v.H, K,
-                    kchunk, s, LiveRows{v.live, cdiv(K, kchunk)});
-}
-
-void vocab_x3_dw(const VocabNet& v, int col0, int cols, const VocabOut& o, hipStream_t s) {
-  const int nch = cdiv(v.n, kBK), kchunk = cdiv(nch, v.Sw) * kBK;
-  x3_gemm<3, 15, 2>("k_x3_gemm<vocab dw>", zero_net(v), X3Cols{(const float*)v.hp, v.H, v.H},
-                    X3Cols{(const float*)v.dZ, v.P, v.P}, X3VocabOut{o}, v.H, cols, nch * kBK,
-                    kchunk, s, LiveK{v.live});
+  const int hchunk = cdiv(cdiv(cols, kBK), v.Sh) * kBK;
+  const VocabOut sums{v.hpart, v.H, (size_t)v.rows * v.H, v.rows, v.H, 0, col0 > 0, nullptr};
+  const X3Product dh(X3Rows{(const float*)v.dZ, v.P, v.rows}, X3Rows{(const float*)v.Ws + col0, v.ldw, v.H},
+                     X3VocabOut{sums}, LiveRows{v.live, cdiv(cols, hchunk)}, v.rows, v.H, cols, hchunk);
+  const int nch = cdiv(v.n, kBK), wchunk = cdiv(nch, v.Sw) * kBK;
+  const X3Product dw(X3Cols{(const float*)v.hp, v.H, v.H}, X3Cols{(const float*)v.dZ, v.P, v.P}, X3VocabOut{o},
+                     LiveK{v.live}, v.H, cols, nch * kBK, wchunk);
+  if (wchunk >= hchunk) x3_two("k_x3_two<vocab dw, dh>", zero_net(v), dw, dh, s);   // longer items first
+  else x3_two("k_x3_two<vocab dw, dh>", zero_net(v), dh, dw, s);
 }
 
 }  // namespace cavs

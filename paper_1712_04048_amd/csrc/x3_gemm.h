@@ -122,14 +122,10 @@ struct X3Sized {
   __device__ void operator()(int&, int&, int&, int&) const {}
 };
 constexpr int kX3Band = 8;
-template <class LA, class LB, class EP, class LV, int PARTS, int BLOCKS, int WGS>
-__global__ void __launch_bounds__(256, WGS) k_x3_gemm(Net n, LA la, LB lb, EP ep, LV lv, int ty,
-                                                      int tx, int K, int kchunk, int items) {
+template <int PARTS, int BLOCKS, class LA, class LB, class EP>
+__device__ __forceinline__ void x3_tile(char* lds, const Net& n, const LA& la, const LB& lb, const EP& ep,
+                                        int ty, int tx, int K, int kchunk, int item) {
   constexpr int OPB = PARTS * kX3Plane;
-  __shared__ __attribute__((aligned(16))) char lds[2 * OPB];
-  lv(ty, tx, K, items);
-  const int item = xcd_item(blockIdx.x, items);
-  if (item < 0) return;
   const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, g = lane >> 4, r = lane & 15;
   const int wm = w & 1, wn = w >> 1, z = item / (tx * ty), it = item % (tx * ty);
   const int band = it / (kX3Band * ty), in = it % (kX3Band * ty);
@@ -170,6 +166,16 @@ __global__ void __launch_bounds__(256, WGS) k_x3_gemm(Net n, LA la, LB lb, EP ep
   ep(n, z, m0, n0, wm, wn, g, r, acc);
 }
 
+template <class LA, class LB, class EP, class LV, int PARTS, int BLOCKS, int WGS>
+__global__ void __launch_bounds__(256, WGS) k_x3_gemm(Net n, LA la, LB lb, EP ep, LV lv, int ty,
+                                                      int tx, int K, int kchunk, int items) {
+  __shared__ __attribute__((aligned(16))) char lds[2 * PARTS * kX3Plane];
+  lv(ty, tx, K, items);
+  const int item = xcd_item(blockIdx.x, items);
+  if (item < 0) return;
+  x3_tile<PARTS, BLOCKS>(lds, n, la, lb, ep, ty, tx, K, kchunk, item);
+}
+
 template <int PARTS, int BLOCKS, int WGS, class LA, class LB, class EP, class LV = X3Sized>
 void x3_gemm(const char* name, const Net& n, LA la, LB lb, EP ep, int M, int Nc, int K, int kchunk,
              hipStream_t s, LV lv = LV{}) {
@@ -177,6 +183,39 @@ void x3_gemm(const char* name, const Net& n, LA la, LB lb, EP ep, int M, int Nc,
   const int items = tx * ty * (K > 0 ? cdiv(K, kchunk) : 1);
   CAVS_LAUNCH(name, (k_x3_gemm<LA, LB, EP, LV, PARTS, BLOCKS, WGS>), dim3(xcd_grid(items)), dim3(256),
               0, s, n, la, lb, ep, lv, ty, tx, K, kchunk, items);
+}
+
+// Two independent products of split operands in one launch, the first one's
+// workgroups first: either fills the CUs that the other leaves.
+template <class LA, class LB, class EP, class LV>
+struct X3Product {
+  LA la;
+  LB lb;
+  EP ep;
+  LV lv;
+  int ty, tx, K, kchunk, items;
+  X3Product(LA a, LB b, EP e, LV l, int M, int Nc, int K_, int kchunk_)
+      : la(a), lb(b), ep(e), lv(l), ty(cdiv(M, kX3Tile)), tx(cdiv(Nc, kX3Tile)), K(K_), kchunk(kchunk_),
+        items(ty * tx * cdiv(K_, kchunk_)) {}
+};
+template <class P, class Q>
+__global__ void __launch_bounds__(256, 2) k_x3_two(Net n, P p, Q q) {
+  __shared__ __attribute__((aligned(16))) char lds[2 * 3 * kX3Plane];
+  p.lv(p.ty, p.tx, p.K, p.items);
+  q.lv(q.ty, q.tx, q.K, q.items);
+  const int x = blockIdx.x & 7, at = blockIdx.x >> 3, per = (p.items + 7) / 8;
+  if (at < per) {
+    const int item = x * per + at;
+    if (item < p.items) x3_tile<3, 15>(lds, n, p.la, p.lb, p.ep, p.ty, p.tx, p.K, p.kchunk, item);
+  } else {
+    const int per2 = (q.items + 7) / 8, item = x * per2 + at - per;
+    if (at - per < per2 && item < q.items)
+      x3_tile<3, 15>(lds, n, q.la, q.lb, q.ep, q.ty, q.tx, q.K, q.kchunk, item);
+  }
+}
+template <class P, class Q>
+void x3_two(const char* name, const Net& n, const P& p, const Q& q, hipStream_t s) {
+  CAVS_LAUNCH(name, (k_x3_two<P, Q>), dim3(xcd_grid(p.items) + xcd_grid(q.items)), dim3(256), 0, s, n, p, q);
 }
 
 }  // namespace cavs
