@@ -369,9 +369,8 @@ __device__ __forceinline__ void vocab_few_end(const VocabEp& e, float (&stats)[3
   if (TEACH && e.two) e.pt[at] = t;
 }
 
-// Eight (bf16) or two (float) adjacent values from element o on of a matrix of
-// `end` elements (at least 64): where it ends among them, or before, what there
-// is and zeros.
+// Eight adjacent values from element o on of a matrix of `end` elements (at least
+// 64): where it ends among them, or before, what there is and zeros.
 __device__ __forceinline__ uint4 vocab_load8(const u16* W, size_t o, size_t end) {
   uint4 x;
   if (o + 8 <= end) {
@@ -380,6 +379,17 @@ __device__ __forceinline__ uint4 vocab_load8(const u16* W, size_t o, size_t end)
     unsigned __int128 t;
     __builtin_memcpy(&t, W + (end - 8), 16);
     t = o < end ? t >> (16 * (int)(o - (end - 8))) : 0;
+    __builtin_memcpy(&x, &t, 16);
+  }
+  return x;
+}
+// The same of one row that has `left` values from o on: zeros behind them.
+__device__ __forceinline__ uint4 vocab_row8(const u16* W, size_t o, size_t end, int left) {
+  uint4 x = vocab_load8(W, o, end);
+  if (left < 8) {
+    unsigned __int128 t;
+    __builtin_memcpy(&t, &x, 16);
+    t = left > 0 ? t & (((unsigned __int128)1 << (16 * left)) - 1) : 0;
     __builtin_memcpy(&x, &t, 16);
   }
   return x;

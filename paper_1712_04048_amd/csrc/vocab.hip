@@ -99,26 +99,13 @@ __global__ void __launch_bounds__(256) k_vocab_rows(VocabNet v, int R, const int
   for (size_t o = from + 16 * tid; o < to; o += 256 * 16) st4((float*)((char*)v.hp + o), f4zero());
 }
 
-// W_s with its rows padded to whole 16 bytes (zeros), for a C that is not: 16
-// bytes a thread, read at the alignment of their elements.
-template <class T>
-__global__ void __launch_bounds__(256) k_vocab_pad(int H, int C, int Cq, const T* __restrict__ W, T* out) {
-  constexpr int VEC = 16 / sizeof(T);
-  const int c = (blockIdx.x * 256 + threadIdx.x) * VEC, left = C - c;
-  if (left <= 0) return;
-  for (int row = blockIdx.y; row < H; row += gridDim.y) {
-    const T* src = W + (size_t)row * C + c;
-    uint4 x;
-    if (left >= VEC) {
-      __builtin_memcpy(&x, src, 16);
-    } else {
-      T t[VEC];
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) t[i] = i < left ? src[i] : T(0);
-      __builtin_memcpy(&x, t, 16);
-    }
-    *reinterpret_cast<uint4*>(out + (size_t)row * Cq + c) = x;
-  }
+// bf16 W_s with its rows padded to whole 16 bytes (zeros), for a C that is not:
+// 16 bytes a thread, read at the alignment of an element.
+__global__ void __launch_bounds__(256) k_vocab_pad(int H, int C, int Cq, const u16* __restrict__ W, u16* out) {
+  const int c = (blockIdx.x * 256 + threadIdx.x) * 8;
+  if (c >= C) return;
+  const size_t row = blockIdx.y;
+  *reinterpret_cast<uint4*>(out + row * Cq + c) = vocab_row8(W, row * C + c, (size_t)H * C, C - c);
 }
 
 // The teacher's distribution over its words of a live row, q = softmax(t / T)
@@ -496,11 +483,11 @@ size_t vocab_net(const cavs_vocab* p, bool train, char* base, VocabNet& v) {
   const int big = v.bf ? 256 : 128;
   const long large = (long)((v.n + big - 1) / big) * ((v.C + big - 1) / big);
   v.small = v.few || large < (v.bf ? 128 : 256);
-  const bool pad = v.Cq != v.C && (train || !v.small);
+  const bool pad = v.bf && v.Cq != v.C && (train || !v.small);
   v.pad = pad;
   char* wq = take(pad ? H * (size_t)v.Cq * es : 0);
   v.Ws = pad ? wq : p->Ws;
-  v.ldw = v.Cq;
+  v.ldw = pad ? v.Cq : v.C;
   const size_t stat = slots * rows * 4;
   v.pm = (float*)take(stat);
   v.ps = (float*)take(stat);
@@ -664,15 +651,9 @@ cavs_status vocab_run(cavs_ctx* ctx, const cavs_vocab* p, float* loss, float* ro
   int* err = ctx->dev_err_dev;
   if (v.hbf) v.bf ? rows<u16, u16>(v, p, row_loss, err, s) : rows<u16, float>(v, p, row_loss, err, s);
   else v.bf ? rows<float, u16>(v, p, row_loss, err, s) : rows<float, float>(v, p, row_loss, err, s);
-  if (v.pad) {
-    const dim3 grid(cdiv(v.Cq, 256 * (v.bf ? 8 : 4)), v.H);
-    if (v.bf)
-      CAVS_LAUNCH("k_vocab_pad", k_vocab_pad<u16>, grid, dim3(256), 0, s, v.H, v.C, v.Cq, (const u16*)p->Ws,
-                  (u16*)v.Ws);
-    else
-      CAVS_LAUNCH("k_vocab_pad", k_vocab_pad<float>, grid, dim3(256), 0, s, v.H, v.C, v.Cq,
-                  (const float*)p->Ws, (float*)v.Ws);
-  }
+  if (v.pad)
+    CAVS_LAUNCH("k_vocab_pad", k_vocab_pad, dim3(cdiv(v.C, 256 * 8), v.H), dim3(256), 0, s, v.H, v.C, v.Cq,
+                (const u16*)p->Ws, (u16*)v.Ws);
   if (v.K > 0)
     CAVS_LAUNCH("k_vocab_teacher", k_vocab_teacher, dim3(v.rows / 4), dim3(256), 0, s, v, p->top_word,
                 p->top_logit, err);

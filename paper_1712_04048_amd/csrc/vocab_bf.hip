@@ -443,12 +443,10 @@ void vocab_bf_loss(const VocabNet& v, const void* W, hipStream_t s) {
   if (v.small) {
     const dim3 grid(cdiv(v.C, kFewWords), cdiv(v.n, kVocabFew));
     const VocabEp e = vocab_ep(v, 0);
-    if (v.K > 0)
-      CAVS_LAUNCH("k_vocab_few", k_vocab_few<true>, grid, dim3(256), 0, s, e, (const u16*)W, (const u16*)v.hp,
-                  v.H);
-    else
-      CAVS_LAUNCH("k_vocab_few", k_vocab_few<false>, grid, dim3(256), 0, s, e, (const u16*)W,
-                  (const u16*)v.hp, v.H);
+    auto go = [&](auto* kernel) {
+      CAVS_LAUNCH("k_vocab_few", kernel, grid, dim3(256), 0, s, e, (const u16*)W, (const u16*)v.hp, v.H);
+    };
+    v.K > 0 ? go(k_vocab_few<true>) : go(k_vocab_few<false>);
     return;
   }
   if (v.K > 0) launch<Big>("k_vocab_bf<loss>", s, logits<true, true>(v, 0, v.C));

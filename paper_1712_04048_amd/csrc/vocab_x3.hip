@@ -28,6 +28,51 @@ struct LiveK {
   __device__ void operator()(int&, int&, int& K, int&) const { K = min(K, (*live + 3) & ~3); }
 };
 
+// W_s of a C that is no multiple of 4: its quads are loaded at the alignment of a
+// float, one that reaches past a row's end an element at a time (the next row's
+// values, or none behind the last row, must not meet zeros of the other operand).
+// 3 to 5 % of the products' time; a padded copy took 72 of 330 us of 64 rows, 50
+// 001 words, H = 1024.
+__device__ __forceinline__ float4 load4_upto(const float* p, int there) {
+  float4 x = f4zero();
+  if (there >= 4) {
+    __builtin_memcpy(&x, p, 16);
+  } else {
+    if (there > 0) x.x = p[0];
+    if (there > 1) x.y = p[1];
+    if (there > 2) x.z = p[2];
+  }
+  return x;
+}
+struct X3WRows : X3Rows {
+  __device__ void load(const Net&, const State& s, int k0, int kend, float4 (&v)[8]) const {
+    const int k = k0 + 8 * s.q;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        v[2 * j + h] = load4_upto(s.p[j] ? s.p[j] + k0 + 4 * h : nullptr, s.p[j] ? kend - k - 4 * h : 0);
+  }
+};
+struct X3WCols : X3Cols {
+  struct State : X3Cols::State {
+    int there;
+  };
+  __device__ void init(const Net& n, State& s, int t, int r0) const {
+    X3Cols::init(n, s, t, r0);
+    s.there = cols - (r0 + 4 * s.i);
+  }
+  __device__ void load(const Net&, const State& s, int k0, int kend, float4 (&v)[8]) const {
+    const int k = k0 + 8 * s.q;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      v[e] = load4_upto(s.p ? s.p + (k + e) * s.ld : nullptr, k + e < kend ? s.there : 0);
+  }
+};
+
+template <class L>
+struct X3Whole : L {};   // the same braces for whole quads
+
 // Words are the tile's rows: lane (r, g) holds words 64 wm + 16 g + 4 e + j of
 // rows 64 wn + 4 r + c.
 template <bool LOSS, bool TEACH>
@@ -76,9 +121,9 @@ Net zero_net(const VocabNet& v) {
   return n;
 }
 
-template <bool LOSS>
+template <bool LOSS, class W>
 void logits(const char* name, const VocabNet& v, int col0, int cols, hipStream_t s) {
-  const X3Cols w{(const float*)v.Ws + col0, v.ldw, std::min(cols, v.Cq - col0)};
+  const W w{{(const float*)v.Ws + col0, v.ldw, v.C - col0}};
   const X3Rows h{(const float*)v.hp, v.H, v.rows};
   const VocabEp e = vocab_ep(v, col0);
   const LiveCols lv{v.live};
@@ -86,6 +131,11 @@ void logits(const char* name, const VocabNet& v, int col0, int cols, hipStream_t
     x3_gemm<3, 15, 2>(name, zero_net(v), w, h, X3Vocab<LOSS, true>{e}, cols, v.rows, v.H, v.H, s, lv);
   else
     x3_gemm<3, 15, 2>(name, zero_net(v), w, h, X3Vocab<LOSS, false>{e}, cols, v.rows, v.H, v.H, s, lv);
+}
+template <bool LOSS>
+void logits(const char* name, const VocabNet& v, int col0, int cols, hipStream_t s) {
+  if (v.C % 4 == 0) logits<LOSS, X3Whole<X3Cols>>(name, v, col0, cols, s);
+  else logits<LOSS, X3WCols>(name, v, col0, cols, s);
 }
 
 // The loss of few rows or words: 128 words x 64 rows to a workgroup, four
@@ -211,17 +261,22 @@ void vocab_x3_dz(const VocabNet& v, int col0, int cols, hipStream_t s) {
   logits<false>("k_x3_gemm<vocab dz>", v, col0, cols, s);
 }
 
-void vocab_x3_grads(const VocabNet& v, int col0, int cols, const VocabOut& o, hipStream_t s) {
-  // a quad past C is the padded copy's zeros (X3Rows reads whole quads)
+template <class W>
+static void grads(const VocabNet& v, int col0, int cols, const VocabOut& o, hipStream_t s) {
   const int hchunk = cdiv(cdiv(cols, kBK), v.Sh) * kBK;
   const VocabOut sums{v.hpart, v.H, (size_t)v.rows * v.H, v.rows, v.H, 0, col0 > 0, nullptr};
-  const X3Product dh(X3Rows{(const float*)v.dZ, v.P, v.rows}, X3Rows{(const float*)v.Ws + col0, v.ldw, v.H},
+  const X3Product dh(X3Rows{(const float*)v.dZ, v.P, v.rows}, W{{(const float*)v.Ws + col0, v.ldw, v.H}},
                      X3VocabOut{sums}, LiveRows{v.live, cdiv(cols, hchunk)}, v.rows, v.H, cols, hchunk);
   const int nch = cdiv(v.n, kBK), wchunk = cdiv(nch, v.Sw) * kBK;
   const X3Product dw(X3Cols{(const float*)v.hp, v.H, v.H}, X3Cols{(const float*)v.dZ, v.P, v.P}, X3VocabOut{o},
                      LiveK{v.live}, v.H, cols, nch * kBK, wchunk);
   if (wchunk >= hchunk) x3_two("k_x3_two<vocab dw, dh>", zero_net(v), dw, dh, s);   // longer items first
   else x3_two("k_x3_two<vocab dw, dh>", zero_net(v), dh, dw, s);
+}
+
+void vocab_x3_grads(const VocabNet& v, int col0, int cols, const VocabOut& o, hipStream_t s) {
+  if (v.C % 4 == 0) grads<X3Whole<X3Rows>>(v, col0, cols, o, s);
+  else grads<X3WRows>(v, col0, cols, o, s);
 }
 
 }  // namespace cavs
