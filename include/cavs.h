@@ -71,8 +71,8 @@
  *                                 after n polls (n < 0: at once) and record
  *                                 the error that cavs_sync reports.
  *   - Errors found by kernels after a call has returned (a bounded wait that
- *     gave up, a word out of range) are kept by the context and returned by the next cavs_sync or
- *     cavs_timing_read.
+ *     gave up, a word out of range) are kept by the context and returned by the
+ *     next cavs_sync or cavs_timing_read.
  */
 #ifndef CAVS_H
 #define CAVS_H
@@ -383,13 +383,15 @@ typedef struct {
   int32_t K;                /* teacher's words per row, 0 .. 256; 0: no teacher */
   const int32_t* top_word;  /* [n, K] */
   const float* top_logit;   /* [n, K] */
-  float alpha, temp;        /* weight of KD, in [0, 1]; T > 0 (read with K > 0) */
+  float alpha, temp;        /* weight of KD, in [0, 1]; T in [1/64, 64] (read with K > 0) */
 } cavs_vocab;
 
 /* Bytes of device workspace cavs_vocab_loss (train = 0) or cavs_vocab_grad
-   (train = 1) needs: of n (H + C / 8) order for the loss, and for the gradient
-   pieces of dL/dz of about 256 MB (and, where a piece is all of it, z), whatever
-   C is.  The pointers are not read, but a NULL label is none.  0 on bad args. */
+   (train = 1) needs: a copy of h and some 8 bytes for each row and 64 words for
+   the loss; for the gradient also sums of dh's size in fp32, pieces of dL/dz of
+   about 256 MB and, where one piece is all of it, up to 512 MB of z, whatever C
+   is (bf16 weights of C % 8 != 0: a copy of Ws too).  The pointers are not read,
+   but a NULL label is none.  0 on bad args. */
 size_t cavs_vocab_workspace_bytes(const cavs_vocab* v, int32_t train);
 
 /* loss [1] = L; row_loss [n] (or NULL) the terms of the mean, 0 for rows that

@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(256) k_embed_sum(int n, int n_words, int D, in
   float s[V];
   const int parts = cdiv_dev(n, kPart);
   if (item >= parts) {
-    const int w0 = (item - parts) * each;   // each is at most 8
+    const int w0 = (item - parts) * each;   // each is at most 63: a lane for each start
     const int at = start[min(w0 + min(lane, each), n_words)];
     for (int k = 0; k < each && w0 + k < n_words; ++k) {
       const int from = __builtin_amdgcn_readlane(at, k), to = __builtin_amdgcn_readlane(at, k + 1);
@@ -333,8 +333,11 @@ void embed_grad_launch(cavs_ctx* ctx, const cavs_embedding* e, const int* word, 
                        void* dE, const EmbedWs& w) {
   const int parts = cdiv(n, kPart);
   const int cols = cdiv(e->D, 64 * V);
-  // some 8192 wavefronts, eight words each at most
-  const int each = std::min(8, std::max(1, (int)((size_t)e->n_words * cols / 8192)));
+  // some 8192 wavefronts, eight words each at most; more of the largest tables,
+  // whose launch stays below 2^32 threads (at most 43, as n_words cols is below 2^30
+  // and the parts take 2^25 wavefronts)
+  const size_t blocks = (size_t)e->n_words * cols;
+  const int each = std::max(std::min(8, std::max(1, (int)(blocks / 8192))), (int)(blocks / (3 << 23) + 1));
   CAVS_LAUNCH("k_embed_sum", (k_embed_sum<E, X, V>), dim3(cdiv(((long)parts + cdiv(e->n_words, each)) * cols, 4)),
               dim3(256), 0, ctx->stream, n, e->n_words, e->D, each, e->scale, word, w.start, w.order,
               (const X*)dX, (E*)dE, w.part, w.begins);

@@ -10,6 +10,7 @@
 // gradients' contraction hold zeros.
 #pragma once
 
+#include <algorithm>
 #include <type_traits>
 
 #include "kernels.h"
@@ -37,7 +38,7 @@ struct VocabNet {
   const void* h;
   const void* Ws;          // [H, ldw] of the products' type: the caller's, or its padded copy
   long long ldw;
-  int Cq;                  // readable columns of Ws (a multiple of 16 bytes)
+  int Cq;                  // bf16: readable columns of Ws (a multiple of 16 bytes)
   const float* bs;
   // workspace
   int* rows_list;          // [rows] live row -> caller's row
@@ -346,6 +347,10 @@ __device__ __forceinline__ void vocab_few_end(const VocabEp& e, float (&stats)[3
     float x[NC / 4];
 #pragma unroll
     for (int i = 0; i < NC / 4; ++i) x[i] = z(i, f) + bias[i];
+    if (aw + NC > e.C) {   // what was read past a row's end is the next row's: any value
+#pragma unroll
+      for (int i = 0; i < NC / 4; ++i) x[i] = aw + col(i, g) < e.C ? x[i] : -INFINITY;
+    }
     const int row = row0 + 16 * f + r;
     vocab_rows16<true, TEACH, float, NC>(own, x, col, row, vocab_row<true, TEACH>(e, row, aw / SW, live), aw,
                                          16 * f + r, db);
@@ -427,6 +432,14 @@ __device__ __forceinline__ void vocab_store4(const VocabOut& o, float w, int z, 
 }
 
 VocabEp vocab_ep(const VocabNet& v, int col0);
+
+// f(col0, cols) over the vocabulary, in launches of at most 2^22 tiles: a grid has
+// fewer than 2^32 threads.
+template <class F>
+void vocab_launches(const VocabNet& v, F f) {
+  const int step = (int)std::min<size_t>((size_t)1 << 30, ((size_t)1 << 36) / v.rows / kVocabTile * kVocabTile);
+  for (int col0 = 0; col0 < v.C; col0 += step) f(col0, std::min(step, v.C - col0));
+}
 
 // The piece of dZ that begins with word col0: the two halves in turn.
 inline char* vocab_dz_at(const VocabNet& v, int col0) {

@@ -3,12 +3,13 @@
 // products (vocab_x3.hip, vocab_bf.hip).
 //
 //   loss       z = h W_s + b_s tile by tile; a tile leaves each row's largest z
-//              and sum of exponentials over its words, never z itself
+//              and sum of exponentials over its words, not z itself
 //   gradient   for each piece of P words: z again, dz from the joined
 //              statistics into dZ [rows, P], then dW_s of the piece = h^T dZ and
 //              dL/dh += dZ W_s^T
 // The second pass over z costs two of eight units of work; what it saves is
-// rows x C values of memory (the head inside cavs_forward keeps them).
+// rows x C values of memory (the head inside cavs_forward keeps them).  Where one
+// piece is the whole vocabulary, z is kept in it instead if that is faster.
 #include <math.h>
 
 #include <algorithm>
@@ -18,8 +19,9 @@
 namespace cavs {
 namespace {
 
+constexpr size_t kPieceBytes = (size_t)256 << 20;   // of dZ
+constexpr size_t kKeepBytes = (size_t)96 << 20;     // of z in bf16, see vocab_net
 // Sizes whose tiles and offsets the kernels count in 32 bits.
-constexpr size_t kKeepBytes = (size_t)128 << 20;
 constexpr int kVocabMaxRows = 1 << 20, kVocabMaxWords = 1 << 20, kVocabMaxH = 1 << 15;
 
 // The live rows: their list and numbering, their labels, their rows of h in the
@@ -447,7 +449,6 @@ size_t vocab_net(const cavs_vocab* p, bool train, char* base, VocabNet& v) {
   v.h = p->h;
   v.bs = p->bs;
   const size_t es = v.bf ? 2 : 4, rows = (size_t)v.rows, H = (size_t)v.H, K = (size_t)v.K;
-  const int vec = (int)(16 / es);
   size_t o = 0;
   auto take = [&](size_t bytes) {
     const size_t r = o;
@@ -473,8 +474,6 @@ size_t vocab_net(const cavs_vocab* p, bool train, char* base, VocabNet& v) {
   const size_t slots = (size_t)((v.C + kVocabTile - 1) / kVocabTile) * (kVocabTile / v.slot_words);
   v.trange = (uint32_t*)take(K ? slots * rows * 4 : 0);
   v.hp = take(rows * H * es);
-  v.Cq = (v.C + vec - 1) / vec * vec;
-  // the loss on small tiles reads W_s as it is, the gradients do not
   // Small tiles where the large ones would leave CUs without one (us, large and
   // small; fp32, fewer than 256 tiles of 128 x 128: 172 x 5 176 x 832 76 and 51, 300
   // x 10 000 x 512 58 and 52, 1000 x 5 000 x 512, 320 tiles, 57 and 66; bf16, fewer
@@ -483,6 +482,9 @@ size_t vocab_net(const cavs_vocab* p, bool train, char* base, VocabNet& v) {
   const int big = v.bf ? 256 : 128;
   const long large = (long)((v.n + big - 1) / big) * ((v.C + big - 1) / big);
   v.small = v.few || large < (v.bf ? 128 : 256);
+  // The copies straight to LDS want whole 16 bytes of bf16; the small tiles and
+  // the fp32 loaders take W_s as it is.
+  v.Cq = (v.C + 7) / 8 * 8;
   const bool pad = v.bf && v.Cq != v.C && (train || !v.small);
   v.pad = pad;
   char* wq = take(pad ? H * (size_t)v.Cq * es : 0);
@@ -496,16 +498,18 @@ size_t vocab_net(const cavs_vocab* p, bool train, char* base, VocabNet& v) {
   // Pieces: dZ of about 256 MB, of equal width, at least 2048 words.  The last
   // ones' tiles are then as full as the first ones'.  In bf16 two of them: the
   // next piece's dz is formed while one is multiplied.
-  const size_t words = std::max<size_t>(((size_t)256 << 20) / (rows * es), 2048);
+  const size_t words = std::max<size_t>(kPieceBytes / (rows * es), 2048);
   const size_t pieces = ((size_t)v.C + words - 1) / words;
   v.P = (int)(((v.C + pieces - 1) / pieces + kVocabTile - 1) / kVocabTile * kVocabTile);
   v.dz_half = v.bf && v.P < v.C ? rows * v.P * es : 0;
   v.dZ = take(rows * v.P * es + v.dz_half);
   // z is kept, and not formed twice, where it is one piece: in fp32 always (3 ps a
-  // value there and back, its product 6 at H = 512); in bf16 up to half the
-  // Infinity Cache, and from H = 1024 on, where the product takes longer (4096
-  // rows, 31 000 words: 755 us without and 788 with at H = 512, 1288 and 1214 at
-  // 1024, 2325 and 2058 at 2048).
+  // value there and back, its product 6 at H = 512); in bf16 while the caches hold
+  // it, and from H = 1024 on, where the product takes longer (us with z formed again
+  // and kept; 2048 rows, 8 300 words, 68 MB: 126 and 124 at H = 256, 162 and 147 at
+  // 512; 3000 rows, 9 000 words, 111 MB: 140 and 156, 184 and 190, at 1024 290 and
+  // 270; 4096 rows, 31 000 words: 482 and 552, 718 and 743, 1076 and 1003, at 2048
+  // 1914 and 1670).
   const bool keep = v.P >= v.C && (!v.bf || v.H >= 1024 || rows * v.P * 4 <= kKeepBytes);
   v.Z = keep ? (float*)(v.bf ? take(rows * v.P * 4) : (char*)v.dZ) : nullptr;
   v.keep = keep;
@@ -568,8 +572,9 @@ cavs_status vocab_sizes(cavs_ctx* ctx, const cavs_vocab* p) {
     return fail(ctx, CAVS_ERR_UNSUPPORTED, "K=%d teacher's words (max %d)", p->K, kVocabMaxK);
   if (p->K > 0) {
     if (!(p->alpha >= 0.f && p->alpha <= 1.f)) return fail(ctx, CAVS_ERR_ARG, "alpha outside [0, 1]");
-    if (!(p->temp > 0.f && p->temp < INFINITY && 1.f / p->temp < INFINITY))
-      return fail(ctx, CAVS_ERR_ARG, "temp must be positive, it and its inverse finite");
+    // T^2 multiplies a difference of sums of a few units, each rounded in 32 bits:
+    // past 64 more than some 1e-3 of the loss would be rounding
+    if (!(p->temp >= 1.f / 64 && p->temp <= 64.f)) return fail(ctx, CAVS_ERR_ARG, "temp outside [1/64, 64]");
   }
   if (!p->label && p->n > 0 && !(p->K > 0 && p->alpha == 1.f))
     return fail(ctx, CAVS_ERR_ARG, "labels are required unless the teacher alone is learned from");

@@ -344,9 +344,10 @@ struct BfOut {
 
 // The loss of few rows or words: 128 words x 64 rows to a workgroup (four
 // wavefronts of 32 x 64), two stages of W_s's columns in flight in registers; of
-// few rows it is bound by reading them (4 x 50 000 x 1024: 26 us, 3.9 TB/s).  They come from W_s as it is, whatever C
-// is: a 16-byte load needs no more than the alignment of its elements, where
-// the copies to LDS want four bytes (padding 50 001 columns took 53 of 140 us).
+// few rows it is bound by reading them (4 x 50 000 x 1024: 26 us, 3.9 TB/s).  They
+// come from W_s as it is, whatever C is: a 16-byte load needs no more than the
+// alignment of its elements, where the copies to LDS want four bytes (padding
+// 50 001 columns took 53 of 140 us).
 constexpr int kFewRows = kVocabFew, kFewWords = 128;
 template <bool TEACH>
 __global__ void __launch_bounds__(256, 2) k_vocab_few(VocabEp e, const u16* __restrict__ W,
@@ -449,8 +450,10 @@ void vocab_bf_loss(const VocabNet& v, const void* W, hipStream_t s) {
     v.K > 0 ? go(k_vocab_few<true>) : go(k_vocab_few<false>);
     return;
   }
-  if (v.K > 0) launch<Big>("k_vocab_bf<loss>", s, logits<true, true>(v, 0, v.C));
-  else launch<Big>("k_vocab_bf<loss>", s, logits<true, false>(v, 0, v.C));
+  vocab_launches(v, [&](int col0, int cols) {
+    if (v.K > 0) launch<Big>("k_vocab_bf<loss>", s, logits<true, true>(v, col0, cols));
+    else launch<Big>("k_vocab_bf<loss>", s, logits<true, false>(v, col0, cols));
+  });
 }
 
 void vocab_bf_dz(const VocabNet& v, int col0, int cols, hipStream_t s) {

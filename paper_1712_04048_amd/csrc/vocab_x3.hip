@@ -254,7 +254,7 @@ void vocab_x3_loss(const VocabNet& v, const void* W, hipStream_t s) {
                   (const float*)v.hp, v.H);
     return;
   }
-  logits<true>("k_x3_gemm<vocab loss>", v, 0, v.C, s);
+  vocab_launches(v, [&](int col0, int cols) { logits<true>("k_x3_gemm<vocab loss>", v, col0, cols, s); });
 }
 
 void vocab_x3_dz(const VocabNet& v, int col0, int cols, hipStream_t s) {

@@ -76,3 +76,37 @@ def test_table(ctx):
     assert torch.equal(dE[0], X[0] * 2) and torch.equal(dE[C - 2], X[2] * 2)
     assert torch.equal(dE[C - 1], ((X[1].float() + X[4].float()) * 2).to(BF16))
     assert int((dE != 0).any(1).sum()) == int(seen.sum())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, BF16])
+def test_loss_of_more_tiles_than_a_launch_has_threads(ctx, dtype):
+    n, H, C = 1 << 20, 64, (1 << 18) + 300
+    g = torch.Generator(device="cuda").manual_seed(1)
+    h = torch.randn(n, H, generator=g, device="cuda", dtype=torch.float32).to(dtype)
+    W = (torch.randn(H, C, generator=g, device="cuda", dtype=torch.float32) / 8).to(dtype)
+    y = torch.randint(0, C, (n,), generator=g, device="cuda", dtype=torch.int32)
+    head = B.VocabHead(h=h, Ws=W, label=y)
+    loss, row = (torch.empty(k, dtype=torch.float32, device="cuda") for k in (1, n))
+    ws = torch.empty(B.vocab_workspace_bytes(head, False), dtype=torch.uint8, device="cuda")
+    B.vocab_loss(ctx, head, loss, row, ws)
+    ctx.sync()
+    at = torch.cat([torch.arange(100), torch.arange(n - 100, n)]).cuda()
+    want, bound = R.head(h[at], W, None, y[at])
+    assert R.outside(row[at], want["row_loss"], bound["row_loss"]) <= 1.0
+    mean = float(row.double().mean())
+    assert abs(float(loss) - mean) <= 2 * R.U * abs(mean)
+
+
+def test_table_of_more_blocks_than_a_launch_has_threads(ctx):
+    """Rows of an odd length, so a block of 64 values to a wavefront."""
+    C, D = (1 << 21) + 5, 16383
+    word = torch.tensor([0, C - 1, C - 2, 5, C - 1], dtype=torch.int32, device="cuda")
+    dX = torch.randn(5, D, device="cuda", dtype=torch.float32).to(BF16)
+    dE = torch.full((C, D), 3.0, dtype=BF16, device="cuda")
+    emb = B.Embedding(dE, 1.0)   # its size and type; the table itself is not read
+    ws = torch.empty(B.embed_grad_workspace_bytes(emb, 5), dtype=torch.uint8, device="cuda")
+    B.embed_grad(ctx, emb, word, dX, dE, ws)
+    ctx.sync()
+    assert torch.equal(dE[0], dX[0]) and torch.equal(dE[5], dX[3]) and torch.equal(dE[C - 2], dX[2])
+    assert torch.equal(dE[C - 1], (dX[1].float() + dX[4].float()).to(BF16))
+    assert sum(int((part != 0).any(1).sum()) for part in dE.split(1 << 16)) == 4

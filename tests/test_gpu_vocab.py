@@ -199,6 +199,34 @@ def test_masked_words(ctx, types):
 
 
 @pytest.mark.parametrize("types", [(F32, F32), (BF16, BF16)])
+@pytest.mark.parametrize("n", [5, 200])
+def test_a_word_masked_by_its_weights(ctx, types, n):
+    """-inf times a positive state: the word is out of every row's softmax, and
+    what the next row of W_s holds behind the last word stays out too."""
+    head = make(12, n, 70, 64, types)
+    head.h[:, 1] = head.h[:, 1].abs() + 0.1
+    head.h[:, 0] = -head.h[:, 0].abs() - 0.1
+    head.label[head.label == 0] = 1
+    masked = B.VocabHead(h=head.h, Ws=head.Ws.clone(), bs=head.bs.clone(), label=head.label)
+    masked.bs[0] = -math.inf
+    want, bound = reference(masked)
+    head.Ws[1, 0] = -math.inf
+    got = loss(ctx, head)
+    ctx.sync()
+    check(got, want, bound)
+
+
+@pytest.mark.parametrize("types", [(F32, F32), (BF16, BF16)])
+@pytest.mark.parametrize("n,temp", [(40, 1 / 64), (300, 0.25), (40, 64.0), (300, 16.0)])
+def test_temperatures(ctx, types, n, temp):
+    head = make(13, n, 700, 128, types, K=9, alpha=0.5, temp=temp)
+    want, bound = reference(head)
+    got = grad(ctx, head)
+    ctx.sync()
+    check(got, want, bound)
+
+
+@pytest.mark.parametrize("types", [(F32, F32), (BF16, BF16)])
 def test_nan_stays_in_its_row(ctx, types):
     # In fp32 the NaN's tile is formed again on the fp32 instruction: its other
     # rows' sums round in another order, each within the bounds of its terms.

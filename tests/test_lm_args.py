@@ -89,6 +89,13 @@ def test_refused_heads_have_no_workspace(kw):
     assert B.vocab_workspace_bytes(_head(**kw), False) == 0
 
 
+@pytest.mark.parametrize("temp,ok", [(1 / 64, True), (64.0, True), (0.015, False), (64.1, False), (-1.0, False),
+                                     (float("nan"), False)])
+def test_temperatures(temp, ok):
+    _ensure_built()
+    assert (B.vocab_workspace_bytes(_head(**dict(TEACHER, temp=temp)), True) > 0) == ok
+
+
 def test_head_workspace_does_not_hold_the_logits():
     _ensure_built()
 
