@@ -235,22 +235,44 @@ __global__ void __launch_bounds__(1024) k_vocab_join(VocabNet v, float* row_loss
     if (loss && threadIdx.x == 0) *loss = 0.f;
     return;
   }
-  float m = -INFINITY;
-#pragma unroll 4
-  for (int k = k0; k < v.slots; k += 64) m = fmaxf(m, v.pm[(size_t)k * v.rows + row]);
+  // a thread's slots, eight at a time and all asked for before the first is used,
+  // relative to the largest z so far
+  constexpr int U = 8;
+  float m = -INFINITY, s = 0.f, t = 0.f, dot = 0.f;
+  auto at0 = [](float x) { return x == -INFINITY ? 0.f : x; };
+  const float invT = 1.f / v.temp;
+  for (int kk = k0; kk < v.slots; kk += 64 * U) {
+    float pm[U], ps[U], pt[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const size_t at = (size_t)(kk + 64 * u) * v.rows + row;
+      const bool there = kk + 64 * u < v.slots;
+      pm[u] = there ? v.pm[at] : -INFINITY;
+      ps[u] = there ? v.ps[at] : 0.f;
+      pt[u] = there && v.two ? v.pt[at] : 0.f;
+    }
+    float mu = m;
+#pragma unroll
+    for (int u = 0; u < U; ++u) mu = fmaxf(mu, pm[u]);
+    const float m0 = at0(mu), d0 = (m - m0) * kLog2e;
+    s *= __builtin_amdgcn_exp2f(d0);
+    t *= __builtin_amdgcn_exp2f(d0 * invT);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float d = (pm[u] - m0) * kLog2e;
+      s += ps[u] * __builtin_amdgcn_exp2f(d);
+      if (v.two) t += pt[u] * __builtin_amdgcn_exp2f(d * invT);
+    }
+    m = mu;
+  }
   sm[k0][i] = m;
   __syncthreads();
+  const float own = m;
 #pragma unroll
   for (int k = 0; k < 64; ++k) m = fmaxf(m, sm[k][i]);
-  const float mm = m == -INFINITY ? 0.f : m;
-  float s = 0.f, t = 0.f, dot = 0.f;
-#pragma unroll 4
-  for (int k = k0; k < v.slots; k += 64) {
-    const size_t at = (size_t)k * v.rows + row;
-    const float d = (v.pm[at] - mm) * kLog2e;
-    s += v.ps[at] * __builtin_amdgcn_exp2f(d);
-    if (v.two) t += v.pt[at] * __builtin_amdgcn_exp2f(d / v.temp);
-  }
+  const float d0 = (own - at0(m)) * kLog2e;
+  s *= __builtin_amdgcn_exp2f(d0);
+  t *= __builtin_amdgcn_exp2f(d0 * invT);
   if (row < nl)
     for (int j = k0; j < v.K; j += 64) {
       const size_t at = (size_t)row * v.K + j;
