@@ -326,10 +326,10 @@ __device__ __forceinline__ void vocab_bias(const VocabEp& e, int a0, int g, Col 
   }
 }
 
-// A workgroup of the loss's small tiles: four wavefronts of 32 words each by 64
+// A workgroup of the loss's small tiles: four wavefronts of 32 words each by 16 FB
 // rows from row0 on, z(i, f) lane (g, r)'s word col(i, g) of row row0 + 16 f + r.
 // The wavefronts' statistics are joined into the slots of SW words.
-template <bool TEACH, int SW, class Z>
+template <bool TEACH, int SW, int FB, class Z>
 __device__ __forceinline__ void vocab_few_end(const VocabEp& e, float (&stats)[3][4][kVocabFew], int a0,
                                               int row0, Z z) {
   constexpr int NC = 32, PER = SW / NC;   // wavefronts of a slot
@@ -343,7 +343,7 @@ __device__ __forceinline__ void vocab_few_end(const VocabEp& e, float (&stats)[3
   vocab_bias(e, aw, g, col, bias);
   const int live = *e.live;
 #pragma unroll
-  for (int f = 0; f < kVocabFew / 16; ++f) {
+  for (int f = 0; f < FB; ++f) {
     float x[NC / 4];
 #pragma unroll
     for (int i = 0; i < NC / 4; ++i) x[i] = z(i, f) + bias[i];
@@ -357,7 +357,7 @@ __device__ __forceinline__ void vocab_few_end(const VocabEp& e, float (&stats)[3
   }
   __syncthreads();
   const int row = tid & 63;
-  if (w >= 4 / PER) return;
+  if (w >= 4 / PER || row >= 16 * FB) return;
   float m = -INFINITY, s = 0.f, t = 0.f;
 #pragma unroll
   for (int k = 0; k < PER; ++k) m = fmaxf(m, stats[0][PER * w + k][row]);

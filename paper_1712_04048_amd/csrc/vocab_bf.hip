@@ -344,15 +344,19 @@ struct BfOut {
 
 // The loss of few rows or words: 128 words x 64 rows to a workgroup (four
 // wavefronts of 32 x 64), two stages of W_s's columns in flight in registers; of
-// few rows it is bound by reading them (4 x 50 000 x 1024: 26 us, 3.9 TB/s).  They
+// few rows it is bound by reading them (4 x 50 000 x 1024: 24 us, 4.3 TB/s; 4 x 128
+// 000 x 2048: 97 us, 5.4 TB/s).  They
 // come from W_s as it is, whatever C is: a 16-byte load needs no more than the
 // alignment of its elements, where the copies to LDS want four bytes (padding
 // 50 001 columns took 53 of 140 us).
+// FB: groups of 16 rows.  Of at most 16 rows one alone: the products and reads of
+// h of the other three took 27 us instead of 24 of 4 x 50 000 x 1024, 111 instead of
+// 97 of the larger.
 constexpr int kFewRows = kVocabFew, kFewWords = 128;
-template <bool TEACH>
+template <bool TEACH, int FB>
 __global__ void __launch_bounds__(256, 2) k_vocab_few(VocabEp e, const u16* __restrict__ W,
                                                       const u16* __restrict__ hp, int H) {
-  constexpr int FA = 2, FB = 4, kA = kFewWords * 128, kB = kFewRows * 128;
+  constexpr int FA = 2, kA = kFewWords * 128, kB = 16 * FB * 128;
   __shared__ __attribute__((aligned(16))) char lds[2][kA + kB];
   __shared__ float stats[3][4][kFewRows];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g = lane >> 4, r = lane & 15;
@@ -375,7 +379,8 @@ __global__ void __launch_bounds__(256, 2) k_vocab_few(VocabEp e, const u16* __re
 #pragma unroll
     for (int i = 0; i < 4; ++i) x.a[i] = vocab_load8(W, (size_t)(k0 + ka[i]) * C + ca[i], end);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) x.b[i] = *reinterpret_cast<const uint4*>(hb + k0 + kCK * i);
+    for (int i = 0; i < 2; ++i)
+      if (FB == 4 || tid < 64 * FB) x.b[i] = *reinterpret_cast<const uint4*>(hb + k0 + kCK * i);
   };
   ColsOp::Frag<kFewWords> fa;
   RowsOp::Frag<kFewRows> fb;
@@ -393,7 +398,8 @@ __global__ void __launch_bounds__(256, 2) k_vocab_few(VocabEp e, const u16* __re
 #pragma unroll
       for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(L + 16 * (i * 256 + tid)) = st[s].a[i];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) *reinterpret_cast<uint4*>(L + kA + 16 * (i * 256 + tid)) = st[s].b[i];
+      for (int i = 0; i < 2; ++i)
+        if (FB == 4 || tid < 64 * FB) *reinterpret_cast<uint4*>(L + kA + i * (kB / 2) + 16 * tid) = st[s].b[i];
       __syncthreads();   // the other buffer's readers are past this one's barrier
       load(st[s], min(k0 + (s + 2) * kKB, H - kKB));   // past the end: the last stage, unused
       __builtin_amdgcn_sched_barrier(0);   // the loads go out before these products
@@ -411,7 +417,7 @@ __global__ void __launch_bounds__(256, 2) k_vocab_few(VocabEp e, const u16* __re
       }
     }
   }
-  vocab_few_end<TEACH, kFewWords>(e, stats, a0, row0, [&](int i, int f) { return acc[i >> 2][f][i & 3]; });
+  vocab_few_end<TEACH, kFewWords, FB>(e, stats, a0, row0, [&](int i, int f) { return acc[i >> 2][f][i & 3]; });
 }
 
 using Big = Shape<2, 4, 8, 4>;    // 256 x 256, eight wavefronts, 128 KB
@@ -447,7 +453,8 @@ void vocab_bf_loss(const VocabNet& v, const void* W, hipStream_t s) {
     auto go = [&](auto* kernel) {
       CAVS_LAUNCH("k_vocab_few", kernel, grid, dim3(256), 0, s, e, (const u16*)W, (const u16*)v.hp, v.H);
     };
-    v.K > 0 ? go(k_vocab_few<true>) : go(k_vocab_few<false>);
+    if (v.n <= 16) v.K > 0 ? go(k_vocab_few<true, 1>) : go(k_vocab_few<false, 1>);
+    else v.K > 0 ? go(k_vocab_few<true, 4>) : go(k_vocab_few<false, 4>);
     return;
   }
   vocab_launches(v, [&](int col0, int cols) {

@@ -141,13 +141,14 @@ void logits(const char* name, const VocabNet& v, int col0, int cols, hipStream_t
 // The loss of few rows or words: 128 words x 64 rows to a workgroup, four
 // wavefronts of 32 x 64, two stages of 32 k in flight in registers, split on
 // their way to LDS (split3.h's parts, a plane of 64-byte rows each).  W_s is read
-// as it is, at the alignment of its elements.  The 128 x 128 tiles, one chunk in
+// as it is, at the alignment of its elements.  FB: groups of 16 rows; of at most 16
+// one alone (4 x 50 001 x 1024: 51 us, 67 with all four).  The 128 x 128 tiles, one chunk in
 // flight and twice the work, took 83 us for 9 rows, 8 043 words, H = 1152.
 constexpr int kFewWords = 128;
-template <bool TEACH>
+template <bool TEACH, int FB>
 __global__ void __launch_bounds__(256, 2) k_vocab_few_x3(VocabEp e, const float* __restrict__ W,
                                                          const float* __restrict__ hp, int H) {
-  constexpr int FA = 2, FB = 4, kA = kFewWords * 64, kB = kVocabFew * 64, kPlanes = 3 * (kA + kB);
+  constexpr int FA = 2, kA = kFewWords * 64, kB = 16 * FB * 64, kPlanes = 3 * (kA + kB);
   __shared__ __attribute__((aligned(16))) char lds[2][kPlanes];
   __shared__ float stats[3][4][kVocabFew];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g = lane >> 4, r = lane & 15;
@@ -167,8 +168,10 @@ __global__ void __launch_bounds__(256, 2) k_vocab_few_x3(VocabEp e, const float*
       if (o + 2 <= end) __builtin_memcpy(&x.a[k], W + o, 8);
       else x.a[k] = make_float2(o < end ? W[o] : 0.f, 0.f);
     }
-    x.b[0] = ldg4(hb + k0);
-    x.b[1] = ldg4(hb + k0 + 4);
+    if (FB == 4 || tid < 64 * FB) {
+      x.b[0] = ldg4(hb + k0);
+      x.b[1] = ldg4(hb + k0 + 4);
+    }
   };
   auto put = [&](char* base, int plane, int row, int octet, const float (&v)[8]) {
     const Split8 p = split8(v);
@@ -190,9 +193,11 @@ __global__ void __launch_bounds__(256, 2) k_vocab_few_x3(VocabEp e, const float*
         for (int k = 0; k < 8; ++k) v[k] = c ? st[s].a[k].y : st[s].a[k].x;
         put(L, kA, 2 * lane + c, w, v);
       }
-      const float4 b0 = st[s].b[0], b1 = st[s].b[1];
-      const float v[8] = {b0.x, b0.y, b0.z, b0.w, b1.x, b1.y, b1.z, b1.w};
-      put(L + 3 * kA, kB, tid >> 2, tid & 3, v);
+      if (FB == 4 || tid < 64 * FB) {
+        const float4 b0 = st[s].b[0], b1 = st[s].b[1];
+        const float v[8] = {b0.x, b0.y, b0.z, b0.w, b1.x, b1.y, b1.z, b1.w};
+        put(L + 3 * kA, kB, tid >> 2, tid & 3, v);
+      }
       __syncthreads();   // the other buffer's readers are past this one's barrier
       load(st[s], min(k0 + (s + 2) * kBK, H - kBK));   // past the end: the last stage, unused
       __builtin_amdgcn_sched_barrier(0);   // the loads go out before these products
@@ -237,7 +242,7 @@ __global__ void __launch_bounds__(256, 2) k_vocab_few_x3(VocabEp e, const float*
           acc[i][f][q] = s;
         }
   }
-  vocab_few_end<TEACH, 64>(e, stats, a0, row0, [&](int i, int f) { return acc[i >> 2][f][i & 3]; });
+  vocab_few_end<TEACH, 64, FB>(e, stats, a0, row0, [&](int i, int f) { return acc[i >> 2][f][i & 3]; });
 }
 
 }  // namespace
@@ -246,12 +251,11 @@ void vocab_x3_loss(const VocabNet& v, const void* W, hipStream_t s) {
   if (v.small) {
     const dim3 grid(cdiv(v.C, kFewWords), cdiv(v.n, kVocabFew));
     const VocabEp e = vocab_ep(v, 0);
-    if (v.K > 0)
-      CAVS_LAUNCH("k_vocab_few_x3", k_vocab_few_x3<true>, grid, dim3(256), 0, s, e, (const float*)W,
-                  (const float*)v.hp, v.H);
-    else
-      CAVS_LAUNCH("k_vocab_few_x3", k_vocab_few_x3<false>, grid, dim3(256), 0, s, e, (const float*)W,
-                  (const float*)v.hp, v.H);
+    auto go = [&](auto* kernel) {
+      CAVS_LAUNCH("k_vocab_few_x3", kernel, grid, dim3(256), 0, s, e, (const float*)W, (const float*)v.hp, v.H);
+    };
+    if (v.n <= 16) v.K > 0 ? go(k_vocab_few_x3<true, 1>) : go(k_vocab_few_x3<false, 1>);
+    else v.K > 0 ? go(k_vocab_few_x3<true, 4>) : go(k_vocab_few_x3<false, 4>);
     return;
   }
   vocab_launches(v, [&](int col0, int cols) { logits<true>("k_x3_gemm<vocab loss>", v, col0, cols, s); });

@@ -250,6 +250,21 @@ def test_nan_stays_in_its_row(ctx, types):
     assert not any(torch.isnan(v).any() for v in got.values())
 
 
+@pytest.mark.parametrize("types", [(F32, F32), (BF16, BF16), (F32, BF16)])
+@pytest.mark.parametrize("n", [2, 15, 16, 17])
+@pytest.mark.parametrize("C,H,K", [(1000, 64, 0), (9001, 192, 5), (130, 320, 40)])
+def test_rows_of_one_group(ctx, types, n, C, H, K):
+    """The kernels for at most 16 rows, and the first row past them."""
+    head = make(n + C, n, C, H, types, pad=0.3, K=K, alpha=0.5 if K else 0.0, temp=2.0 if K else 1.0)
+    want, bound = reference(head)
+    got = grad(ctx, head)
+    ctx.sync()
+    check(got, want, bound)
+    got = loss(ctx, head)
+    ctx.sync()
+    check(got, want, bound)
+
+
 def test_large_logits(ctx):
     """Scores of thousands: only the largest words of a row count."""
     head = make(6, 100, 700, 64)
