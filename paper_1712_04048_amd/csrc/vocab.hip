@@ -332,6 +332,35 @@ __global__ void __launch_bounds__(256) k_vocab_dz(VocabNet v, float* db_out) {
   const int c0 = blockIdx.x * 256, c = c0 + 4 * lane, r0 = blockIdx.y * 64;
   if (!db_out && r0 >= cdiv_dev(nl, kVocabTile) * kVocabTile) return;
   const float invT = 1.f / v.temp;
+  // The teacher's words here of the wavefront's 16 rows: their ranges in one load, a
+  // lane a word in another (one row after the other they are two dependent loads
+  // each).  More than 64 are looked up row by row.
+  int first = 0, there = 0, lo = 0, total = 0, tw = -1;
+  float tq = 0.f;
+  if (v.K > 0) {
+    const int s0 = c0 / v.slot_words, s1 = s0 + 256 / v.slot_words - 1, row = r0 + 16 * w + (lane & 15);
+    if (row < nl) {
+      lo = v.trange[(size_t)s0 * v.rows + row] & 0xffffu;
+      there = (int)(v.trange[(size_t)s1 * v.rows + row] >> 16) - lo;
+    }
+    int past = there;   // the sum up to a lane's row
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) {
+      const int y = __shfl_up(past, o, 16);
+      if ((lane & 15) >= o) past += y;
+    }
+    first = past - there;
+    total = __builtin_amdgcn_readlane(past, 15);
+    int k = 0;   // the row of word `lane` of them
+#pragma unroll
+    for (int i = 0; i < 15; ++i) k += __builtin_amdgcn_readlane(past, i) <= lane;
+    const int j = __shfl(lo, k, kWave) + lane - __shfl(first, k, kWave);
+    if (lane < total) {
+      const size_t t = (size_t)(r0 + 16 * w + k) * v.K + j;
+      tw = v.tword[t];
+      tq = v.distw * v.tq[t];
+    }
+  }
   float4 db = f4zero();
 #pragma unroll 4
   for (int rr = 0; rr < 16; ++rr) {
@@ -348,17 +377,20 @@ __global__ void __launch_bounds__(256) k_vocab_dz(VocabNet v, float* db_out) {
         if (v.two) d[i] += k.z * __builtin_amdgcn_exp2f(x[i] * (invT * kLog2e));
         if (c + i == lab) d[i] -= k.w;
       }
-      if (v.K > 0) {
-        const int s0 = c0 / v.slot_words, s1 = s0 + 256 / v.slot_words - 1;
-        const int lo = v.trange[(size_t)s0 * v.rows + row] & 0xffffu;
-        const int hi = v.trange[(size_t)s1 * v.rows + row] >> 16;
-        for (int j = lo; j < hi; ++j) {
-          const size_t t = (size_t)row * v.K + j;
-          const int word = v.tword[t];
-          const float q = v.distw * v.tq[t];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) d[i] -= c + i == word ? q : 0.f;
+      const int n = __builtin_amdgcn_readlane(there, rr), at0 = __builtin_amdgcn_readlane(first, rr);
+      const size_t t0 = (size_t)row * v.K + __builtin_amdgcn_readlane(lo, rr);
+      for (int j = 0; j < n; ++j) {
+        int word;
+        float q;
+        if (total <= 64) {
+          word = __builtin_amdgcn_readlane(tw, at0 + j);
+          q = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(tq), at0 + j));
+        } else {
+          word = v.tword[t0 + j];
+          q = v.distw * v.tq[t0 + j];
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) d[i] -= c + i == word ? q : 0.f;
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) d[i] = c + i < v.C ? d[i] : 0.f;
