@@ -119,8 +119,8 @@ __global__ void __launch_bounds__(256) k_vocab_pad(int H, int C, int Cq, const u
 __global__ void __launch_bounds__(256) k_vocab_teacher(VocabNet v, const int* __restrict__ top_word,
                                                        const float* __restrict__ top_logit, int* err) {
   constexpr int PER = kVocabMaxK / 64, kNone = 0x7fffffff;
-  __shared__ int words[4][kVocabMaxK], sorted[4][kVocabMaxK];
-  __shared__ float qs[4][kVocabMaxK];
+  __shared__ __attribute__((aligned(16))) int words[4][kVocabMaxK], sorted[4][kVocabMaxK];
+  __shared__ __attribute__((aligned(16))) float qs[4][kVocabMaxK];
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, row = blockIdx.x * 4 + w, K = v.K;
   if (row >= *v.live) return;
   const size_t src = (size_t)v.rows_list[row] * K, dst = (size_t)row * K;
@@ -160,26 +160,41 @@ __global__ void __launch_bounds__(256) k_vocab_teacher(VocabNet v, const int* __
   s = wave_sum(s);
   if (lane == 0) v.tsum[row] = make_float2(s, some ? 1.f : 0.f);
   wave_lds_fence();
-  const int reach = (K + 63) / 64;
+  // four entries at a time against all of a lane's (one by one, an entry of theirs
+  // after the other, 600 rows of 200 words took 70 us); entries past K are kNone
+  auto rank = [&](auto reach) {
+    constexpr int R = decltype(reach)::value;
+    int place[R] = {};
+    bool first[R];
+    float total[R] = {};
 #pragma unroll
-  for (int k = 0; k < PER; ++k) {
-    if (k >= reach) break;
-    const int j = lane + 64 * k;
-    if (j >= K) continue;
-    int place = 0;
-    bool first = true;
-    float total = 0.f;
-    for (int i = 0; i < K; ++i) {
-      const int x = words[w][i];
-      const bool same = x == id[k], before = same && i < j;
-      place += x < id[k] || before;
-      first = first && !before;
-      total += same ? qs[w][i] : 0.f;
+    for (int k = 0; k < R; ++k) first[k] = true;
+    for (int i0 = 0; i0 < K; i0 += 4) {
+      const int4 x4 = *reinterpret_cast<const int4*>(words[w] + i0);
+      const float4 q4 = *reinterpret_cast<const float4*>(qs[w] + i0);
+      const int x[4] = {x4.x, x4.y, x4.z, x4.w};
+      const float y[4] = {q4.x, q4.y, q4.z, q4.w};
+#pragma unroll
+      for (int k = 0; k < R; ++k)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const bool same = x[u] == id[k], before = same && i0 + u < lane + 64 * k;
+          place[k] += x[u] < id[k] || before;
+          first[k] = first[k] && !before;
+          total[k] += same ? y[u] : 0.f;
+        }
     }
-    sorted[w][place] = id[k];
-    v.tword[dst + place] = id[k];
-    v.tq[dst + place] = first && id[k] != kNone ? total : 0.f;
-  }
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      if (lane + 64 * k >= K) continue;
+      sorted[w][place[k]] = id[k];
+      v.tword[dst + place[k]] = id[k];
+      v.tq[dst + place[k]] = first[k] && id[k] != kNone ? total[k] : 0.f;
+    }
+  };
+  if (K <= 64) rank(std::integral_constant<int, 1>{});
+  else if (K <= 128) rank(std::integral_constant<int, 2>{});
+  else rank(std::integral_constant<int, PER>{});
   wave_lds_fence();
   auto below = [&](long long word) {   // the row's words below this one
     int lo = 0, hi = K;
@@ -190,11 +205,11 @@ __global__ void __launch_bounds__(256) k_vocab_teacher(VocabNet v, const int* __
     }
     return lo;
   };
-  // the last tile's slots past C as well
+  // the last tile's slots past C as well; a slot ends where the next one begins
   const int slots = cdiv_dev(v.C, kVocabTile) * (kVocabTile / v.slot_words);
-  for (int k = lane; k < slots; k += 64) {
-    const long long a = (long long)k * v.slot_words;
-    v.trange[(size_t)k * v.rows + row] = below(a) | (uint32_t)below(a + v.slot_words) << 16;
+  for (int k0 = 0; k0 < slots; k0 += 63) {
+    const int k = k0 + lane, from = below((long long)k * v.slot_words), to = __shfl_down(from, 1, kWave);
+    if (lane < 63 && k < slots) v.trange[(size_t)k * v.rows + row] = from | (uint32_t)to << 16;
   }
 }
 
