@@ -578,8 +578,9 @@ size_t vocab_net(const cavs_vocab* p, bool train, char* base, VocabNet& v) {
   // and kept; 2048 rows, 8 300 words, 68 MB: 126 and 124 at H = 256, 162 and 147 at
   // 512; 3000 rows, 9 000 words, 111 MB: 140 and 156, 184 and 190, at 1024 290 and
   // 270; 4096 rows, 31 000 words: 482 and 552, 718 and 743, 1076 and 1003, at 2048
-  // 1914 and 1670).
-  const bool keep = v.P >= v.C && (!v.bf || v.H >= 1024 || rows * v.P * 4 <= kKeepBytes);
+  // 1914 and 1670).  Few rows always keep it: the tiles that form it again are of
+  // 256 rows, their buffers are not.
+  const bool keep = v.P >= v.C && (!v.bf || v.few || v.H >= 1024 || rows * v.P * 4 <= kKeepBytes);
   v.Z = keep ? (float*)(v.bf ? take(rows * v.P * 4) : (char*)v.dZ) : nullptr;
   v.keep = keep;
   v.db_rows = 64;

@@ -265,6 +265,19 @@ def test_rows_of_one_group(ctx, types, n, C, H, K):
     check(got, want, bound)
 
 
+@pytest.mark.parametrize("types", [(F32, F32), (BF16, BF16)])
+@pytest.mark.parametrize("n,C,H", [(3, 600001, 64), (64, 450000, 64), (1, (1 << 20), 128), (65, 420000, 64)])
+def test_few_rows_of_many_words_stay_in_their_workspace(ctx, types, n, C, H):
+    head = make(31, n, C, H, types, bias=False)
+    need = B.vocab_workspace_bytes(head, True)
+    ws = torch.full((need + (1 << 28),), 255, dtype=torch.uint8, device="cuda")
+    got = grad(ctx, head, ws=ws[:need])
+    ctx.sync()
+    assert bool((ws[need:] == 255).all())
+    want, bound = reference(head)
+    check(got, want, bound)
+
+
 def test_large_logits(ctx):
     """Scores of thousands: only the largest words of a row count."""
     head = make(6, 100, 700, 64)
