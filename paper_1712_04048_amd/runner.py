@@ -167,14 +167,16 @@ class LmBatch(Batch):
         self.grads["dbs"] = torch.empty_like(self.bs)
         self.grads["dE"] = torch.empty_like(self.emb.E)
         self.row_loss = torch.empty(wl.V, dtype=torch.float32, device=dev)
+        # CAVS_LOSS_NONE's 0; kept, as the context's stream may write it after the call
+        self.no_loss = torch.empty_like(self.loss)
         u8 = dict(dtype=torch.uint8, device=dev)
         self.ws_head = torch.empty(max(1, B.vocab_workspace_bytes(self.head, True)), **u8)
         self.ws_emb = torch.empty(max(1, B.embed_grad_workspace_bytes(self.emb, wl.n_x)), **u8)
 
     def forward(self):
         B.embed(self.ctx, self.emb, self.words, self.X)
-        none = torch.empty(1, dtype=torch.float32, device=self.dev)   # CAVS_LOSS_NONE's 0
-        B.forward(self.ctx, self.params, self.sched, self.X, None, self.ws, self.h, self.c, none)
+        B.forward(self.ctx, self.params, self.sched, self.X, None, self.ws, self.h, self.c,
+                  self.no_loss)
         g = self.grads
         B.vocab_grad(self.ctx, self.head, self.loss, self.row_loss, self.dH_ext, g["dWs"], g["dbs"],
                      self.ws_head)
@@ -189,6 +191,6 @@ class LmBatch(Batch):
         if self.ws_infer is None:
             n = B.infer_workspace_bytes(self.params, self.sched)
             self.ws_infer = torch.empty(max(n, 1), dtype=torch.uint8, device=self.dev)
-        none = torch.empty(1, dtype=torch.float32, device=self.dev)
-        B.infer(self.ctx, self.params, self.sched, self.X, None, self.ws_infer, self.h, self.c, none)
+        B.infer(self.ctx, self.params, self.sched, self.X, None, self.ws_infer, self.h, self.c,
+                self.no_loss)
         B.vocab_loss(self.ctx, self.head, self.loss, self.row_loss, self.ws_head)
