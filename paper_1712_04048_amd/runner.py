@@ -146,7 +146,10 @@ class LmBatch(Batch):
         self.emb = B.Embedding(table, scale)
         self.words = torch.as_tensor(np.ascontiguousarray(words, dtype=np.int32)).to(dev)
         self.X = torch.empty(wl.n_x, wl.D, dtype=torch.float32, device=dev)
-        self.Ws, self.bs = p.Ws.to(head_dtype), p.bs
+        # rounded on the host: a kernel on torch's stream is one that ctx's does not wait for
+        self.Ws = (p.Ws if head_dtype == torch.float32 else
+                   torch.from_numpy(np.ascontiguousarray(wl.Ws, dtype=np.float32)).to(head_dtype).to(dev))
+        self.bs = p.bs
         self.params = B.Params(p.cell, p.prec, B.LOSS_NONE, p.D, p.H, p.N, 0, p.Wx, p.U, p.b,
                                None, None)
         self.teacher = teacher

@@ -3,6 +3,7 @@ are replaced by ones that record their arguments)."""
 import numpy as np
 import pytest
 import torch
+from torch.utils._python_dispatch import TorchDispatchMode
 
 from paper_1712_04048_amd import binding as B
 from paper_1712_04048_amd import workloads as W
@@ -61,3 +62,29 @@ def test_outputs_of_its_calls_stay_its_own(calls):
         for a in args:
             if isinstance(a, torch.Tensor):
                 assert any(a is t for t in held), name
+
+
+class _DeviceWork(TorchDispatchMode):
+    """The operations that read a tensor of the batch's device."""
+
+    def __init__(self, device):
+        super().__init__()
+        self.device, self.seen = torch.device(device), []
+
+    def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+        if any(isinstance(a, torch.Tensor) and a.device == self.device for a in args):
+            self.seen.append(str(func))
+        return func(*args, **(kwargs or {}))
+
+
+@pytest.mark.parametrize("head_dtype", [torch.float32, torch.bfloat16])
+def test_it_is_made_without_work_on_torch_s_stream(calls, head_dtype):
+    """Copies from the host are complete when they return; a kernel on torch's
+    current stream is not, and the context's stream does not wait for it."""
+    word = np.zeros((15, 2), dtype=np.int32)
+    with _DeviceWork("meta") as work:
+        b = _batch("meta", head_dtype=head_dtype,
+                   teacher=(word, word.astype(np.float32), 0.5, 2.0))
+        b.alloc()
+    assert b.Ws.dtype == head_dtype and b.Ws.shape == (64, 9)
+    assert not [f for f in work.seen if not f.startswith("aten.empty_like")]
