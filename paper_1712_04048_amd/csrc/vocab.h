@@ -60,7 +60,8 @@ struct VocabNet {
   float* zlab;             // [rows] z of the label
   float* ztop;             // [rows, K] z of tword
   float4* rowc;            // [rows] largest z, weight of exp(z - largest), weight of
-                           //   exp((z - largest) / temp), weight of the label
+                           //   exp((z - largest) / temp), weight of the label; inf and
+                           //   zeros for a row without dz
   float* val;              // [rows] the row's loss
   float* zrow;             // a row of zeros (16 bytes and more)
   // gradient, one piece of words at a time
@@ -266,6 +267,15 @@ __device__ __forceinline__ void vocab_rows16(const VocabEp& e, float (&z)[NC / 4
       });
   } else {
     const float4 c = info.c;
+    // A row in which no exponential counts (behind the last live one, or with the
+    // teacher alone and none of its words; c.x is inf) has no dz, whatever its z is:
+    // the score of a word that W_s masks with -inf is a NaN where the state is 0, as
+    // behind the last row, and would stay one times a weight of 0.
+    const bool none = c.y == 0.f && c.z == 0.f;
+    if (__any(none)) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) z[i] = none ? 0.f : z[i];
+    }
     if (TEACH && e.two) {
       const float k = e.invT * kLog2e;
 #pragma unroll

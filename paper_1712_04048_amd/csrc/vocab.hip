@@ -230,6 +230,7 @@ __device__ float vocab_row_end(const VocabNet& v, int row, float m, float s, flo
   // in units of v.unit
   const float lab = a < 1.f ? 1.f : 0.f, c1 = lab != 0.f ? 1.f / s : 0.f;
   const float cT = has != 0.f ? v.distw / t : 0.f;
+  if (c1 == 0.f && cT == 0.f) m = INFINITY;   // no dz, as behind the last row
   v.rowc[row] = v.two ? make_float4(m, c1, cT, lab) : make_float4(m, c1 + cT, 0.f, lab);
   return val;
 }
@@ -408,7 +409,8 @@ __global__ void __launch_bounds__(256) k_vocab_dz(VocabNet v, float* db_out) {
         for (int i = 0; i < 4; ++i) d[i] -= c + i == word ? q : 0.f;
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) d[i] = c + i < v.C ? d[i] : 0.f;
+      for (int i = 0; i < 4; ++i)   // no weights: no dz, whatever z is (vocab_rows16)
+        d[i] = c + i < v.C && (k.y != 0.f || k.z != 0.f) ? d[i] : 0.f;
     }
     const float4 o = make_float4(d[0], d[1], d[2], d[3]);
     if constexpr (sizeof(OUT) == 2) st_bf4((u16*)v.dZ + at, o);
