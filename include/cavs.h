@@ -72,7 +72,8 @@
  *                                 the error that cavs_sync reports.
  *   - Errors found by kernels after a call has returned (a bounded wait that
  *     gave up, a word out of range) are kept by the context and returned by the
- *     next cavs_sync or cavs_timing_read.
+ *     next cavs_sync or cavs_timing_read: one a call, the wait's first and a
+ *     word's, where there are both, by the call after it.
  */
 #ifndef CAVS_H
 #define CAVS_H

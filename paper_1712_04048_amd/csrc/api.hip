@@ -57,17 +57,19 @@ hipError_t zero_async(void* p, size_t bytes, hipStream_t s) {
 
 cavs_status device_errors(cavs_ctx* ctx) {
   if (!ctx->dev_err) return CAVS_OK;
-  const bool range = ctx->dev_err[1] != 0;
-  ctx->dev_err[1] = 0;
-  if (!ctx->dev_err[0])
-    return range ? fail(ctx, CAVS_ERR_RANGE,
-                        "a word or label of an earlier call on this context was out of range")
-                 : CAVS_OK;
-  ctx->dev_err[0] = 0;
-  return fail(ctx, CAVS_ERR_HIP,
-              "a persistent or XCD-local level loop's grid barrier gave up waiting in an "
-              "earlier call on "
-              "this context: that call's states and gradients are invalid");
+  if (ctx->dev_err[0]) {
+    ctx->dev_err[0] = 0;
+    return fail(ctx, CAVS_ERR_HIP,
+                "a persistent or XCD-local level loop's grid barrier gave up waiting in an "
+                "earlier call on "
+                "this context: that call's states and gradients are invalid");
+  }
+  if (ctx->dev_err[1]) {
+    ctx->dev_err[1] = 0;
+    return fail(ctx, CAVS_ERR_RANGE,
+                "a word or label of an earlier call on this context was out of range");
+  }
+  return CAVS_OK;
 }
 
 namespace {

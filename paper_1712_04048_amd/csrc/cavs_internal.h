@@ -27,8 +27,9 @@ struct cavs_ctx {
   std::vector<cavs_timed_launch> timed;   // pending records
   std::vector<hipEvent_t> event_pool;     // reusable events
   hipEvent_t stage_ready = nullptr;       // the schedule's host stage has arrived
-  int32_t* dev_err = nullptr;             // pinned, coherent, mapped: set by kernels whose
-  int32_t* dev_err_dev = nullptr;         // bounded waits gave up (device view of dev_err)
+  int32_t* dev_err = nullptr;             // pinned, coherent, mapped: [0] set by kernels whose
+  int32_t* dev_err_dev = nullptr;         // bounded waits gave up, [1] by those that read a
+                                          // word out of range (device view of dev_err)
   void* sched_scratch = nullptr;          // this device's static scheduling scratch
   hipStream_t side = nullptr;             // the two-stream ablation's second stream and its
   hipEvent_t fork_ev = nullptr;           // fork / join events (created on first use)
@@ -75,8 +76,8 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 // error plumbing
 // ---------------------------------------------------------------------------
 cavs_status fail(cavs_ctx* ctx, cavs_status st, const char* fmt, ...);
-// After the context's stream has been synchronised: CAVS_OK, or the error a
-// kernel recorded in ctx->dev_err since the last check (then cleared).
+// After the context's stream has been synchronised: CAVS_OK, or an error that a
+// kernel recorded in ctx->dev_err (then cleared, another one kept).
 cavs_status device_errors(cavs_ctx* ctx);
 // Clears `bytes` (a multiple of 4) at p with a kernel on stream s.
 hipError_t zero_async(void* p, size_t bytes, hipStream_t s);
