@@ -48,11 +48,17 @@ __global__ void k_zero_words(uint32_t* p, long long n) {
 }
 
 hipError_t zero_async(void* p, size_t bytes, hipStream_t s) {
+  // a launch has fewer than 2^32 threads
+  constexpr long long kStep = 1ll << 31;
   const long long n = (long long)(bytes / 4);
-  if (n <= 0) return hipSuccess;
-  hipLaunchKernelGGL(k_zero_words, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s,
-                     (uint32_t*)p, n);
-  return hipGetLastError();
+  for (long long at = 0; at < n; at += kStep) {
+    const long long m = std::min(kStep, n - at);
+    hipLaunchKernelGGL(k_zero_words, dim3((unsigned)((m + 255) / 256)), dim3(256), 0, s,
+                       (uint32_t*)p + at, m);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 cavs_status device_errors(cavs_ctx* ctx) {
