@@ -2,6 +2,7 @@
 // straight to LDS (global_load_lds_dwordx4), fp32 accumulation on
 // v_mfma_f32_16x16x32_bf16.
 #include <algorithm>
+#include <type_traits>
 
 #include "lds_ring.h"
 #include "vocab.h"
@@ -133,6 +134,7 @@ struct Shape {
   static constexpr int WA = WA_, WB = WB_, FA = FA_, FB = FB_, S = 4;
   static constexpr int T = 64 * WA * WB, BA = 16 * FA * WA, BB = 16 * FB * WB;
   static constexpr int kStage = (BA + BB) * 64, kBytes = S * kStage;
+  static constexpr int kWgs = 8 / (WA * WB);   // that share a CU, two wavefronts a SIMD
 };
 
 constexpr int kBand = 8;
@@ -250,7 +252,11 @@ struct Product {
 // One or more independent products, the workgroups of the first ones first.
 template <class SH, class... P>
 __global__ void __launch_bounds__(SH::T, 2) k_vocab_bf(P... p) {
-  __shared__ __attribute__((aligned(16))) char lds[SH::kBytes + std::max({sizeof(typename P::Own)...})];
+  // an empty struct has a size of 1, and a workgroup of 80 KB + 1 a CU to itself
+  // (dL/dh of 64 rows, 32 000 words, H = 2048: 42 us, two a CU 38)
+  constexpr size_t kOwn = std::max({std::is_empty_v<typename P::Own> ? 0 : sizeof(typename P::Own)...});
+  static_assert(SH::kBytes + kOwn <= 160 * 1024 / SH::kWgs, "workgroups that share a CU");
+  __shared__ __attribute__((aligned(16))) char lds[SH::kBytes + kOwn];
   const int x = blockIdx.x & 7;
   int at = blockIdx.x >> 3;
   (void)(p.take(x, at, lds) || ...);
