@@ -1,8 +1,11 @@
 """The vocabulary head's gradients at sizes past 2^32 of something: words that
 are cleared, terms of a sum."""
+import math
+
 import pytest
 import torch
 
+import lm_ref as R
 from paper_1712_04048_amd import binding as B
 
 pytestmark = pytest.mark.gpu
@@ -41,3 +44,62 @@ def test_no_row_clears_every_gradient(ctx):
     ctx.sync()
     assert float(loss) == 0.0 and int(torch.count_nonzero(dbs)) == 0
     assert sum(int(torch.count_nonzero(part)) for part in dW.split(1 << 12)) == 0
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("C", [70, 2100])
+def test_weight_gradient_of_a_million_rows(ctx, dtype, C):
+    """dW_s and dbs summed over 2^20 rows of 2^31 states, exactly but for their last
+    roundings, z kept (70 words) and formed again for two pieces (2 100).
+
+    W_s = 0 and 64 words that the bias does not mask: p = 1/64 and dz = 1/64 or
+    -63/64, which bf16 holds; states of +-1 by the row's word.  Every partial sum is
+    a multiple of 1/64 below 2^18, so fp32 adds them exactly in any order.  Then
+    comes unit / rows (a rounding), its product (another) and the store."""
+    n, H = 1 << 20, 2112
+    assert n * H > 2 ** 31
+    g = torch.Generator(device="cuda").manual_seed(C)
+    words = (torch.arange(64, device="cuda") * ((C - 1) // 63)).int()
+    bs = torch.full((C,), -math.inf, device="cuda")
+    bs[words.long()] = 0.0
+    kind = torch.randint(0, 64, (n,), generator=g, device="cuda")
+    sign = (torch.randint(0, 2, (64, H), generator=g, device="cuda") * 2 - 1).to(dtype)
+    h = sign[kind]
+    y = words[kind]
+    y[: n // 2: 3] = -1
+    head = B.VocabHead(h=h, Ws=torch.zeros(H, C, dtype=dtype, device="cuda"), bs=bs, label=y)
+    loss, dh = torch.empty(1, device="cuda"), torch.empty_like(h)
+    dW, dbs = torch.empty_like(head.Ws), torch.empty_like(bs)
+    ws = torch.empty(B.vocab_workspace_bytes(head, True), dtype=torch.uint8, device="cuda")
+    B.vocab_grad(ctx, head, loss, None, dh, dW, dbs, ws)
+    ctx.sync()
+    on = y >= 0
+    live = int(on.sum())
+
+    def sums(rows):
+        """sum of h_i dz_i and of dz_i over some rows, [H, 64] and [64]"""
+        count = torch.bincount(kind[rows], minlength=64).double()
+        own = count[:, None] * sign.double()     # by word, the states of its rows
+        return own.sum(0)[:, None] / 64 - own.t(), count.sum() / 64 - count
+
+    total, db = sums(on)
+    assert float(torch.bincount(kind[on]).max()) + live / 64 < 2 ** 18
+    rounding = 3 * R.U + (R.BF if dtype == BF16 else 0.0)
+
+    def spread(t):
+        out = torch.zeros(*t.shape[:-1], C, dtype=torch.float64, device="cuda")
+        out[..., words.long()] = t / live
+        return out
+
+    want, bound = spread(total), spread(total).abs() * rounding
+    assert R.outside(dW, want, bound) <= 1.0
+    assert R.outside(dbs, spread(db), spread(db).abs() * 3 * R.U) <= 1.0
+    assert int(torch.count_nonzero(dh)) == 0
+    assert abs(float(loss) - math.log(64)) <= 8 * R.U * math.log(64)
+    # rows that were left out would be seen: one in fp32, in bf16 some hundredth of them
+    part = 1 if dtype == F32 else 1 << 14
+    for at in (1, n // 2, n - part):
+        left = on.clone()
+        left[at: at + part] = False
+        assert R.outside(spread(sums(left)[0]), want, bound) > 1.0
+    assert R.outside(torch.zeros_like(dW), want, bound) > 1.0
