@@ -388,11 +388,22 @@ typedef struct {
 } cavs_vocab;
 
 /* Bytes of device workspace cavs_vocab_loss (train = 0) or cavs_vocab_grad
-   (train = 1) needs: a copy of h and some 8 bytes for each row and 64 words for
-   the loss; for the gradient also sums of dh's size in fp32, pieces of dL/dz of
-   about 256 MB and, where one piece is all of it, up to 512 MB of z, whatever C
-   is (bf16 weights of C % 8 != 0: a copy of Ws too).  The pointers are not read,
-   but a NULL label is none.  0 on bad args. */
+   (train = 1) needs, with e = 4 bytes for fp32 weights and 2 for bf16 ones and
+   rows padded to 256 (64 of at most 64):
+     loss      a copy of h of e bytes a value; for each row and 64 (fp32) or 128
+               (bf16) words, padded to 256, 8 bytes, with a teacher 12, and 16 at
+               a temperature other than 1; 36 a row, with a teacher 44 + 12 K;
+               bf16 weights of C % 8 != 0: a copy of Ws, unless the loss alone
+               takes small tiles
+     gradient  besides, dh's sums in fp32, as often as fits into 64 MB but at
+               least once; up to 128 MB of parts of dWs; a piece of dL/dz of e
+               bytes a value, of as many words (padded to 256) as fit into 256
+               MB but at least 2048 -- more than 256 MB above 32 768 rows in
+               fp32, 65 536 in bf16.  In bf16 two such pieces where one is not
+               all of C, and where one is, up to twice its size of z besides;
+               a sixteenth of each piece's values, in fp32, for dbs.
+   Nothing else grows with n C.  The pointers are not read, but a NULL label is
+   none.  0 on bad args. */
 size_t cavs_vocab_workspace_bytes(const cavs_vocab* v, int32_t train);
 
 /* loss [1] = L; row_loss [n] (or NULL) the terms of the mean, 0 for rows that
