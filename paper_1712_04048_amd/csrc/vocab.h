@@ -5,9 +5,11 @@
 //
 // Rows without a label take no part: the live rows are listed first (rows[],
 // ascending) and everything below works on that compact numbering, whose
-// length only the device knows (live[0]).  Every buffer by row has kVocabTile-
-// padded capacity; the rows of hp and dZ that follow the live ones in the
-// gradients' contraction hold zeros.
+// length only the device knows (live[0]).  Every buffer by row has a capacity of
+// n padded to kVocabTile, or kVocabFew of at most that many: those take no tile of
+// 256 rows but of operands whose rows it bounds, and keep z, so that no such tile
+// forms their dz.  The rows of hp and dZ that follow the live ones in the gradients'
+// contraction hold zeros.
 #pragma once
 
 #include <algorithm>
@@ -23,7 +25,7 @@ constexpr int kVocabMaxK = 256;   // most teacher's words per row
 
 struct VocabNet {
   int n, H, C, K;
-  int rows;                // n padded to kVocabTile
+  int rows;                // n padded to kVocabTile (few: to kVocabFew)
   int bf;                  // products in bf16 (h and W_s rounded), else split fp32
   int hbf, wbf;            // element types of h / dh and of W_s / dW_s
   int few, pad, keep;      // at most kVocabFew rows; Ws is a padded copy; z is kept

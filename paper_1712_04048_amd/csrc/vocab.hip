@@ -23,6 +23,8 @@ constexpr size_t kPieceBytes = (size_t)256 << 20;   // of dZ
 constexpr size_t kKeepBytes = (size_t)96 << 20;     // of z in bf16, see vocab_net
 // Sizes whose tiles and offsets the kernels count in 32 bits.
 constexpr int kVocabMaxRows = 1 << 20, kVocabMaxWords = 1 << 20, kVocabMaxH = 1 << 15;
+static_assert(kPieceBytes / (kVocabFew * 4) >= kVocabMaxWords,
+              "few rows are one piece, whose z is kept: their buffers end before a tile of 256 rows");
 
 // The live rows: their list and numbering, their labels, their rows of h in the
 // products' type (zeros behind the last), and unit / their number.
