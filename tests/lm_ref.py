@@ -8,9 +8,14 @@ value (torch.finfo(torch.bfloat16).eps / 2).
   terms each included: at most (2 n + 16) u of the sum of the terms' magnitudes.
 * exp(x) of a rounded x: x carries two roundings (the difference, the change of
   base), the instruction one step: relative (2 |x| + 4) 2u.
-* Positive sums over the vocabulary pass at most 32 + 2 + ceil(slots / 16) + 16
-  additions: 600 u covers 2^20 words on 64-word slots per workgroup's wavefront
-  up to 32 768 words; the tests stay below.
+* Positive sums over the vocabulary: a term passes the additions of its slot of
+  64 (fp32) or 128 (bf16) words, 16 or 32 in a lane and two between lanes, then
+  one for each slot of its lane of the join, which takes every 64th, and 64 for
+  the lanes.  It is multiplied by an exponential (9 u each, their exponents add up
+  to the term's own) where the slot is joined from wavefronts, where it joins the
+  lane's sum, wherever the largest z grows between groups of eight slots, and
+  with the lanes'.  600 u covers all of that up to 900 000 words, and 2^20 where
+  the largest z grows in no more than 25 of a lane's 32 groups (test_lm_bounds).
 """
 import math
 
