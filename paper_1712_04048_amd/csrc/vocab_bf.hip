@@ -268,7 +268,9 @@ void launch(const char* name, hipStream_t s, P... p) {
 }
 
 // Words are the tile's A rows: lane (g, r) holds words 16 f + 4 g .. + 3 of its
-// row r of each group of 16.
+// row r of each group of 16.  dz with a teacher needs 14 registers more than there
+// are beside the sums: they go through scratch in the epilogue, 14 stores and 43
+// loads of a lane each tile; the products spill nothing, nor do the other epilogues.
 template <bool LOSS, bool TEACH>
 struct BfVocab {
   VocabEp e;
