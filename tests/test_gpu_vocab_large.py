@@ -7,6 +7,7 @@ import torch
 
 import lm_ref as R
 from paper_1712_04048_amd import binding as B
+from test_gpu_vocab import check, grad, loss, make, reference
 
 pytestmark = pytest.mark.gpu
 
@@ -103,3 +104,28 @@ def test_weight_gradient_of_a_million_rows(ctx, dtype, C):
         left[at: at + part] = False
         assert R.outside(spread(sums(left)[0]), want, bound) > 1.0
     assert R.outside(torch.zeros_like(dW), want, bound) > 1.0
+
+
+@pytest.mark.parametrize("types", [(F32, F32), (BF16, BF16), (F32, BF16)])
+@pytest.mark.parametrize("n,C,K", [(1, 3, 0), (70, 300, 4), (300, 2001, 0), (600, 33000, 3)])
+def test_largest_width_of_the_states(ctx, types, n, C, K):
+    """H = 2^15, on tiles of every size."""
+    head = make(n, n, C, 1 << 15, types, pad=0.1 if n > 1 else 0.0, K=K, alpha=0.5, temp=2.0 if K else 1.0)
+    want, bound = reference(head)
+    got = grad(ctx, head)
+    ctx.sync()
+    check(got, want, bound)
+    alone = loss(ctx, head)
+    ctx.sync()
+    assert torch.equal(alone["loss"], got["loss"])
+
+
+@pytest.mark.parametrize("types", [(F32, F32), (BF16, BF16)])
+def test_many_pieces(ctx, types):
+    """Seven (fp32) and four pieces of the vocabulary, the halves of dz in turn, the last
+    one narrower."""
+    head = make(7, 40000, 12301, 64, types, pad=0.1)
+    want, bound = reference(head)
+    got = grad(ctx, head)
+    ctx.sync()
+    check(got, want, bound)
