@@ -12,7 +12,8 @@ namespace cavs {
 namespace {
 
 // Sizes whose indices the kernels count in 32 bits.  The gradient's sort reads
-// every place once for each 512 words of the table, which bounds both.
+// every place for each 512 words of the table, once of up to 32 768 places and
+// twice of more, which bounds both.
 constexpr int kEmbedMax = 1 << 28, kEmbedMaxD = 1 << 14, kGradMax = 1 << 22;
 constexpr int kPart = 32;         // rows of a word that one wavefront adds
 constexpr int kSortWords = 512;   // most words of a sorting workgroup
