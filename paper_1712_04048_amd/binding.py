@@ -385,15 +385,11 @@ def backward(ctx: Context, params: Params, sched: Schedule, X: Optional[torch.Te
 _TYPES = {torch.float32: T_F32, torch.bfloat16: T_BF16}
 
 
-def _tensor(name: str, t) -> torch.Tensor:
-    if not isinstance(t, torch.Tensor):
-        raise CavsError(ERR_ARG, "%s: a tensor is required" % name)
-    return t
-
-
 def _operand(name: str, t: Optional[torch.Tensor], shape, dtypes, device) -> Optional[int]:
     """The address of a tensor after the checks that the C ABI cannot make."""
-    if _tensor(name, t).dtype not in dtypes:
+    if not isinstance(t, torch.Tensor):
+        raise CavsError(ERR_ARG, "%s: a tensor is required" % name)
+    if t.dtype not in dtypes:
         raise CavsError(ERR_ARG, "%s: %s, not %s" % (name, t.dtype, " or ".join(map(str, dtypes))))
     if tuple(t.shape) != tuple(shape):
         raise CavsError(ERR_ARG, "%s: shape %s, not %s" % (name, tuple(t.shape), tuple(shape)))
@@ -404,9 +400,17 @@ def _operand(name: str, t: Optional[torch.Tensor], shape, dtypes, device) -> Opt
     return t.data_ptr() if t.numel() else None
 
 
+def _sized(name: str, t: torch.Tensor) -> int:
+    """The elements of a tensor whose other properties _operand checks."""
+    try:
+        return t.numel()
+    except AttributeError:
+        raise CavsError(ERR_ARG, "%s: a tensor is required" % name) from None
+
+
 def _workspace(ws: torch.Tensor, device):
-    _operand("ws", ws, (_tensor("ws", ws).numel(),), (torch.uint8,), device)
-    return ws.data_ptr(), ws.numel()
+    n = _sized("ws", ws)
+    return _operand("ws", ws, (n,), (torch.uint8,), device), n
 
 
 @dataclass
@@ -427,8 +431,8 @@ class Embedding:
 
 def embed(ctx: Context, emb: Embedding, word: torch.Tensor, X: torch.Tensor) -> None:
     """cavs_embed: X [n, D] = scale * E[word] (asynchronous); int32 word -1: zeros."""
-    dev, n = ctx.torch_device, int(_tensor("word", word).numel())
-    e = emb.raw(_tensor("X", X).dtype, dev)
+    dev, n = ctx.torch_device, _sized("word", word)
+    e = emb.raw(getattr(X, "dtype", None), dev)
     ctx.check(lib().cavs_embed(ctx._h, ct.byref(e), _operand("word", word, (n,), (torch.int32,), dev),
                                n, _operand("X", X, (n, e.D), _TYPES, dev)))
 
@@ -442,8 +446,8 @@ def embed_grad(ctx: Context, emb: Embedding, word: torch.Tensor, dX: torch.Tenso
                dE: torch.Tensor, ws: torch.Tensor) -> None:
     """cavs_embed_grad: dE [n_words, D] of E's type, overwritten, from dX [n, D]
     (asynchronous)."""
-    dev, n = ctx.torch_device, int(_tensor("word", word).numel())
-    e = emb.raw(_tensor("dX", dX).dtype, dev)
+    dev, n = ctx.torch_device, _sized("word", word)
+    e = emb.raw(getattr(dX, "dtype", None), dev)
     ctx.check(lib().cavs_embed_grad(
         ctx._h, ct.byref(e), _operand("word", word, (n,), (torch.int32,), dev), n,
         _operand("dX", dX, (n, e.D), _TYPES, dev),
@@ -472,7 +476,8 @@ class VocabHead:
         n, H, C = int(self.h.shape[0]), int(self.h.shape[1]), int(self.Ws.shape[1])
         K = 0
         if self.top_word is not None or self.top_logit is not None:
-            if self.top_logit is None or _tensor("top_word", self.top_word).dim() != 2:
+            if (not isinstance(self.top_word, torch.Tensor) or self.top_logit is None
+                    or self.top_word.dim() != 2):
                 raise CavsError(ERR_ARG, "top_word and top_logit [n, K] go together")
             K = int(self.top_word.shape[1])
         f, i = (torch.float32,), (torch.int32,)
