@@ -419,6 +419,125 @@ cavs_status cavs_vocab_grad(cavs_ctx* ctx, const cavs_vocab* v, float* loss, flo
                             void* dh, void* dWs, float* dbs, void* ws, size_t ws_bytes);
 
 /* ---------------------------------------------------------------------------
+ * The end of a training step: the norm of all gradients together, and the
+ * gradients scaled so that it stays below a limit,
+ *   norm = |scale| sqrt(sum of all g^2),   out = scale min(1, max_norm / norm) g
+ * with squares and sums in fp64 and one rounding of each product to fp32 and of
+ * each output to its type; the same bits from run to run.  A norm that is not
+ * finite (a gradient is not) clips nothing: out = scale g, and norm says so.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  const void* g;            /* [n] gradient, aligned to its elements */
+  void* out;                /* [n]: g itself (of one type then), other memory, or NULL: g
+                               counts for the norm and is not written */
+  int64_t n;                /* 0 .. 2^32 */
+  int32_t g_type, out_type; /* CAVS_T_* */
+} cavs_grad;
+
+/* Bytes of device workspace cavs_clip_grads needs, whatever the gradients. */
+size_t cavs_clip_workspace_bytes(void);
+
+/* grads (host) [count], read before the call returns; norm [1].  max_norm >= 0;
+   infinity clips nothing.  Where nothing changes (the factor is 1 and out is g)
+   nothing is written.  Outputs must not overlap other gradients or each other.
+   Asynchronous, allocates nothing, may be captured into a graph, which keeps the
+   list's addresses. */
+cavs_status cavs_clip_grads(cavs_ctx* ctx, const cavs_grad* grads, int32_t count, float scale,
+                            float max_norm, float* norm, void* ws, size_t ws_bytes);
+
+/* ---------------------------------------------------------------------------
+ * The next word: a vocabulary head in 4 bits that scores pushed states, and the
+ * rules that turn its scores into what the next word is taken from.  A step of a
+ * model that answers is
+ *   cavs_embed -> cavs_infer -> cavs_embed (the last states' rows) ->
+ *   cavs_quant_product -> cavs_adjust_logits.
+ * The calls allocate nothing, synchronise nothing and may be captured into a
+ * graph.  Outputs must not overlap inputs or each other, but for logits that are
+ * adjusted in place.
+ *
+ * Weights in 4 bits: of each column of W [H, C], `group` rows share a scale
+ * (and a shift), both bf16:
+ *   What[k, c] = s (q[k, c] - 8) + m,   q in 0 .. 15,
+ * q - 8 the nearest whole number to (w - m) / s (the even one of two), kept in
+ * -8 .. 7.  Without shifts m = 0 and s = -e / 8, e the group's end that is further
+ * from 0 (the lower of two alike); with them s = (highest - lowest) / 15 and m =
+ * (highest + lowest + s) / 2.  Both are rounded to fp32 and that to bf16 before q is taken; a group
+ * of zeros has s = 0; one with a weight that is not finite has s = NaN.
+ *
+ * `data` is cavs_quant_bytes(q) bytes, aligned to 16, that cavs_quant_pack writes
+ * and a program may keep in files.  With T = ceil(C / 16) and KB = ceil(H / 128):
+ * first the codes: of word c and row k, block (c / 16) KB + k / 128 of 1024 bytes;
+ * in it, lane 16 (k / 8 % 4) + c % 16 of 16 bytes; in it, dword k / 32 % 4; in it,
+ * with i = k % 8, bits 4 p .. 4 p + 3, p = i / 2 for even i and 4 + i / 2 (rounded
+ * down) for odd ones.  Then (s) or (s, m) in bf16 at
+ * ((block 16 + c % 16) 128 / group + k % 128 / group).  What lies past H or C has
+ * q = 8, s = m = 0.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  int32_t H, C;             /* rows and words, > 0; at most 2^15 and 2^20 */
+  int32_t group;            /* 32, 64 or 128 rows; the last group may be shorter */
+  int32_t shift;            /* 1: groups have shifts, 0: none */
+  const void* data;         /* cavs_quant_unpack, _product: the packed weights */
+} cavs_quant;
+
+/* Bytes of the packed weights.  0 on bad args. */
+size_t cavs_quant_bytes(const cavs_quant* q);
+
+/* Rounds W [H, C] (w_type) to 4 bits; writes all of data (q->data is not read). */
+cavs_status cavs_quant_pack(cavs_ctx* ctx, const cavs_quant* q, int32_t w_type, const void* W,
+                            void* data);
+
+/* W = What, rounded once to w_type. */
+cavs_status cavs_quant_unpack(cavs_ctx* ctx, const cavs_quant* q, int32_t w_type, void* W);
+
+/* y [n, C] = x [n, H] What + bias (bias [C] or NULL), n <= 2^20, made for the few
+   rows of a decoding step.  x is not rounded (an fp32 x by 2^-24 of it at most);
+   products are exact, sums fp32, y is rounded once.  A row of x that is not finite
+   gives infinities or NaN in that row alone. */
+cavs_status cavs_quant_product(cavs_ctx* ctx, const cavs_quant* q, int32_t x_type, const void* x,
+                               int32_t n, const float* bias, int32_t y_type, void* y);
+
+/* Rules on logits.  Of row i and word c, said k times in the row's past, in this
+ * order, each step rounded to fp32:
+ *   v = z;  where k > 0: v = v > 0 ? v / repeat : v repeat, v -= presence,
+ *                        v -= frequency k
+ *   v += bias_c;  v += sum of the row's extra of c (in the list's order)
+ *   v = -inf where the row's mask has c's bit clear;  v /= temp
+ * Every array may be NULL: its step is left out (with all three penalties NULL, or
+ * L = 0, past is not read).  Words -1 are none; a word or mask row out of range
+ * counts as -1, and the next cavs_sync or cavs_timing_read returns
+ * CAVS_ERR_RANGE.  repeat and temp should be above 0: they are not checked. */
+typedef struct {
+  int32_t z_type, out_type; /* CAVS_T_* */
+  int32_t n, C;             /* rows, words; at most 2^20 each */
+  int32_t L;                /* words of a row's past, at most 2^20 */
+  const int32_t* past;      /* [n, L] */
+  const float* repeat;      /* [n] */
+  const float* presence;    /* [n] */
+  const float* frequency;   /* [n] */
+  const float* bias;        /* [C], every row's */
+  int32_t K;                /* words with a bias of their own in a row, at most 1024 */
+  const int32_t* extra_word;/* [n, K] */
+  const float* extra;       /* [n, K] */
+  int32_t M;                /* masks */
+  const uint32_t* mask;     /* [M, ceil(C / 32)], word c in bit c % 32 of c / 32: 1 may come */
+  const int32_t* mask_row;  /* [n] each row's mask, -1: none; NULL: row i has mask i (M = n), or
+                               all the only one (M = 1) */
+  const float* temp;        /* [n] */
+} cavs_rules;
+
+/* Bytes of device workspace cavs_adjust_logits needs.  0 on bad args. */
+size_t cavs_adjust_workspace_bytes(int32_t n, int32_t C);
+
+/* out [n, C] (may be z itself, of one type then, or NULL) the v; best [n] (or
+   NULL) the first of each row's largest v, not NaN, or -1 where no v is above
+   -inf; lse [n] (or NULL) ln sum_c exp(v_c), so that v - lse is the word's log
+   probability: -inf for a row without words, NaN with one.  best and lse are of
+   the v before out is rounded. */
+cavs_status cavs_adjust_logits(cavs_ctx* ctx, const cavs_rules* rules, const void* z, void* out,
+                               int32_t* best, float* lse, void* ws, size_t ws_bytes);
+
+/* ---------------------------------------------------------------------------
  * Instrumentation (not part of the computation).  When enabled, every kernel
  * the library launches on the context's stream is bracketed by a pair of HIP
  * events, so per-kernel GPU durations can be read back.  Off by default; the

@@ -88,12 +88,30 @@ class cavs_vocab(ct.Structure):
                 ("temp", ct.c_float)]
 
 
+class cavs_grad(ct.Structure):
+    _fields_ = [("g", _vp), ("out", _vp), ("n", ct.c_int64), ("g_type", _i32), ("out_type", _i32)]
+
+
+class cavs_quant(ct.Structure):
+    _fields_ = [("H", _i32), ("C", _i32), ("group", _i32), ("shift", _i32), ("data", _vp)]
+
+
+class cavs_rules(ct.Structure):
+    _fields_ = [("z_type", _i32), ("out_type", _i32), ("n", _i32), ("C", _i32), ("L", _i32),
+                ("past", _vp), ("repeat", _vp), ("presence", _vp), ("frequency", _vp), ("bias", _vp),
+                ("K", _i32), ("extra_word", _vp), ("extra", _vp), ("M", _i32), ("mask", _vp),
+                ("mask_row", _vp), ("temp", _vp)]
+
+
 EXPORTS = ["cavs_create", "cavs_set_stream", "cavs_destroy", "cavs_last_error", "cavs_sync",
            "cavs_schedule_workspace_bytes", "cavs_schedule", "cavs_schedule_static",
            "cavs_workspace_bytes",
            "cavs_forward", "cavs_backward", "cavs_infer_workspace_bytes", "cavs_infer",
            "cavs_embed", "cavs_embed_grad_workspace_bytes", "cavs_embed_grad",
            "cavs_vocab_workspace_bytes", "cavs_vocab_loss", "cavs_vocab_grad",
+           "cavs_clip_workspace_bytes", "cavs_clip_grads", "cavs_quant_bytes", "cavs_quant_pack",
+           "cavs_quant_unpack", "cavs_quant_product", "cavs_adjust_workspace_bytes",
+           "cavs_adjust_logits",
            "cavs_timing_enable", "cavs_timing_read"]
 
 _lib = None
@@ -149,6 +167,23 @@ def lib():
         L.cavs_vocab_loss.argtypes = [_vp, voc, _vp, _vp, _vp, ct.c_size_t]
         L.cavs_vocab_grad.restype = _i32
         L.cavs_vocab_grad.argtypes = [_vp, voc, _vp, _vp, _vp, _vp, _vp, _vp, ct.c_size_t]
+        quant, f32 = ct.POINTER(cavs_quant), ct.c_float
+        L.cavs_clip_workspace_bytes.restype = ct.c_size_t
+        L.cavs_clip_workspace_bytes.argtypes = []
+        L.cavs_clip_grads.restype = _i32
+        L.cavs_clip_grads.argtypes = [_vp, ct.POINTER(cavs_grad), _i32, f32, f32, _vp, _vp, ct.c_size_t]
+        L.cavs_quant_bytes.restype = ct.c_size_t
+        L.cavs_quant_bytes.argtypes = [quant]
+        L.cavs_quant_pack.restype = _i32
+        L.cavs_quant_pack.argtypes = [_vp, quant, _i32, _vp, _vp]
+        L.cavs_quant_unpack.restype = _i32
+        L.cavs_quant_unpack.argtypes = [_vp, quant, _i32, _vp]
+        L.cavs_quant_product.restype = _i32
+        L.cavs_quant_product.argtypes = [_vp, quant, _i32, _vp, _i32, _vp, _i32, _vp]
+        L.cavs_adjust_workspace_bytes.restype = ct.c_size_t
+        L.cavs_adjust_workspace_bytes.argtypes = [_i32, _i32]
+        L.cavs_adjust_logits.restype = _i32
+        L.cavs_adjust_logits.argtypes = [_vp, ct.POINTER(cavs_rules), _vp, _vp, _vp, _vp, _vp, ct.c_size_t]
         L.cavs_timing_enable.restype = _i32
         L.cavs_timing_enable.argtypes = [_vp, _i32]
         L.cavs_timing_read.restype = _i32
@@ -520,3 +555,173 @@ def vocab_grad(ctx: Context, head: VocabHead, loss: torch.Tensor,
         _operand("dh", dh, (v.n, v.H), (head.h.dtype,), dev),
         _operand("dWs", dWs, (v.H, v.C), (head.Ws.dtype,), dev),
         None if dbs is None else _operand("dbs", dbs, (v.C,), f, dev), *_workspace(ws, dev)))
+
+
+# --------------------------------------------------------------------------
+# The end of a training step (gradient norm and clipping)
+# --------------------------------------------------------------------------
+
+
+class GradList:
+    """Gradients (float32 or bfloat16, any shapes) and where they go scaled:
+    ``out`` a list of as many tensors of the same shapes (None: not written), or
+    None for in place.  Holds the tensors; made once for many calls."""
+
+    def __init__(self, grads, out=None):
+        self.grads = list(grads)
+        self.out = self.grads if out is None else list(out)
+        if len(self.out) != len(self.grads):
+            raise CavsError(ERR_ARG, "out: %d tensors for %d gradients" % (len(self.out), len(self.grads)))
+        device = None
+        self.raw = (cavs_grad * len(self.grads))()
+        for k, (g, o) in enumerate(zip(self.grads, self.out)):
+            if not isinstance(g, torch.Tensor):
+                raise CavsError(ERR_ARG, "gradient %d: a tensor is required" % k)
+            device = device if device is not None else g.device
+            p = _operand("gradient %d" % k, g, g.shape, _TYPES, device)
+            q = None if o is None else _operand("out %d" % k, o, g.shape, _TYPES, device)
+            self.raw[k] = cavs_grad(p, q, g.numel(), _TYPES[g.dtype], _TYPES[(g if o is None else o).dtype])
+        self.device = device
+
+
+def clip_workspace_bytes() -> int:
+    return int(lib().cavs_clip_workspace_bytes())
+
+
+def clip_grads(ctx: Context, grads: GradList, max_norm: float, norm: torch.Tensor, ws: torch.Tensor,
+               scale: float = 1.0) -> None:
+    """cavs_clip_grads (asynchronous): norm [1] of all gradients times scale, and
+    the gradients times scale, and times max_norm / norm where that is below 1."""
+    dev = ctx.torch_device
+    if not isinstance(grads, GradList):
+        raise CavsError(ERR_ARG, "grads: a GradList is required")
+    if grads.device is not None and grads.device != dev:
+        raise CavsError(ERR_ARG, "the gradients are on %s, the context on %s" % (grads.device, dev))
+    ctx.check(lib().cavs_clip_grads(ctx._h, grads.raw, len(grads.grads), float(scale), float(max_norm),
+                                    _operand("norm", norm, (1,), (torch.float32,), dev),
+                                    *_workspace(ws, dev)))
+
+
+# --------------------------------------------------------------------------
+# The next word (a head in 4 bits, rules on logits)
+# --------------------------------------------------------------------------
+
+
+def quant_bytes(H: int, C: int, group: int = 128, shift: bool = False) -> int:
+    """Bytes of the packed weights; 0 for sizes that are refused."""
+    q = cavs_quant(int(H), int(C), int(group), int(bool(shift)), None)
+    return int(lib().cavs_quant_bytes(ct.byref(q)))
+
+
+@dataclass
+class QuantWeights:
+    """Weights [H, C] in 4 bits: data, a uint8 tensor of quant_bytes(H, C, group,
+    shift), as quant_pack writes it; group rows share a scale, and with shift a
+    shift."""
+    data: torch.Tensor
+    H: int
+    C: int
+    group: int = 128
+    shift: bool = False
+
+    def raw(self, device=None) -> cavs_quant:
+        n = quant_bytes(self.H, self.C, self.group, self.shift)
+        # refused sizes are the library's to name
+        shape = (n,) if n else getattr(self.data, "shape", ())
+        p = _operand("data", self.data, shape, (torch.uint8,), device)
+        return cavs_quant(int(self.H), int(self.C), int(self.group), int(bool(self.shift)), p)
+
+
+def quant_pack(ctx: Context, q: QuantWeights, W: torch.Tensor) -> None:
+    """cavs_quant_pack (asynchronous): q's data from W [H, C]."""
+    dev = ctx.torch_device
+    r = q.raw(dev)
+    p = _operand("W", W, (q.H, q.C), _TYPES, dev)
+    ctx.check(lib().cavs_quant_pack(ctx._h, ct.byref(r), _TYPES[W.dtype], p, r.data))
+
+
+def quant_unpack(ctx: Context, q: QuantWeights, W: torch.Tensor) -> None:
+    """cavs_quant_unpack (asynchronous): W [H, C], the weights that q stands for."""
+    dev = ctx.torch_device
+    r = q.raw(dev)
+    p = _operand("W", W, (q.H, q.C), _TYPES, dev)
+    ctx.check(lib().cavs_quant_unpack(ctx._h, ct.byref(r), _TYPES[W.dtype], p))
+
+
+def quant_product(ctx: Context, q: QuantWeights, x: torch.Tensor, y: torch.Tensor,
+                  bias: Optional[torch.Tensor] = None) -> None:
+    """cavs_quant_product (asynchronous): y [n, C] = x [n, H] What + bias [C]."""
+    dev = ctx.torch_device
+    r = q.raw(dev)
+    if not isinstance(x, torch.Tensor) or x.dim() != 2:
+        raise CavsError(ERR_ARG, "x: a matrix is required")
+    n = int(x.shape[0])
+    px, py = _operand("x", x, (n, q.H), _TYPES, dev), _operand("y", y, (n, q.C), _TYPES, dev)
+    pb = None if bias is None else _operand("bias", bias, (q.C,), (torch.float32,), dev)
+    ctx.check(lib().cavs_quant_product(ctx._h, ct.byref(r), _TYPES[x.dtype], px, n, pb, _TYPES[y.dtype], py))
+
+
+@dataclass
+class LogitRules:
+    """What turns a model's logits [n, C] into those that its next word is taken
+    from: words so far past [n, L] int32 (-1: none) with repeat, presence and
+    frequency [n]; bias [C]; extra_word [n, K] int32 with extra [n, K]; mask
+    [M, ceil(C / 32)] int32 (bit c % 32 of word c / 32: c may come) with mask_row
+    [n] int32 (-1: no mask); temp [n].  Floats are float32; None leaves a rule out."""
+    bias: Optional[torch.Tensor] = None
+    past: Optional[torch.Tensor] = None
+    repeat: Optional[torch.Tensor] = None
+    presence: Optional[torch.Tensor] = None
+    frequency: Optional[torch.Tensor] = None
+    extra_word: Optional[torch.Tensor] = None
+    extra: Optional[torch.Tensor] = None
+    mask: Optional[torch.Tensor] = None
+    mask_row: Optional[torch.Tensor] = None
+    temp: Optional[torch.Tensor] = None
+
+    def raw(self, n: int, C: int, z_type: int, out_type: int, device=None) -> cavs_rules:
+        f, i = (torch.float32,), (torch.int32,)
+
+        def columns(name, t):
+            if t is None:
+                return 0
+            if not isinstance(t, torch.Tensor) or t.dim() != 2:
+                raise CavsError(ERR_ARG, "%s: a matrix is required" % name)
+            return int(t.shape[1])
+
+        def p(name, shape, types):
+            t = getattr(self, name)
+            return None if t is None else _operand(name, t, shape, types, device)
+
+        L, K = columns("past", self.past), columns("extra_word", self.extra_word)
+        columns("mask", self.mask)
+        M = 0 if self.mask is None else int(self.mask.shape[0])
+        if self.past is None and any(t is not None for t in (self.repeat, self.presence, self.frequency)):
+            raise CavsError(ERR_ARG, "repeat, presence and frequency need past")
+        if (self.extra_word is None) != (self.extra is None):
+            raise CavsError(ERR_ARG, "extra_word and extra [n, K] go together")
+        return cavs_rules(
+            z_type, out_type, n, C, L, p("past", (n, L), i), p("repeat", (n,), f), p("presence", (n,), f),
+            p("frequency", (n,), f), p("bias", (C,), f), K, p("extra_word", (n, K), i),
+            p("extra", (n, K), f), M, p("mask", (M, -(-C // 32)), i), p("mask_row", (n,), i),
+            p("temp", (n,), f))
+
+
+def adjust_workspace_bytes(n: int, C: int) -> int:
+    return int(lib().cavs_adjust_workspace_bytes(int(n), int(C)))
+
+
+def adjust_logits(ctx: Context, rules: LogitRules, z: torch.Tensor, out: Optional[torch.Tensor],
+                  best: Optional[torch.Tensor], lse: Optional[torch.Tensor], ws: torch.Tensor) -> None:
+    """cavs_adjust_logits (asynchronous): out [n, C] (may be z), best [n] int32,
+    lse [n] float32; what is None is not written."""
+    dev = ctx.torch_device
+    if not isinstance(z, torch.Tensor) or z.dim() != 2:
+        raise CavsError(ERR_ARG, "z: a matrix is required")
+    n, C = int(z.shape[0]), int(z.shape[1])
+    pz = _operand("z", z, (n, C), _TYPES, dev)
+    po = None if out is None else _operand("out", out, (n, C), _TYPES, dev)
+    r = rules.raw(n, C, _TYPES[z.dtype], _TYPES[(z if out is None else out).dtype], dev)
+    ctx.check(lib().cavs_adjust_logits(
+        ctx._h, ct.byref(r), pz, po, None if best is None else _operand("best", best, (n,), (torch.int32,), dev),
+        None if lse is None else _operand("lse", lse, (n,), (torch.float32,), dev), *_workspace(ws, dev)))

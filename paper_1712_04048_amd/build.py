@@ -19,7 +19,8 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
 SOURCES = ["api.hip", "schedule.hip", "lstm.hip", "lstm_loop.hip", "lstm_tile.hip", "fc.hip", "lazy.hip",
-           "generic.hip", "x3.hip", "embed.hip", "vocab.hip", "vocab_x3.hip", "vocab_bf.hip"]
+           "generic.hip", "x3.hip", "embed.hip", "vocab.hip", "vocab_x3.hip", "vocab_bf.hip",
+           "quant.hip", "rules.hip", "clip.hip"]
 
 CFLAGS = [
     "-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",

@@ -873,4 +873,54 @@ cavs_status cavs_vocab_grad(cavs_ctx* ctx, const cavs_vocab* v, float* loss, flo
   return vocab_run(ctx, v, loss, row_loss, dh, dWs, dbs, ws, ws_bytes, true);
 }
 
+size_t cavs_clip_workspace_bytes(void) { return clip_ws_bytes(); }
+
+cavs_status cavs_clip_grads(cavs_ctx* ctx, const cavs_grad* grads, int32_t count, float scale,
+                            float max_norm, float* norm, void* ws, size_t ws_bytes) {
+  if (!ctx) return CAVS_ERR_ARG;
+  ctx->err.clear();
+  CAVS_HIP_CHECK(ctx, hipSetDevice(ctx->device));
+  ActiveCtx active(ctx);
+  return clip_run(ctx, grads, count, scale, max_norm, norm, ws, ws_bytes);
+}
+
+size_t cavs_quant_bytes(const cavs_quant* q) { return quant_bytes(q); }
+
+cavs_status cavs_quant_pack(cavs_ctx* ctx, const cavs_quant* q, int32_t w_type, const void* W,
+                            void* data) {
+  if (!ctx) return CAVS_ERR_ARG;
+  ctx->err.clear();
+  CAVS_HIP_CHECK(ctx, hipSetDevice(ctx->device));
+  ActiveCtx active(ctx);
+  return quant_pack_run(ctx, q, w_type, W, data);
+}
+
+cavs_status cavs_quant_unpack(cavs_ctx* ctx, const cavs_quant* q, int32_t w_type, void* W) {
+  if (!ctx) return CAVS_ERR_ARG;
+  ctx->err.clear();
+  CAVS_HIP_CHECK(ctx, hipSetDevice(ctx->device));
+  ActiveCtx active(ctx);
+  return quant_unpack_run(ctx, q, w_type, W);
+}
+
+cavs_status cavs_quant_product(cavs_ctx* ctx, const cavs_quant* q, int32_t x_type, const void* x,
+                               int32_t n, const float* bias, int32_t y_type, void* y) {
+  if (!ctx) return CAVS_ERR_ARG;
+  ctx->err.clear();
+  CAVS_HIP_CHECK(ctx, hipSetDevice(ctx->device));
+  ActiveCtx active(ctx);
+  return quant_product_run(ctx, q, x_type, x, n, bias, y_type, y);
+}
+
+size_t cavs_adjust_workspace_bytes(int32_t n, int32_t C) { return adjust_ws_bytes(n, C); }
+
+cavs_status cavs_adjust_logits(cavs_ctx* ctx, const cavs_rules* rules, const void* z, void* out,
+                               int32_t* best, float* lse, void* ws, size_t ws_bytes) {
+  if (!ctx) return CAVS_ERR_ARG;
+  ctx->err.clear();
+  CAVS_HIP_CHECK(ctx, hipSetDevice(ctx->device));
+  ActiveCtx active(ctx);
+  return adjust_run(ctx, rules, z, out, best, lse, ws, ws_bytes);
+}
+
 }  // extern "C"

@@ -1,0 +1,509 @@
+// A head in 4 bits: its rounding, and its product with a few rows.
+//
+//   What[k, c] = s[g, c] (q[k, c] - 8) + m[g, c],  g = k / group,  q in 0 .. 15
+//
+// Layout.  Words are cut into tiles of 16, rows of W into blocks of 128; a tile's
+// block is 1024 bytes, 16 for each lane l = 16 j + (c % 16) of a wavefront: four
+// dwords, dword b holding k = 32 b + 8 j + i, i = 0 .. 7, of column c -- what the
+// lane feeds to the four 32-deep matrix instructions of the block.  Nibble p of a
+// dword (bits 4p ..) is i = 2p (p < 4) or 2 (p - 4) + 1: two masks and a shift then
+// leave adjacent i in the two halves of a register.  A tile's blocks follow each
+// other, then the next tile's.  The scales come after all codes: for each tile,
+// block and column the 128 / group scales of its groups (bf16), each followed by its
+// shift where there are any.  What is past H or C has q = 8 and s = m = 0.
+#include <algorithm>
+
+#include "vocab.h"
+
+namespace cavs {
+namespace {
+
+constexpr int kQuantMaxH = 1 << 15, kQuantMaxC = 1 << 20, kQuantMaxN = 1 << 20;
+constexpr int kQB = 128;   // rows of W in a block
+
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+
+struct QuantNet {
+  int H, C, T, KB;             // T tiles of 16 words, KB blocks of kQB rows
+  const uint4* code;           // [T][KB][64]
+  const u16* scale;            // [T][KB][16][128 / group][1 + shift]
+};
+
+__device__ __forceinline__ float load_one(const float* p) { return *p; }
+__device__ __forceinline__ float load_one(const u16* p) { return __uint_as_float((uint32_t)*p << 16); }
+__device__ __forceinline__ void store_one(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store_one(u16* p, float v) { *p = f2bf(v); }
+__device__ __forceinline__ float bf2f(u16 v) { return __uint_as_float((uint32_t)v << 16); }
+
+// To fp32 and then to bf16, as the format says; in one expression with contraction
+// the two roundings become one.
+__device__ __forceinline__ u16 round_twice(double v) {
+#pragma clang fp contract(off)
+  const float f = (float)v;
+  return f2bf(f);
+}
+
+// The code of w: the whole number nearest to (w - m) / s, the even one of two, in
+// -8 .. 7.  t is off by a few roundings (of 1 / s, of the difference and of the
+// product: `near` bounds them), so what is that close to a border is divided in 64
+// bits, where every such quotient of a float less a bf16 and a bf16 falls on the
+// right side.
+__device__ __forceinline__ int quant_code(float w, float s, float m, float inv, float near) {
+  const float t = (w - m) * inv, r = rintf(t);
+  float q = r;
+  if (!(fabsf(fabsf(t - r) - 0.5f) > near)) q = (float)rint(((double)w - (double)m) / (double)s);
+  return (int)fminf(fmaxf(q, -8.f), 7.f);
+}
+
+// 64 columns of a block of 128 rows to a workgroup: wavefront b has rows 32 b ..
+// of them in registers, so that W is read once; groups of more than 32 rows join
+// their ends through LDS.  The dwords are turned into the layout's order in LDS.
+// Bound by memory: W once in, 4 bits a weight out.
+template <class T, int G, bool SHIFT>
+__global__ void __launch_bounds__(256) k_quant_pack(QuantNet q, const T* __restrict__ W, uint4* code,
+                                                    u16* scale) {
+  __shared__ float ends[2][4][64];
+  __shared__ uint32_t dw[4][4][4][16];   // [tile][j][column][b], 16 bytes a lane of the layout
+  const int lane = threadIdx.x & 63, b = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kb = blockIdx.y, c = blockIdx.x * 64 + lane, k0 = kb * kQB + 32 * b;
+  const int rows = min(32, q.H - k0);   // may be negative
+  const bool in = c < q.C;
+  float w[32];
+#pragma unroll
+  for (int i = 0; i < 32; ++i) w[i] = in && i < rows ? load_one(W + (size_t)(k0 + i) * q.C + c) : 0.f;
+  float lo = INFINITY, hi = -INFINITY;
+  bool fine = true;
+#pragma unroll
+  for (int i = 0; i < 32; ++i)
+    if (i < rows) {
+      lo = fminf(lo, w[i]);
+      hi = fmaxf(hi, w[i]);
+      fine &= fabsf(w[i]) < INFINITY;
+    }
+  if (!fine) lo = -INFINITY, hi = INFINITY;
+  if (G > 32) {
+    ends[0][b][lane] = lo;
+    ends[1][b][lane] = hi;
+    __syncthreads();
+    const int b0 = b & ~(G / 32 - 1);
+#pragma unroll
+    for (int i = 0; i < G / 32; ++i) {
+      lo = fminf(lo, ends[0][b0 + i][lane]);
+      hi = fmaxf(hi, ends[1][b0 + i][lane]);
+    }
+  }
+  u16 s16 = 0, m16 = 0;
+  if (in && lo <= hi) {   // the group has rows
+    if (hi == INFINITY) {
+      s16 = 0x7fc0;
+    } else if (SHIFT) {
+      s16 = round_twice(((double)hi - (double)lo) / 15.0);
+      m16 = round_twice(0.5 * ((double)lo + (double)hi) + 0.5 * (double)bf2f(s16));
+    } else {
+      // the end that is further from 0 (the lower of two alike) becomes -8
+      s16 = f2bf(-0.125f * (hi > -lo ? hi : lo));
+    }
+  }
+  const float s = bf2f(s16), m = SHIFT ? bf2f(m16) : 0.f, inv = 1.f / s;
+  const float near = 1e-5f + fabsf(m * inv) * 0x1p-21f;
+  const bool some = s != 0.f && s == s;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    uint32_t d = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int v = some && 8 * j + i < rows ? quant_code(w[8 * j + i], s, m, inv, near) + 8 : 8;
+      d |= (uint32_t)v << (4 * (i & 1 ? 4 + i / 2 : i / 2));
+    }
+    dw[lane >> 4][j][b][lane & 15] = d;
+  }
+  constexpr int NS = kQB / G, W16 = NS * (SHIFT ? 2 : 1);
+  const int tile = blockIdx.x * 4 + (lane >> 4);
+  if (tile < q.T && (b & (G / 32 - 1)) == 0) {
+    u16* at = scale + (((size_t)tile * q.KB + kb) * 16 + (lane & 15)) * W16 + b / (G / 32) * (SHIFT ? 2 : 1);
+    at[0] = s16;
+    if (SHIFT) at[1] = m16;
+  }
+  __syncthreads();
+  const int t = threadIdx.x >> 6, j = lane >> 4, col = lane & 15;
+  if (blockIdx.x * 4 + t < q.T)
+    code[((size_t)(blockIdx.x * 4 + t) * q.KB + kb) * 64 + lane] =
+        make_uint4(dw[t][j][0][col], dw[t][j][1][col], dw[t][j][2][col], dw[t][j][3][col]);
+}
+
+// What in rows: the same split, a dword of eight rows at a time.
+template <class T, int G, bool SHIFT>
+__global__ void __launch_bounds__(256) k_quant_unpack(QuantNet q, T* W) {
+  const int lane = threadIdx.x & 63, b = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kb = blockIdx.y, c = blockIdx.x * 64 + lane, k0 = kb * kQB + 32 * b;
+  if (c >= q.C) return;
+  constexpr int W16 = kQB / G * (SHIFT ? 2 : 1);
+  const size_t block = (size_t)(c >> 4) * q.KB + kb;
+  const u16* at = q.scale + (block * 16 + (c & 15)) * W16 + b / (G / 32) * (SHIFT ? 2 : 1);
+  const float s = bf2f(at[0]), m = SHIFT ? bf2f(at[1]) : 0.f;
+  uint32_t d[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    d[j] = reinterpret_cast<const uint32_t*>(q.code + block * 64 + j * 16 + (c & 15))[b];
+#pragma unroll
+  for (int i = 0; i < 32; ++i) {
+    const int p = i & 1 ? 4 + i % 8 / 2 : i % 8 / 2;
+    if (k0 + i < q.H)
+      store_one(W + (size_t)(k0 + i) * q.C + c, fmaf((float)(d[i / 8] >> (4 * p) & 15u) - 8.f, s, m));
+  }
+}
+
+// Eight codes less 8 as halves, exact: 0x6400 | q is 1024 + q, 0x6400 | q << 4 is
+// 1024 + 16 q.  Nine instructions; the bound by memory leaves about 26 for them.
+__device__ __forceinline__ h8 halves(uint32_t w) {
+  const h2 a = {(_Float16)-1032.f, (_Float16)-1032.f}, f = {(_Float16)0.0625f, (_Float16)0.0625f},
+           g = {(_Float16)-72.f, (_Float16)-72.f};
+  auto at = [&](uint32_t mask) { return __builtin_bit_cast(h2, (w & mask) | 0x64006400u); };
+  const h2 v0 = at(0x000f000fu) + a, v1 = __builtin_elementwise_fma(at(0x00f000f0u), f, g);
+  w >>= 8;
+  const h2 v2 = at(0x000f000fu) + a, v3 = __builtin_elementwise_fma(at(0x00f000f0u), f, g);
+  return h8{v0.x, v0.y, v1.x, v1.y, v2.x, v2.y, v3.x, v3.y};
+}
+
+// The rows' side of the product.  x is scaled by a power of two for each row and
+// block of 128 columns, so that the block's largest finite value lies in 2^14 ..
+// 2^15 and a half holds what a bf16 has (values 2^-32 of the block's largest and
+// less lose bits, which is less than an fp32 sum keeps of them); an fp32 x is the
+// sum of two halves, 2^-24 of it away at most.  Products of halves and codes are
+// exact, their sums are fp32, and 2^-e times the group's scale brings them back.
+//   LDS: xh [KC][parts][4 b][4 j][R] of 16 bytes (row fastest), xs [KC][R16].
+struct QuantX {
+  const void* x;
+  int n, H, R, R16;   // rows of this workgroup: R kept, R16 padded to 16
+};
+
+template <class X>
+__device__ __forceinline__ void quant_stage(const X* __restrict__ x, int H, int rows, int R16, int kb0, int nkb,
+                                            uint4* xh, float* xs) {
+  constexpr int P = sizeof(X) == 4 ? 2 : 1;
+  const int units = rows * nkb * 16;   // eight columns each, sixteen lanes to a row's block
+  for (int u = threadIdx.x; u < units; u += blockDim.x) {
+    const int o = u & 15, rb = u >> 4, r = rb % rows, kb = rb / rows, k = (kb0 + kb) * kQB + 8 * o;
+    const X* p = x + (size_t)r * H + k;
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = k + i < H ? load_one(p + i) : 0.f;
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t a = __float_as_uint(v[i]) & 0x7fffffffu;
+      top = max(top, a < 0x7f800000u ? a : 0u);
+    }
+#pragma unroll
+    for (int d = 1; d < 16; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d, 16));
+    // 2^-126 at least: a block of subnormals keeps fewer bits, as they do
+    const int e = max((int)(top >> 23) - 127, -112), up = top ? 14 - e : 0;
+    uint32_t hi[4], lo[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      h2 h, l;
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        const float t = ldexpf(v[2 * i + z], up);
+        h[z] = (_Float16)t;
+        l[z] = fabsf(t) < INFINITY ? (_Float16)(t - (float)h[z]) : (_Float16)0.f;
+      }
+      hi[i] = __builtin_bit_cast(uint32_t, h);
+      lo[i] = __builtin_bit_cast(uint32_t, l);
+    }
+    // columns 8 o ..: dword b = o / 4 of lane group j = o % 4
+    uint4* at = xh + ((size_t)kb * P * 16 + o) * rows + r;
+    at[0] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+    if (P == 2) at[16 * rows] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    if (o == 0) xs[kb * R16 + r] = ldexpf(1.f, -up);
+  }
+}
+
+// y[rows, C] = x What + bias.  A workgroup of eight wavefronts has R rows of x (KC
+// blocks of them at a time) in LDS and goes through groups of tiles; S wavefronts
+// share a tile, each S-th block to one, and join their sums in LDS.  Each wavefront
+// keeps PF blocks of codes in flight, over the ends of tiles.
+constexpr int kQW = 8;
+constexpr size_t kQLds = 64 << 10;   // most LDS of a workgroup
+struct QuantJob {
+  QuantNet q;
+  const void* x;
+  const float* bias;
+  void* y;
+  int n, R, KC, S, groups, ybf;
+};
+
+template <class X, int RT, int G, bool SHIFT>
+__global__ void __launch_bounds__(64 * kQW) k_quant_product(QuantJob a) {
+  constexpr int P = sizeof(X) == 4 ? 2 : 1, NS = kQB / G, W16 = NS * (SHIFT ? 2 : 1), PF = 4, R16 = 16 * RT;
+  extern __shared__ uint4 lds[];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r0 = blockIdx.y * R16, rows = min(a.R, a.n - r0);
+  uint4* xh = lds;
+  float* xs = reinterpret_cast<float*>(lds + (size_t)a.KC * P * 16 * a.R);
+  const X* x = (const X*)a.x + (size_t)r0 * a.q.H;
+  const int KB = a.q.KB, T = a.q.T, S = a.S, ks = w % S, tw = w / S, per = kQW / S;
+  const int steps = (KB + S - 1) / S, cstep = a.KC / S;   // blocks of a wavefront: of a tile, of a chunk
+  const int mine = (a.groups - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x;   // groups of tiles
+  const int items = mine * steps;
+  struct Block {
+    uint4 c;
+    u16 s[W16];
+  } ring[PF];
+  int ls = 0, lg = 0;   // the next block to ask for; past the last one, it again
+  auto load = [&](Block& f) {
+    const int kb = min(ls * S + ks, KB - 1), t = min(((int)blockIdx.x + lg * (int)gridDim.x) * per + tw, T - 1);
+    const size_t block = (size_t)t * KB + kb;
+    f.c = a.q.code[block * 64 + lane];
+    const u16* s = a.q.scale + (block * 16 + (lane & 15)) * W16;
+    if constexpr (W16 == 1) f.s[0] = *s;
+    else __builtin_memcpy(f.s, __builtin_assume_aligned(s, 2 * W16), 2 * W16);
+    if (++ls == steps) {
+      ls = 0;
+      lg = min(lg + 1, mine - 1);
+    }
+  };
+#pragma unroll
+  for (int u = 0; u < PF; ++u) load(ring[u]);
+  int row[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) row[rt] = min(rt * 16 + (lane & 15), rows - 1);
+  v4f acc[RT] = {};
+  int step = 0, grp = 0;
+  for (int it0 = 0; it0 < items; it0 += PF) {
+#pragma unroll
+    for (int u = 0; u < PF; ++u) {
+      if (it0 + u >= items) break;
+      const int cs = step % cstep;   // step of the chunk
+      if (cs == 0 && (it0 + u == 0 || a.KC < KB)) {
+        if (it0 + u > 0) __syncthreads();   // the last chunk has been read
+        const int kb0 = step * S;
+        quant_stage<X>(x, a.q.H, rows, R16, kb0, min(a.KC, KB - kb0), xh, xs);
+        __syncthreads();
+      }
+      const int kb = step * S + ks;
+      if (kb < KB) {
+        const int kc = cs * S + ks;
+        const uint32_t d[4] = {ring[u].c.x, ring[u].c.y, ring[u].c.z, ring[u].c.w};
+        v4f blk[RT] = {};
+#pragma unroll
+        for (int g = 0; g < NS; ++g) {
+          v4f part[RT] = {}, sum[RT] = {};
+#pragma unroll
+          for (int b = g * (4 / NS); b < (g + 1) * (4 / NS); ++b) {
+            const h8 c8 = halves(d[b]);
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+              for (int rt = 0; rt < RT; ++rt) {
+                const uint4 f = xh[((size_t)(kc * P + p) * 16 + 4 * b + (lane >> 4)) * rows + row[rt]];
+                const h8 x8 = __builtin_bit_cast(h8, f);
+                part[rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x8, c8, part[rt], 0, 0, 0);
+                if (SHIFT) {   // the rows' sums, in every column
+                  const _Float16 o = (_Float16)1.f;
+                  sum[rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x8, h8{o, o, o, o, o, o, o, o}, sum[rt], 0, 0, 0);
+                }
+              }
+          }
+          const float s = bf2f(ring[u].s[g * (SHIFT ? 2 : 1)]), m = SHIFT ? bf2f(ring[u].s[2 * g + 1]) : 0.f;
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              blk[rt][i] = fmaf(s, part[rt][i], blk[rt][i]);
+              if (SHIFT) blk[rt][i] = fmaf(m, sum[rt][i], blk[rt][i]);
+            }
+        }
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          const float4 up = *reinterpret_cast<const float4*>(xs + kc * R16 + rt * 16 + 4 * (lane >> 4));
+          acc[rt][0] = fmaf(up.x, blk[rt][0], acc[rt][0]);
+          acc[rt][1] = fmaf(up.y, blk[rt][1], acc[rt][1]);
+          acc[rt][2] = fmaf(up.z, blk[rt][2], acc[rt][2]);
+          acc[rt][3] = fmaf(up.w, blk[rt][3], acc[rt][3]);
+        }
+      }
+      load(ring[u]);
+      if (++step < steps) continue;
+      // the tile is done
+      step = 0;
+      const int t = ((int)blockIdx.x + grp++ * (int)gridDim.x) * per + tw;
+      if (S > 1) {
+        float* red = xs + a.KC * R16;   // [kQW][RT * 4][64]
+        __syncthreads();
+        if (ks > 0)
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) red[(w * RT * 4 + rt * 4 + i) * 64 + lane] = acc[rt][i];
+        __syncthreads();
+        if (ks == 0)
+          for (int o = 1; o < S; ++o)
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) acc[rt][i] += red[((w + o) * RT * 4 + rt * 4 + i) * 64 + lane];
+      }
+      const int c = t * 16 + (lane & 15);
+      if (ks == 0 && t < T && c < a.q.C) {
+        const float bias = a.bias ? a.bias[c] : 0.f;
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int r = rt * 16 + 4 * (lane >> 4) + i;
+            const size_t at = (size_t)(r0 + r) * a.q.C + c;
+            if (r < rows) a.ybf ? store_one((u16*)a.y + at, acc[rt][i] + bias) : store_one((float*)a.y + at, acc[rt][i] + bias);
+          }
+      }
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) acc[rt] = v4f{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+}
+
+cavs_status quant_args(cavs_ctx* ctx, const cavs_quant* q) {
+  if (!q) return fail(ctx, CAVS_ERR_ARG, "null weights");
+  if (q->H <= 0 || q->C <= 0) return fail(ctx, CAVS_ERR_ARG, "bad H/C");
+  if (q->group != 32 && q->group != 64 && q->group != 128)
+    return fail(ctx, CAVS_ERR_ARG, "group=%d: 32, 64 or 128", q->group);
+  if (q->shift != 0 && q->shift != 1) return fail(ctx, CAVS_ERR_ARG, "shift=%d: 0 or 1", q->shift);
+  if (q->H > kQuantMaxH || q->C > kQuantMaxC)
+    return fail(ctx, CAVS_ERR_UNSUPPORTED, "H=%d, C=%d: at most %d, %d", q->H, q->C, kQuantMaxH, kQuantMaxC);
+  return CAVS_OK;
+}
+
+size_t code_bytes(const cavs_quant* q) {
+  return (size_t)cdiv(q->C, 16) * cdiv(q->H, kQB) * 1024;
+}
+
+QuantNet quant_net(const cavs_quant* q, const void* data) {
+  QuantNet n{q->H, q->C, cdiv(q->C, 16), cdiv(q->H, kQB), (const uint4*)data,
+             (const u16*)((const char*)data + code_bytes(q))};
+  return n;
+}
+
+cavs_status quant_data(cavs_ctx* ctx, const void* data) {
+  if (!data) return fail(ctx, CAVS_ERR_ARG, "data is required");
+  if (((uintptr_t)data & 15) != 0) return fail(ctx, CAVS_ERR_ARG, "data must be aligned to 16 bytes");
+  return CAVS_OK;
+}
+
+cavs_status quant_type(cavs_ctx* ctx, int type, const void* p, const char* name) {
+  if (type != CAVS_T_F32 && type != CAVS_T_BF16) return fail(ctx, CAVS_ERR_ARG, "unknown element type");
+  if (!p) return fail(ctx, CAVS_ERR_ARG, "%s is required", name);
+  if (((uintptr_t)p & (type == CAVS_T_BF16 ? 1 : 3)) != 0)
+    return fail(ctx, CAVS_ERR_ARG, "%s is not aligned to its elements", name);
+  return CAVS_OK;
+}
+
+template <class F>
+void by_group(const cavs_quant* q, F f) {
+  auto g = [&](auto shift) {
+    if (q->group == 32) f(std::integral_constant<int, 32>{}, shift);
+    else if (q->group == 64) f(std::integral_constant<int, 64>{}, shift);
+    else f(std::integral_constant<int, 128>{}, shift);
+  };
+  q->shift ? g(std::true_type{}) : g(std::false_type{});
+}
+
+template <class F>
+void by_element(int type, F f) {
+  type == CAVS_T_BF16 ? f(u16{}) : f(float{});
+}
+
+}  // namespace
+
+size_t quant_bytes(const cavs_quant* q) {
+  if (quant_args(nullptr, q) != CAVS_OK) return 0;
+  const size_t blocks = (size_t)cdiv(q->C, 16) * cdiv(q->H, kQB);
+  return code_bytes(q) + blocks * 16 * (kQB / q->group) * (q->shift ? 4 : 2);
+}
+
+cavs_status quant_pack_run(cavs_ctx* ctx, const cavs_quant* q, int w_type, const void* W, void* data) {
+  cavs_status st = quant_args(ctx, q);
+  if (st == CAVS_OK) st = quant_type(ctx, w_type, W, "W");
+  if (st == CAVS_OK) st = quant_data(ctx, data);
+  if (st != CAVS_OK) return st;
+  const QuantNet n = quant_net(q, data);
+  by_group(q, [&](auto g, auto shift) {
+    by_element(w_type, [&](auto t) {
+      using T = decltype(t);
+      CAVS_LAUNCH("k_quant_pack", (k_quant_pack<T, g(), shift()>), dim3(cdiv(n.T, 4), n.KB), dim3(256), 0,
+                  ctx->stream, n, (const T*)W, (uint4*)data, (u16*)((char*)data + code_bytes(q)));
+    });
+  });
+  CAVS_LAUNCH_CHECK(ctx);
+  return CAVS_OK;
+}
+
+cavs_status quant_unpack_run(cavs_ctx* ctx, const cavs_quant* q, int w_type, void* W) {
+  cavs_status st = quant_args(ctx, q);
+  if (st == CAVS_OK) st = quant_type(ctx, w_type, W, "W");
+  if (st == CAVS_OK) st = quant_data(ctx, q->data);
+  if (st != CAVS_OK) return st;
+  const QuantNet n = quant_net(q, q->data);
+  by_group(q, [&](auto g, auto shift) {
+    by_element(w_type, [&](auto t) {
+      using T = decltype(t);
+      CAVS_LAUNCH("k_quant_unpack", (k_quant_unpack<T, g(), shift()>), dim3(cdiv(n.T, 4), n.KB), dim3(256), 0,
+                  ctx->stream, n, (T*)W);
+    });
+  });
+  CAVS_LAUNCH_CHECK(ctx);
+  return CAVS_OK;
+}
+
+cavs_status quant_product_run(cavs_ctx* ctx, const cavs_quant* q, int x_type, const void* x, int n,
+                              const float* bias, int y_type, void* y) {
+  cavs_status st = quant_args(ctx, q);
+  if (st != CAVS_OK) return st;
+  if (n < 0) return fail(ctx, CAVS_ERR_ARG, "bad n");
+  if (n > kQuantMaxN) return fail(ctx, CAVS_ERR_UNSUPPORTED, "n=%d: at most %d", n, kQuantMaxN);
+  if ((x_type != CAVS_T_F32 && x_type != CAVS_T_BF16) || (y_type != CAVS_T_F32 && y_type != CAVS_T_BF16))
+    return fail(ctx, CAVS_ERR_ARG, "unknown element type");
+  if (n == 0) return CAVS_OK;
+  st = quant_type(ctx, x_type, x, "x");
+  if (st == CAVS_OK) st = quant_type(ctx, y_type, y, "y");
+  if (st == CAVS_OK) st = quant_data(ctx, q->data);
+  if (st != CAVS_OK) return st;
+  if (((uintptr_t)bias & 3) != 0) return fail(ctx, CAVS_ERR_ARG, "bias is not aligned to its elements");
+  QuantJob a{quant_net(q, q->data), x, bias, y, n};
+  a.ybf = y_type == CAVS_T_BF16;
+  const int P = x_type == CAVS_T_F32 ? 2 : 1, T = a.q.T, KB = a.q.KB;
+  // rows of a workgroup, and wavefronts of a tile: as many as leave each of 2048
+  // wavefronts something to do, then fewer rows
+  int rt = n <= 16 ? 1 : n <= 32 ? 2 : 4, rows;
+  size_t block, red;
+  for (;; rt /= 2) {
+    rows = cdiv(n, 16 * rt);
+    a.R = std::min(n, 16 * rt);
+    block = (size_t)P * 256 * a.R + 64 * rt;
+    red = (size_t)kQW * rt * 1024;
+    a.S = 1;
+    while (a.S < kQW && a.S < KB && (long)T * a.S * rows < 2048 && 2 * a.S * block + red <= kQLds) a.S *= 2;
+    if (rt == 1 || (long)T * a.S * rows >= 2048) break;
+  }
+  if (a.S == 1) red = 0;
+  a.KC = std::min(cdiv(KB, a.S), (int)((kQLds - red) / block) / a.S) * a.S;
+  a.groups = cdiv(T, kQW / a.S);
+  const size_t shmem = a.KC * block + red;
+  const dim3 grid(std::min(a.groups, std::max(1, cdiv(512, rows))), rows);
+  by_group(q, [&](auto g, auto shift) {
+    by_element(x_type, [&](auto t) {
+      using X = decltype(t);
+      auto launch = [&](auto R) {
+        CAVS_LAUNCH("k_quant_product", (k_quant_product<X, R(), g(), shift()>), grid, dim3(64 * kQW), shmem,
+                    ctx->stream, a);
+      };
+      if (rt == 1) launch(std::integral_constant<int, 1>{});
+      else if (rt == 2) launch(std::integral_constant<int, 2>{});
+      else launch(std::integral_constant<int, 4>{});
+    });
+  });
+  CAVS_LAUNCH_CHECK(ctx);
+  return CAVS_OK;
+}
+
+}  // namespace cavs

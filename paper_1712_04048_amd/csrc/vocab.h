@@ -479,4 +479,21 @@ size_t vocab_ws_bytes(const cavs_vocab* p, bool train);
 cavs_status vocab_run(cavs_ctx* ctx, const cavs_vocab* p, float* loss, float* row_loss, void* dh,
                       void* dWs, float* dbs, void* ws, size_t ws_bytes, bool train);
 
+// quant.hip
+size_t quant_bytes(const cavs_quant* q);
+cavs_status quant_pack_run(cavs_ctx* ctx, const cavs_quant* q, int w_type, const void* W, void* data);
+cavs_status quant_unpack_run(cavs_ctx* ctx, const cavs_quant* q, int w_type, void* W);
+cavs_status quant_product_run(cavs_ctx* ctx, const cavs_quant* q, int x_type, const void* x, int n,
+                              const float* bias, int y_type, void* y);
+
+// rules.hip
+size_t adjust_ws_bytes(int n, int C);
+cavs_status adjust_run(cavs_ctx* ctx, const cavs_rules* r, const void* z, void* out, int* best, float* lse,
+                       void* ws, size_t ws_bytes);
+
+// clip.hip
+size_t clip_ws_bytes();
+cavs_status clip_run(cavs_ctx* ctx, const cavs_grad* grads, int count, float scale, float max_norm, float* norm,
+                     void* ws, size_t ws_bytes);
+
 }  // namespace cavs

@@ -136,11 +136,13 @@ class LmBatch(Batch):
     state is scored over the vocabulary by cavs_vocab_grad, which keeps no
     logits.  The workload's X is not used; its Ws, bs and push_idx are the head
     and the labels.  ``teacher``: (words [V, K], logits [V, K], alpha, temp) of a
-    model to learn from; ``head_dtype``: the type of the head's weights."""
+    model to learn from; ``head_dtype``: the type of the head's weights;
+    ``max_norm``: backward ends with cavs_clip_grads over the parameters'
+    gradients (dX, an input's, is no part of it), and ``norm`` holds their norm."""
 
     def __init__(self, wl: Workload, table: torch.Tensor, words, ctx: Optional[B.Context] = None,
                  device: int = 0, scale: float = 1.0, teacher=None,
-                 head_dtype: torch.dtype = torch.float32):
+                 head_dtype: torch.dtype = torch.float32, max_norm: Optional[float] = None):
         super().__init__(wl, ctx, device)
         p, dev = self.params, self.dev
         self.emb = B.Embedding(table, scale)
@@ -154,6 +156,8 @@ class LmBatch(Batch):
                                None, None)
         self.teacher = teacher
         self.head: Optional[B.VocabHead] = None
+        self.max_norm = max_norm
+        self.quant: Optional[B.QuantWeights] = None
 
     def alloc(self):
         super().alloc()
@@ -175,6 +179,10 @@ class LmBatch(Batch):
         u8 = dict(dtype=torch.uint8, device=dev)
         self.ws_head = torch.empty(max(1, B.vocab_workspace_bytes(self.head, True)), **u8)
         self.ws_emb = torch.empty(max(1, B.embed_grad_workspace_bytes(self.emb, wl.n_x)), **u8)
+        if self.max_norm is not None:
+            self.norm = torch.empty(1, dtype=torch.float32, device=dev)
+            self.ws_clip = torch.empty(B.clip_workspace_bytes(), **u8)
+            self.clip = B.GradList([g for k, g in self.grads.items() if k != "dX"])
 
     def forward(self):
         B.embed(self.ctx, self.emb, self.words, self.X)
@@ -187,13 +195,47 @@ class LmBatch(Batch):
     def backward(self):
         super().backward()
         B.embed_grad(self.ctx, self.emb, self.words, self.grads["dX"], self.grads["dE"], self.ws_emb)
+        if self.max_norm is not None:
+            B.clip_grads(self.ctx, self.clip, self.max_norm, self.norm, self.ws_clip)
 
-    def infer(self):
-        """The states and the loss alone (cavs_infer, cavs_vocab_loss)."""
+    def _states(self):
         B.embed(self.ctx, self.emb, self.words, self.X)
         if self.ws_infer is None:
             n = B.infer_workspace_bytes(self.params, self.sched)
             self.ws_infer = torch.empty(max(n, 1), dtype=torch.uint8, device=self.dev)
         B.infer(self.ctx, self.params, self.sched, self.X, None, self.ws_infer, self.h, self.c,
                 self.no_loss)
+
+    def infer(self):
+        """The states and the loss alone (cavs_infer, cavs_vocab_loss)."""
+        self._states()
         B.vocab_loss(self.ctx, self.head, self.loss, self.row_loss, self.ws_head)
+
+    def quantise(self, group: int = 128, shift: bool = False):
+        """The head in 4 bits, which next_words scores with (cavs_quant_pack)."""
+        H, C = self.Ws.shape
+        data = torch.empty(B.quant_bytes(H, C, group, shift), dtype=torch.uint8, device=self.dev)
+        self.quant = B.QuantWeights(data, H, C, group, shift)
+        B.quant_pack(self.ctx, self.quant, self.Ws)
+
+    def next_words(self, vertices: torch.Tensor, rules: Optional[B.LogitRules] = None) -> torch.Tensor:
+        """The likeliest word at each of ``vertices`` (int32 [n], on the device: the
+        last ones of the sequences, as a rule) under the rules, -1 where they allow
+        none: the states, their rows, the head in 4 bits, the rules.  ``logits``
+        [n, C] and ``lse`` [n] hold what the words were taken from."""
+        n, C, dev = int(vertices.shape[0]), int(self.Ws.shape[1]), self.dev
+        if self.quant is None:
+            self.quantise()
+        if getattr(self, "best", None) is None or self.best.shape[0] != n:
+            self.rows = torch.empty(n, self.wl.H, dtype=torch.float32, device=dev)
+            self.logits = torch.empty(n, C, dtype=torch.float32, device=dev)
+            self.best = torch.empty(n, dtype=torch.int32, device=dev)
+            self.lse = torch.empty(n, dtype=torch.float32, device=dev)
+            self.ws_rules = torch.empty(max(1, B.adjust_workspace_bytes(n, C)), dtype=torch.uint8, device=dev)
+        # kept, as the context's stream may read them after the call
+        self.vertices, self.rules = vertices, rules if rules is not None else B.LogitRules()
+        self._states()
+        B.embed(self.ctx, B.Embedding(self.h), self.vertices, self.rows)
+        B.quant_product(self.ctx, self.quant, self.rows, self.logits, bias=self.bs)
+        B.adjust_logits(self.ctx, self.rules, self.logits, self.logits, self.best, self.lse, self.ws_rules)
+        return self.best
