@@ -154,69 +154,109 @@ __global__ void __launch_bounds__(256) k_quant_unpack(QuantNet q, T* W) {
   }
 }
 
-// Eight codes less 8 as halves, exact: 0x6400 | q is 1024 + q, 0x6400 | q << 4 is
-// 1024 + 16 q.  Nine instructions; the bound by memory leaves about 26 for them.
+// Eight codes q as halves.  A half with an exponent of 0 is its mantissa times
+// 2^-24, so q's bits in place are q 2^-24, four places up 2^-20 q: five
+// instructions, where the bound by memory leaves about 26 for eight weights.  The
+// matrix instruction takes such halves as they are; the rows' side makes up for the
+// factor of 16 (adjacent pairs of columns, in turn) and for the 2^-24.
 __device__ __forceinline__ h8 halves(uint32_t w) {
-  const h2 a = {(_Float16)-1032.f, (_Float16)-1032.f}, f = {(_Float16)0.0625f, (_Float16)0.0625f},
-           g = {(_Float16)-72.f, (_Float16)-72.f};
-  auto at = [&](uint32_t mask) { return __builtin_bit_cast(h2, (w & mask) | 0x64006400u); };
-  const h2 v0 = at(0x000f000fu) + a, v1 = __builtin_elementwise_fma(at(0x00f000f0u), f, g);
-  w >>= 8;
-  const h2 v2 = at(0x000f000fu) + a, v3 = __builtin_elementwise_fma(at(0x00f000f0u), f, g);
-  return h8{v0.x, v0.y, v1.x, v1.y, v2.x, v2.y, v3.x, v3.y};
+  const uint32_t v = w >> 8;
+  return __builtin_bit_cast(h8, make_uint4(w & 0x000f000fu, w & 0x00f000f0u, v & 0x000f000fu, v & 0x00f000f0u));
 }
 
-// The rows' side of the product.  x is scaled by a power of two for each row and
-// block of 128 columns, so that the block's largest finite value lies in 2^14 ..
-// 2^15 and a half holds what a bf16 has (values 2^-32 of the block's largest and
-// less lose bits, which is less than an fp32 sum keeps of them); an fp32 x is the
-// sum of two halves, 2^-24 of it away at most.  Products of halves and codes are
-// exact, their sums are fp32, and 2^-e times the group's scale brings them back.
-//   LDS: xh [KC][parts][4 b][4 j][R] of 16 bytes (row fastest), xs [KC][R16].
-struct QuantX {
-  const void* x;
-  int n, H, R, R16;   // rows of this workgroup: R kept, R16 padded to 16
-};
+// The rows' side of the product.  With f = s 2^12 and X the sum of a group's x,
+//   sum x What = sum over groups of s (sum x q) + (m - 8 s) X.
+// x is scaled by a power of two 2^up for each row and block of 128 columns, so that
+// the block's largest finite value lies in 2^14 .. 2^15 (and every other pair of
+// columns by 1/16): a half then holds what a bf16 has (values 2^-28 of the block's
+// largest and less lose bits, which is less than an fp32 sum keeps of them); an fp32
+// x is the sum of two halves, 2^-24 of it away at most, or 2^-35 of the block's
+// largest.  Products of halves and codes are exact, their sums are fp32.  The sums
+// over blocks are kept times 2^-12, which takes half of the 2^-24 (rows near either
+// end of fp32 stay inside it) and is made up for at the end.
+//   LDS: xh [KC][parts][4 b][4 j][rows] of 16 bytes, xs [KC][R16] = 2^(12 - up),
+//   xg [KC][groups][R16] = 2^-12 X.
+constexpr float kQDown = 0x1p-12f;
 
 template <class X>
+__device__ __forceinline__ void quant_load8(const X* __restrict__ x, int H, int k, float (&v)[8]) {
+  if (k + 8 <= H) {   // at any address that is aligned to its elements
+    if constexpr (sizeof(X) == 4) {
+      typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
+      const f4 a = *reinterpret_cast<const f4*>(x + k), b = *reinterpret_cast<const f4*>(x + k + 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+    } else {
+      typedef u16 s8 __attribute__((ext_vector_type(8), aligned(2)));
+      const s8 a = *reinterpret_cast<const s8*>(x + k);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = bf2f(a[i]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = k + i < H ? load_one(x + k + i) : 0.f;
+  }
+}
+
+template <class X, int G>
+__device__ __forceinline__ void quant_put(const float (&v)[8], int o, int r, int kb, int rows, int R16, uint4* xh,
+                                          float* xs, float* xg) {
+  constexpr int P = sizeof(X) == 4 ? 2 : 1, NS = kQB / G;
+  uint32_t top = 0;
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t a = __float_as_uint(v[i]) & 0x7fffffffu;
+    top = max(top, a < 0x7f800000u ? a : 0u);
+    sum += v[i] * kQDown;
+  }
+#pragma unroll
+  for (int d = 1; d < 16; d <<= 1) {
+    top = max(top, (uint32_t)__shfl_xor((int)top, d, 16));
+    if (d * 8 < G) sum += __shfl_xor(sum, d, 16);
+  }
+  // a block of values below 2^-112 keeps fewer bits
+  const int e = max((int)(top >> 23) - 127, -112), up = top ? 14 - e : 0;
+  uint32_t hi[4], lo[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    h2 h, l;
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+      const float t = ldexpf(v[2 * i + z], up - (i & 1 ? 4 : 0));
+      h[z] = (_Float16)t;
+      l[z] = fabsf(t) < INFINITY ? (_Float16)(t - (float)h[z]) : (_Float16)0.f;
+    }
+    hi[i] = __builtin_bit_cast(uint32_t, h);
+    lo[i] = __builtin_bit_cast(uint32_t, l);
+  }
+  // columns 8 o ..: dword b = o / 4 of lane group j = o % 4
+  uint4* at = xh + ((size_t)kb * P * 16 + o) * rows + r;
+  at[0] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+  if (P == 2) at[16 * rows] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+  if (o == 0) xs[kb * R16 + r] = ldexpf(1.f, 12 - up);
+  if (o % (G / 8) == 0) xg[(kb * NS + o / (G / 8)) * R16 + r] = sum;
+}
+
+// Blocks kb0 .. kb0 + nkb of all rows; a row's block to sixteen lanes, eight columns
+// each, two such blocks in flight.
+template <class X, int G>
 __device__ __forceinline__ void quant_stage(const X* __restrict__ x, int H, int rows, int R16, int kb0, int nkb,
-                                            uint4* xh, float* xs) {
-  constexpr int P = sizeof(X) == 4 ? 2 : 1;
-  const int units = rows * nkb * 16;   // eight columns each, sixteen lanes to a row's block
-  for (int u = threadIdx.x; u < units; u += blockDim.x) {
-    const int o = u & 15, rb = u >> 4, r = rb % rows, kb = rb / rows, k = (kb0 + kb) * kQB + 8 * o;
-    const X* p = x + (size_t)r * H + k;
-    float v[8];
+                                            uint4* xh, float* xs, float* xg) {
+  const int units = rows * nkb * 16, step = blockDim.x;
+  for (int u = threadIdx.x; u < units; u += 2 * step) {
+    float v[2][8];
+    int r[2], kb[2];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = k + i < H ? load_one(p + i) : 0.f;
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t a = __float_as_uint(v[i]) & 0x7fffffffu;
-      top = max(top, a < 0x7f800000u ? a : 0u);
+    for (int z = 0; z < 2; ++z) {
+      const int rb = min(u + z * step, units - 1) >> 4;
+      kb[z] = rb / rows;
+      r[z] = rb - kb[z] * rows;
+      quant_load8(x + (size_t)r[z] * H, H, (kb0 + kb[z]) * kQB + 8 * (u & 15), v[z]);
     }
 #pragma unroll
-    for (int d = 1; d < 16; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d, 16));
-    // 2^-126 at least: a block of subnormals keeps fewer bits, as they do
-    const int e = max((int)(top >> 23) - 127, -112), up = top ? 14 - e : 0;
-    uint32_t hi[4], lo[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      h2 h, l;
-#pragma unroll
-      for (int z = 0; z < 2; ++z) {
-        const float t = ldexpf(v[2 * i + z], up);
-        h[z] = (_Float16)t;
-        l[z] = fabsf(t) < INFINITY ? (_Float16)(t - (float)h[z]) : (_Float16)0.f;
-      }
-      hi[i] = __builtin_bit_cast(uint32_t, h);
-      lo[i] = __builtin_bit_cast(uint32_t, l);
-    }
-    // columns 8 o ..: dword b = o / 4 of lane group j = o % 4
-    uint4* at = xh + ((size_t)kb * P * 16 + o) * rows + r;
-    at[0] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-    if (P == 2) at[16 * rows] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-    if (o == 0) xs[kb * R16 + r] = ldexpf(1.f, -up);
+    for (int z = 0; z < 2; ++z)
+      if (u + z * step < units) quant_put<X, G>(v[z], u & 15, r[z], kb[z], rows, R16, xh, xs, xg);
   }
 }
 
@@ -225,7 +265,7 @@ __device__ __forceinline__ void quant_stage(const X* __restrict__ x, int H, int 
 // share a tile, each S-th block to one, and join their sums in LDS.  Each wavefront
 // keeps PF blocks of codes in flight, over the ends of tiles.
 constexpr int kQW = 8;
-constexpr size_t kQLds = 64 << 10;   // most LDS of a workgroup
+constexpr size_t kQLds = 80 << 10;   // most LDS of a workgroup: two to a CU
 struct QuantJob {
   QuantNet q;
   const void* x;
@@ -242,6 +282,8 @@ __global__ void __launch_bounds__(64 * kQW) k_quant_product(QuantJob a) {
   const int r0 = blockIdx.y * R16, rows = min(a.R, a.n - r0);
   uint4* xh = lds;
   float* xs = reinterpret_cast<float*>(lds + (size_t)a.KC * P * 16 * a.R);
+  float* xg = xs + a.KC * R16;
+  float* red = xg + a.KC * NS * R16;   // [kQW][RT * 4][64]
   const X* x = (const X*)a.x + (size_t)r0 * a.q.H;
   const int KB = a.q.KB, T = a.q.T, S = a.S, ks = w % S, tw = w / S, per = kQW / S;
   const int steps = (KB + S - 1) / S, cstep = a.KC / S;   // blocks of a wavefront: of a tile, of a chunk
@@ -266,71 +308,67 @@ __global__ void __launch_bounds__(64 * kQW) k_quant_product(QuantJob a) {
   };
 #pragma unroll
   for (int u = 0; u < PF; ++u) load(ring[u]);
-  int row[RT];
+  // this lane's place in a dword's fragment of each 16 rows
+  const uint4* frag[RT];
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt) row[rt] = min(rt * 16 + (lane & 15), rows - 1);
+  for (int rt = 0; rt < RT; ++rt) frag[rt] = xh + (lane >> 4) * rows + min(rt * 16 + (lane & 15), rows - 1);
+  const int up = 4 * (lane >> 4);   // this lane's rows of the sums
   v4f acc[RT] = {};
-  int step = 0, grp = 0;
+  int step = 0, cs = 0, grp = 0;
   for (int it0 = 0; it0 < items; it0 += PF) {
 #pragma unroll
     for (int u = 0; u < PF; ++u) {
       if (it0 + u >= items) break;
-      const int cs = step % cstep;   // step of the chunk
       if (cs == 0 && (it0 + u == 0 || a.KC < KB)) {
         if (it0 + u > 0) __syncthreads();   // the last chunk has been read
         const int kb0 = step * S;
-        quant_stage<X>(x, a.q.H, rows, R16, kb0, min(a.KC, KB - kb0), xh, xs);
+        quant_stage<X, G>(x, a.q.H, rows, R16, kb0, min(a.KC, KB - kb0), xh, xs, xg);
         __syncthreads();
       }
-      const int kb = step * S + ks;
-      if (kb < KB) {
+      if (step * S + ks < KB) {
         const int kc = cs * S + ks;
         const uint32_t d[4] = {ring[u].c.x, ring[u].c.y, ring[u].c.z, ring[u].c.w};
-        v4f blk[RT] = {};
+        v4f blk[RT];
 #pragma unroll
         for (int g = 0; g < NS; ++g) {
-          v4f part[RT] = {}, sum[RT] = {};
+          v4f part[RT] = {};
 #pragma unroll
           for (int b = g * (4 / NS); b < (g + 1) * (4 / NS); ++b) {
             const h8 c8 = halves(d[b]);
 #pragma unroll
             for (int p = 0; p < P; ++p)
 #pragma unroll
-              for (int rt = 0; rt < RT; ++rt) {
-                const uint4 f = xh[((size_t)(kc * P + p) * 16 + 4 * b + (lane >> 4)) * rows + row[rt]];
-                const h8 x8 = __builtin_bit_cast(h8, f);
-                part[rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x8, c8, part[rt], 0, 0, 0);
-                if (SHIFT) {   // the rows' sums, in every column
-                  const _Float16 o = (_Float16)1.f;
-                  sum[rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x8, h8{o, o, o, o, o, o, o, o}, sum[rt], 0, 0, 0);
-                }
-              }
+              for (int rt = 0; rt < RT; ++rt)
+                part[rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+                    __builtin_bit_cast(h8, frag[rt][((kc * P + p) * 4 + b) * 4 * rows]), c8, part[rt], 0, 0, 0);
           }
-          const float s = bf2f(ring[u].s[g * (SHIFT ? 2 : 1)]), m = SHIFT ? bf2f(ring[u].s[2 * g + 1]) : 0.f;
+          const float s = bf2f(ring[u].s[g * (SHIFT ? 2 : 1)]);
+          const float t = SHIFT ? fmaf(-8.f, s, bf2f(ring[u].s[2 * g + 1])) : -8.f * s;
 #pragma unroll
-          for (int rt = 0; rt < RT; ++rt)
+          for (int rt = 0; rt < RT; ++rt) {
+            const float4 X4 = *reinterpret_cast<const float4*>(xg + (kc * NS + g) * R16 + rt * 16 + up);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              blk[rt][i] = fmaf(s, part[rt][i], blk[rt][i]);
-              if (SHIFT) blk[rt][i] = fmaf(m, sum[rt][i], blk[rt][i]);
+              blk[rt][i] = g ? fmaf(s, part[rt][i], blk[rt][i]) : s * part[rt][i];
+              acc[rt][i] = fmaf(t, i == 0 ? X4.x : i == 1 ? X4.y : i == 2 ? X4.z : X4.w, acc[rt][i]);
             }
+          }
         }
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-          const float4 up = *reinterpret_cast<const float4*>(xs + kc * R16 + rt * 16 + 4 * (lane >> 4));
-          acc[rt][0] = fmaf(up.x, blk[rt][0], acc[rt][0]);
-          acc[rt][1] = fmaf(up.y, blk[rt][1], acc[rt][1]);
-          acc[rt][2] = fmaf(up.z, blk[rt][2], acc[rt][2]);
-          acc[rt][3] = fmaf(up.w, blk[rt][3], acc[rt][3]);
+          const float4 f = *reinterpret_cast<const float4*>(xs + kc * R16 + rt * 16 + up);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            acc[rt][i] = fmaf(i == 0 ? f.x : i == 1 ? f.y : i == 2 ? f.z : f.w, blk[rt][i], acc[rt][i]);
         }
       }
       load(ring[u]);
+      if (++cs == cstep) cs = 0;
       if (++step < steps) continue;
       // the tile is done
-      step = 0;
+      step = cs = 0;
       const int t = ((int)blockIdx.x + grp++ * (int)gridDim.x) * per + tw;
       if (S > 1) {
-        float* red = xs + a.KC * R16;   // [kQW][RT * 4][64]
         __syncthreads();
         if (ks > 0)
 #pragma unroll
@@ -352,9 +390,10 @@ __global__ void __launch_bounds__(64 * kQW) k_quant_product(QuantJob a) {
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int r = rt * 16 + 4 * (lane >> 4) + i;
+            const int r = rt * 16 + up + i;
             const size_t at = (size_t)(r0 + r) * a.q.C + c;
-            if (r < rows) a.ybf ? store_one((u16*)a.y + at, acc[rt][i] + bias) : store_one((float*)a.y + at, acc[rt][i] + bias);
+            const float v = fmaf(acc[rt][i], 1.f / kQDown, bias);
+            if (r < rows) a.ybf ? store_one((u16*)a.y + at, v) : store_one((float*)a.y + at, v);
           }
       }
 #pragma unroll
@@ -479,7 +518,7 @@ cavs_status quant_product_run(cavs_ctx* ctx, const cavs_quant* q, int x_type, co
   for (;; rt /= 2) {
     rows = cdiv(n, 16 * rt);
     a.R = std::min(n, 16 * rt);
-    block = (size_t)P * 256 * a.R + 64 * rt;
+    block = (size_t)P * 256 * a.R + 64 * rt * (1 + kQB / q->group);
     red = (size_t)kQW * rt * 1024;
     a.S = 1;
     while (a.S < kQW && a.S < KB && (long)T * a.S * rows < 2048 && 2 * a.S * block + red <= kQLds) a.S *= 2;
@@ -494,6 +533,9 @@ cavs_status quant_product_run(cavs_ctx* ctx, const cavs_quant* q, int x_type, co
     by_element(x_type, [&](auto t) {
       using X = decltype(t);
       auto launch = [&](auto R) {
+        if (shmem > 64 << 10)
+          (void)hipFuncSetAttribute((const void*)k_quant_product<X, R(), g(), shift()>,
+                                    hipFuncAttributeMaxDynamicSharedMemorySize, (int)shmem);
         CAVS_LAUNCH("k_quant_product", (k_quant_product<X, R(), g(), shift()>), grid, dim3(64 * kQW), shmem,
                     ctx->stream, a);
       };
