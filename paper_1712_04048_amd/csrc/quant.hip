@@ -20,6 +20,9 @@ namespace {
 
 constexpr int kQuantMaxH = 1 << 15, kQuantMaxC = 1 << 20, kQuantMaxN = 1 << 20;
 constexpr int kQB = 128;   // rows of W in a block
+constexpr int kQR = 16;    // rows of x of a workgroup, at most
+constexpr int kQW = 16;    // wavefronts of a workgroup
+constexpr size_t kQLds = 152 << 10;   // most LDS of a workgroup
 
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
@@ -164,8 +167,8 @@ __device__ __forceinline__ h8 halves(uint32_t w) {
   return __builtin_bit_cast(h8, make_uint4(w & 0x000f000fu, w & 0x00f000f0u, v & 0x000f000fu, v & 0x00f000f0u));
 }
 
-// The rows' side of the product.  With f = s 2^12 and X the sum of a group's x,
-//   sum x What = sum over groups of s (sum x q) + (m - 8 s) X.
+// The rows' side of the product.  With X the sum of a group's x,
+//   sum x What = sum over groups of s (sum x q - 8 X) + m X.
 // x is scaled by a power of two 2^up for each row and block of 128 columns, so that
 // the block's largest finite value lies in 2^14 .. 2^15 (and every other pair of
 // columns by 1/16): a half then holds what a bf16 has (values 2^-28 of the block's
@@ -174,8 +177,8 @@ __device__ __forceinline__ h8 halves(uint32_t w) {
 // largest.  Products of halves and codes are exact, their sums are fp32.  The sums
 // over blocks are kept times 2^-12, which takes half of the 2^-24 (rows near either
 // end of fp32 stay inside it) and is made up for at the end.
-//   LDS: xh [KC][parts][4 b][4 j][rows] of 16 bytes, xs [KC][R16] = 2^(12 - up),
-//   xg [KC][groups][R16] = 2^-12 X.
+//   LDS: xh [KC][parts][4 b][4 j][rows] of 16 bytes, xs [KC][16] = 2^(12 - up),
+//   xg [KC][groups][16] = 2^-12 X.
 constexpr float kQDown = 0x1p-12f;
 
 template <class X>
@@ -199,8 +202,8 @@ __device__ __forceinline__ void quant_load8(const X* __restrict__ x, int H, int 
 }
 
 template <class X, int G>
-__device__ __forceinline__ void quant_put(const float (&v)[8], int o, int r, int kb, int rows, int R16, uint4* xh,
-                                          float* xs, float* xg) {
+__device__ __forceinline__ void quant_put(const float (&v)[8], int o, int r, int kb, int rows, uint4* xh, float* xs,
+                                          float* xg) {
   constexpr int P = sizeof(X) == 4 ? 2 : 1, NS = kQB / G;
   uint32_t top = 0;
   float sum = 0.f;
@@ -234,15 +237,15 @@ __device__ __forceinline__ void quant_put(const float (&v)[8], int o, int r, int
   uint4* at = xh + ((size_t)kb * P * 16 + o) * rows + r;
   at[0] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
   if (P == 2) at[16 * rows] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-  if (o == 0) xs[kb * R16 + r] = ldexpf(1.f, 12 - up);
-  if (o % (G / 8) == 0) xg[(kb * NS + o / (G / 8)) * R16 + r] = sum;
+  if (o == 0) xs[kb * kQR + r] = ldexpf(1.f, 12 - up);
+  if (o % (G / 8) == 0) xg[(kb * NS + o / (G / 8)) * kQR + r] = sum;
 }
 
 // Blocks kb0 .. kb0 + nkb of all rows; a row's block to sixteen lanes, eight columns
 // each, two such blocks in flight.
 template <class X, int G>
-__device__ __forceinline__ void quant_stage(const X* __restrict__ x, int H, int rows, int R16, int kb0, int nkb,
-                                            uint4* xh, float* xs, float* xg) {
+__device__ __forceinline__ void quant_stage(const X* __restrict__ x, int H, int rows, int kb0, int nkb, uint4* xh,
+                                            float* xs, float* xg) {
   const int units = rows * nkb * 16, step = blockDim.x;
   for (int u = threadIdx.x; u < units; u += 2 * step) {
     float v[2][8];
@@ -256,51 +259,49 @@ __device__ __forceinline__ void quant_stage(const X* __restrict__ x, int H, int 
     }
 #pragma unroll
     for (int z = 0; z < 2; ++z)
-      if (u + z * step < units) quant_put<X, G>(v[z], u & 15, r[z], kb[z], rows, R16, xh, xs, xg);
+      if (u + z * step < units) quant_put<X, G>(v[z], u & 15, r[z], kb[z], rows, xh, xs, xg);
   }
 }
 
-// y[rows, C] = x What + bias.  A workgroup of eight wavefronts has R rows of x (KC
-// blocks of them at a time) in LDS and goes through groups of tiles; S wavefronts
-// share a tile, each S-th block to one, and join their sums in LDS.  Each wavefront
-// keeps PF blocks of codes in flight, over the ends of tiles.
-constexpr int kQW = 8;
-constexpr size_t kQLds = 80 << 10;   // most LDS of a workgroup: two to a CU
+// y[rows, C] = x What + bias.  A workgroup of sixteen wavefronts has up to sixteen
+// rows of x (KC blocks of them at a time) in LDS and goes through groups of tiles; S
+// wavefronts share a tile, each S-th block to one, and join their sums in LDS.  Each
+// wavefront keeps PF blocks of codes in flight, over the ends of tiles.  The words
+// are the rows of the matrix instruction's result, so that a lane has four adjacent
+// ones of one row of y.
 struct QuantJob {
   QuantNet q;
   const void* x;
   const float* bias;
   void* y;
-  int n, R, KC, S, groups, ybf;
+  int n, KC, S, groups, ybf;
 };
 
-template <class X, int RT, int G, bool SHIFT>
+template <class X, int G, bool SHIFT>
 __global__ void __launch_bounds__(64 * kQW) k_quant_product(QuantJob a) {
-  constexpr int P = sizeof(X) == 4 ? 2 : 1, NS = kQB / G, W16 = NS * (SHIFT ? 2 : 1), PF = 4, R16 = 16 * RT;
+  constexpr int P = sizeof(X) == 4 ? 2 : 1, NS = kQB / G, W16 = NS * (SHIFT ? 2 : 1), PF = 2;
   extern __shared__ uint4 lds[];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int r0 = blockIdx.y * R16, rows = min(a.R, a.n - r0);
+  const int r0 = blockIdx.y * kQR, rows = min(kQR, a.n - r0);
   uint4* xh = lds;
-  float* xs = reinterpret_cast<float*>(lds + (size_t)a.KC * P * 16 * a.R);
-  float* xg = xs + a.KC * R16;
-  float* red = xg + a.KC * NS * R16;   // [kQW][RT * 4][64]
+  float* xs = reinterpret_cast<float*>(lds + (size_t)a.KC * P * 16 * rows);
+  float* xg = xs + a.KC * kQR;
+  v4f* red = reinterpret_cast<v4f*>(xg + a.KC * NS * kQR);   // [kQW][64]
   const X* x = (const X*)a.x + (size_t)r0 * a.q.H;
   const int KB = a.q.KB, T = a.q.T, S = a.S, ks = w % S, tw = w / S, per = kQW / S;
   const int steps = (KB + S - 1) / S, cstep = a.KC / S;   // blocks of a wavefront: of a tile, of a chunk
   const int mine = (a.groups - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x;   // groups of tiles
-  const int items = mine * steps;
+  const int items = mine * steps, j = lane >> 4, row = min(lane & 15, rows - 1);
   struct Block {
     uint4 c;
-    u16 s[W16];
+    uint32_t s[2 * W16];   // of this lane's four words
   } ring[PF];
   int ls = 0, lg = 0;   // the next block to ask for; past the last one, it again
   auto load = [&](Block& f) {
     const int kb = min(ls * S + ks, KB - 1), t = min(((int)blockIdx.x + lg * (int)gridDim.x) * per + tw, T - 1);
     const size_t block = (size_t)t * KB + kb;
     f.c = a.q.code[block * 64 + lane];
-    const u16* s = a.q.scale + (block * 16 + (lane & 15)) * W16;
-    if constexpr (W16 == 1) f.s[0] = *s;
-    else __builtin_memcpy(f.s, __builtin_assume_aligned(s, 2 * W16), 2 * W16);
+    __builtin_memcpy(f.s, __builtin_assume_aligned(a.q.scale + (block * 16 + 4 * j) * W16, 8), 8 * W16);
     if (++ls == steps) {
       ls = 0;
       lg = min(lg + 1, mine - 1);
@@ -308,12 +309,8 @@ __global__ void __launch_bounds__(64 * kQW) k_quant_product(QuantJob a) {
   };
 #pragma unroll
   for (int u = 0; u < PF; ++u) load(ring[u]);
-  // this lane's place in a dword's fragment of each 16 rows
-  const uint4* frag[RT];
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) frag[rt] = xh + (lane >> 4) * rows + min(rt * 16 + (lane & 15), rows - 1);
-  const int up = 4 * (lane >> 4);   // this lane's rows of the sums
-  v4f acc[RT] = {};
+  const uint4* frag = xh + j * rows + row;   // this lane's place in a dword's fragment
+  v4f acc = {};
   int step = 0, cs = 0, grp = 0;
   for (int it0 = 0; it0 < items; it0 += PF) {
 #pragma unroll
@@ -322,44 +319,32 @@ __global__ void __launch_bounds__(64 * kQW) k_quant_product(QuantJob a) {
       if (cs == 0 && (it0 + u == 0 || a.KC < KB)) {
         if (it0 + u > 0) __syncthreads();   // the last chunk has been read
         const int kb0 = step * S;
-        quant_stage<X, G>(x, a.q.H, rows, R16, kb0, min(a.KC, KB - kb0), xh, xs, xg);
+        quant_stage<X, G>(x, a.q.H, rows, kb0, min(a.KC, KB - kb0), xh, xs, xg);
         __syncthreads();
       }
       if (step * S + ks < KB) {
         const int kc = cs * S + ks;
         const uint32_t d[4] = {ring[u].c.x, ring[u].c.y, ring[u].c.z, ring[u].c.w};
-        v4f blk[RT];
+        const float f = xs[kc * kQR + row];
 #pragma unroll
         for (int g = 0; g < NS; ++g) {
-          v4f part[RT] = {};
+          v4f part = {};
 #pragma unroll
           for (int b = g * (4 / NS); b < (g + 1) * (4 / NS); ++b) {
             const h8 c8 = halves(d[b]);
 #pragma unroll
             for (int p = 0; p < P; ++p)
-#pragma unroll
-              for (int rt = 0; rt < RT; ++rt)
-                part[rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
-                    __builtin_bit_cast(h8, frag[rt][((kc * P + p) * 4 + b) * 4 * rows]), c8, part[rt], 0, 0, 0);
+              part = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+                  c8, __builtin_bit_cast(h8, frag[((kc * P + p) * 4 + b) * 4 * rows]), part, 0, 0, 0);
           }
-          const float s = bf2f(ring[u].s[g * (SHIFT ? 2 : 1)]);
-          const float t = SHIFT ? fmaf(-8.f, s, bf2f(ring[u].s[2 * g + 1])) : -8.f * s;
+          const float X1 = xg[(kc * NS + g) * kQR + row], X8 = -8.f * X1;
 #pragma unroll
-          for (int rt = 0; rt < RT; ++rt) {
-            const float4 X4 = *reinterpret_cast<const float4*>(xg + (kc * NS + g) * R16 + rt * 16 + up);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              blk[rt][i] = g ? fmaf(s, part[rt][i], blk[rt][i]) : s * part[rt][i];
-              acc[rt][i] = fmaf(t, i == 0 ? X4.x : i == 1 ? X4.y : i == 2 ? X4.z : X4.w, acc[rt][i]);
-            }
+          for (int i = 0; i < 4; ++i) {   // word i's numbers: halves W16 i and on
+            const int at = W16 * i + g * (SHIFT ? 2 : 1);
+            const uint32_t s = ring[u].s[at / 2];
+            acc[i] = fmaf(__uint_as_float(at & 1 ? s & 0xffff0000u : s << 16), fmaf(f, part[i], X8), acc[i]);
+            if (SHIFT) acc[i] = fmaf(__uint_as_float(s & 0xffff0000u), X1, acc[i]);
           }
-        }
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-          const float4 f = *reinterpret_cast<const float4*>(xs + kc * R16 + rt * 16 + up);
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            acc[rt][i] = fmaf(i == 0 ? f.x : i == 1 ? f.y : i == 2 ? f.z : f.w, blk[rt][i], acc[rt][i]);
         }
       }
       load(ring[u]);
@@ -370,34 +355,33 @@ __global__ void __launch_bounds__(64 * kQW) k_quant_product(QuantJob a) {
       const int t = ((int)blockIdx.x + grp++ * (int)gridDim.x) * per + tw;
       if (S > 1) {
         __syncthreads();
-        if (ks > 0)
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) red[(w * RT * 4 + rt * 4 + i) * 64 + lane] = acc[rt][i];
+        if (ks > 0) red[w * 64 + lane] = acc;
         __syncthreads();
         if (ks == 0)
-          for (int o = 1; o < S; ++o)
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) acc[rt][i] += red[((w + o) * RT * 4 + rt * 4 + i) * 64 + lane];
+          for (int o = 1; o < S; ++o) acc += red[(w + o) * 64 + lane];
       }
-      const int c = t * 16 + (lane & 15);
-      if (ks == 0 && t < T && c < a.q.C) {
-        const float bias = a.bias ? a.bias[c] : 0.f;
+      const int c = t * 16 + 4 * j;
+      if (ks == 0 && t < T && (lane & 15) < rows && c < a.q.C) {
+        const size_t at = (size_t)(r0 + row) * a.q.C + c;
+        const bool whole = c + 4 <= a.q.C;
+        float v[4];
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
+        for (int i = 0; i < 4; ++i) {
+          const float bias = a.bias && (whole || c + i < a.q.C) ? a.bias[c + i] : 0.f;
+          v[i] = fmaf(acc[i], 1.f / kQDown, bias);
+        }
+        if (whole) {   // at any address that is aligned to its elements
+          typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
+          typedef uint32_t u2 __attribute__((ext_vector_type(2), aligned(2)));
+          if (a.ybf) *reinterpret_cast<u2*>((u16*)a.y + at) = u2{f2bf2(v[0], v[1]), f2bf2(v[2], v[3])};
+          else *reinterpret_cast<f4*>((float*)a.y + at) = f4{v[0], v[1], v[2], v[3]};
+        } else {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int r = rt * 16 + up + i;
-            const size_t at = (size_t)(r0 + r) * a.q.C + c;
-            const float v = fmaf(acc[rt][i], 1.f / kQDown, bias);
-            if (r < rows) a.ybf ? store_one((u16*)a.y + at, v) : store_one((float*)a.y + at, v);
-          }
+          for (int i = 0; i < 4; ++i)
+            if (c + i < a.q.C) a.ybf ? store_one((u16*)a.y + at + i, v[i]) : store_one((float*)a.y + at + i, v[i]);
+        }
       }
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) acc[rt] = v4f{0.f, 0.f, 0.f, 0.f};
+      acc = v4f{0.f, 0.f, 0.f, 0.f};
     }
   }
 }
@@ -511,37 +495,25 @@ cavs_status quant_product_run(cavs_ctx* ctx, const cavs_quant* q, int x_type, co
   QuantJob a{quant_net(q, q->data), x, bias, y, n};
   a.ybf = y_type == CAVS_T_BF16;
   const int P = x_type == CAVS_T_F32 ? 2 : 1, T = a.q.T, KB = a.q.KB;
-  // rows of a workgroup, and wavefronts of a tile: as many as leave each of 2048
-  // wavefronts something to do, then fewer rows
-  int rt = n <= 16 ? 1 : n <= 32 ? 2 : 4, rows;
-  size_t block, red;
-  for (;; rt /= 2) {
-    rows = cdiv(n, 16 * rt);
-    a.R = std::min(n, 16 * rt);
-    block = (size_t)P * 256 * a.R + 64 * rt * (1 + kQB / q->group);
-    red = (size_t)kQW * rt * 1024;
-    a.S = 1;
-    while (a.S < kQW && a.S < KB && (long)T * a.S * rows < 2048 && 2 * a.S * block + red <= kQLds) a.S *= 2;
-    if (rt == 1 || (long)T * a.S * rows >= 2048) break;
-  }
-  if (a.S == 1) red = 0;
+  // wavefronts of a tile: as many as leave each of 2048 something to do
+  const int rows = cdiv(n, kQR);
+  const size_t block = (size_t)P * 256 * std::min(n, kQR) + 4 * kQR * (1 + kQB / q->group);
+  a.S = 1;
+  while (a.S < 8 && a.S < KB && (long)T * a.S * rows < 2048) a.S *= 2;
+  const size_t red = a.S > 1 ? (size_t)kQW * 1024 : 0;
   a.KC = std::min(cdiv(KB, a.S), (int)((kQLds - red) / block) / a.S) * a.S;
   a.groups = cdiv(T, kQW / a.S);
   const size_t shmem = a.KC * block + red;
-  const dim3 grid(std::min(a.groups, std::max(1, cdiv(512, rows))), rows);
+  // a workgroup per CU; the groups of rows of a tile on one XCD
+  const dim3 grid(std::min(a.groups, (int)align_up(cdiv(256, rows), 8)), rows);
   by_group(q, [&](auto g, auto shift) {
     by_element(x_type, [&](auto t) {
       using X = decltype(t);
-      auto launch = [&](auto R) {
-        if (shmem > 64 << 10)
-          (void)hipFuncSetAttribute((const void*)k_quant_product<X, R(), g(), shift()>,
-                                    hipFuncAttributeMaxDynamicSharedMemorySize, (int)shmem);
-        CAVS_LAUNCH("k_quant_product", (k_quant_product<X, R(), g(), shift()>), grid, dim3(64 * kQW), shmem,
-                    ctx->stream, a);
-      };
-      if (rt == 1) launch(std::integral_constant<int, 1>{});
-      else if (rt == 2) launch(std::integral_constant<int, 2>{});
-      else launch(std::integral_constant<int, 4>{});
+      if (shmem > 64 << 10)
+        (void)hipFuncSetAttribute((const void*)k_quant_product<X, g(), shift()>,
+                                  hipFuncAttributeMaxDynamicSharedMemorySize, (int)shmem);
+      CAVS_LAUNCH("k_quant_product", (k_quant_product<X, g(), shift()>), grid, dim3(64 * kQW), shmem, ctx->stream,
+                  a);
     });
   });
   CAVS_LAUNCH_CHECK(ctx);
