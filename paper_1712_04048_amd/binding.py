@@ -625,11 +625,13 @@ class QuantWeights:
     shift: bool = False
 
     def raw(self, device=None) -> cavs_quant:
-        n = quant_bytes(self.H, self.C, self.group, self.shift)
+        H, C, group, shift = int(self.H), int(self.C), int(self.group), int(bool(self.shift))
+        shape = getattr(self.data, "shape", ())
+        if H > 0 and C > 0 and group in (32, 64, 128):
+            # cavs_quant_bytes, without a call for each product
+            shape = (-(-C // 16) * -(-H // 128) * 16 * (64 + 128 // group * (4 if shift else 2)),)
         # refused sizes are the library's to name
-        shape = (n,) if n else getattr(self.data, "shape", ())
-        p = _operand("data", self.data, shape, (torch.uint8,), device)
-        return cavs_quant(int(self.H), int(self.C), int(self.group), int(bool(self.shift)), p)
+        return cavs_quant(H, C, group, shift, _operand("data", self.data, shape, (torch.uint8,), device))
 
 
 def quant_pack(ctx: Context, q: QuantWeights, W: torch.Tensor) -> None:

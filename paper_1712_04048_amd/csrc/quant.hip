@@ -495,10 +495,12 @@ cavs_status quant_product_run(cavs_ctx* ctx, const cavs_quant* q, int x_type, co
   QuantJob a{quant_net(q, q->data), x, bias, y, n};
   a.ybf = y_type == CAVS_T_BF16;
   const int P = x_type == CAVS_T_F32 ? 2 : 1, T = a.q.T, KB = a.q.KB;
-  // wavefronts of a tile: as many as leave each of 2048 something to do
+  // wavefronts of a tile: as many as leave each of 2048 something to do; two of long
+  // tiles, whose blocks are then read in the order of memory by neighbours (16 x
+  // 128 000 x 2048: 37.0 us with one, 35.8 with two, 36.1 with four; of 1024: one)
   const int rows = cdiv(n, kQR);
   const size_t block = (size_t)P * 256 * std::min(n, kQR) + 4 * kQR * (1 + kQB / q->group);
-  a.S = 1;
+  a.S = KB >= 16 ? 2 : 1;
   while (a.S < 8 && a.S < KB && (long)T * a.S * rows < 2048) a.S *= 2;
   const size_t red = a.S > 1 ? (size_t)kQW * 1024 : 0;
   a.KC = std::min(cdiv(KB, a.S), (int)((kQLds - red) / block) / a.S) * a.S;

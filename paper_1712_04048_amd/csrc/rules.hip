@@ -48,31 +48,73 @@ __device__ __forceinline__ void rules_write(const RulesNet& a, int row, Top t, f
   if (a.lse) a.lse[row] = sum != sum || fabsf(t.v) < INFINITY ? t.v + logf(sum) : t.v;
 }
 
-// A workgroup takes kPer words a thread of one row, in pieces of eight adjacent ones.
-// Counts of the words so far and sums of the row's own biases are kept in LDS for
-// its words alone; whole numbers and a fixed order, so that no run differs.
+// V adjacent elements at any address that is aligned to them.
+template <class T, int V>
+__device__ __forceinline__ void load_any(const T* p, float (&v)[V]) {
+  if constexpr (sizeof(T) == 4) {
+    typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
+#pragma unroll
+    for (int i = 0; i < V; i += 4) {
+      const f4 a = *reinterpret_cast<const f4*>(p + i);
+      v[i] = a[0], v[i + 1] = a[1], v[i + 2] = a[2], v[i + 3] = a[3];
+    }
+  } else {
+    typedef u16 s __attribute__((ext_vector_type(V), aligned(2)));
+    const s a = *reinterpret_cast<const s*>(p);
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = __uint_as_float((uint32_t)a[i] << 16);
+  }
+}
+template <class T, int V>
+__device__ __forceinline__ void store_any(T* p, const float (&v)[V]) {
+  if constexpr (sizeof(T) == 4) {
+    typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
+#pragma unroll
+    for (int i = 0; i < V; i += 4) *reinterpret_cast<f4*>(p + i) = f4{v[i], v[i + 1], v[i + 2], v[i + 3]};
+  } else {
+    typedef uint32_t w __attribute__((ext_vector_type(V / 2), aligned(2)));
+    w a;
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) a[i] = f2bf2(v[2 * i], v[2 * i + 1]);
+    *reinterpret_cast<w*>(p) = a;
+  }
+}
+
+// A workgroup takes kPer words a thread of one row, in pieces of V adjacent ones, 16
+// bytes of the narrower type.  Counts of the words so far and sums of the row's own
+// biases are kept in LDS for its words alone; whole numbers and a fixed order, so
+// that no run differs.
 template <class Z, class O, int THREADS>
 __global__ void __launch_bounds__(THREADS) k_rules(RulesNet a, int row0, const Z* z, O* out) {
 #pragma clang fp contract(off)
-  constexpr int SEG = THREADS * kPer, NV = kPer / 8;
-  extern __shared__ uint32_t lds[];
+  constexpr int SEG = THREADS * kPer, V = sizeof(Z) == 4 && sizeof(O) == 4 ? 4 : 8, NV = kPer / V;
+  extern __shared__ uint4 lds[];
   __shared__ Top tops[THREADS / 64];
   __shared__ float sums[THREADS / 64];
   const int tid = threadIdx.x, row = row0 + blockIdx.x / a.segs, seg = blockIdx.x % a.segs;
   const int c0 = seg * SEG, len = min(SEG, a.C - c0);
-  uint32_t* count = lds;
-  float* own = reinterpret_cast<float*>(lds + (a.past ? SEG : 0));
-  float v[NV][8];
+  uint32_t* count = reinterpret_cast<uint32_t*>(lds);
+  float* own = reinterpret_cast<float*>(lds + (a.past ? SEG / 4 : 0));
+  float v[NV][V];
   const Z* zr = z + (size_t)row * a.C + c0;
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
-    const int c = (k * THREADS + tid) * 8;
+    const int c = (k * THREADS + tid) * V;
+    if (c + V <= len) {
+      load_any<Z, V>(zr + c, v[k]);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[k][i] = c + i < len ? sizeof(Z) == 4 ? (float)((const float*)zr)[c + i]
-                                            : __uint_as_float((uint32_t)((const u16*)zr)[c + i] << 16) : -INFINITY;
+      for (int i = 0; i < V; ++i) {
+        v[k][i] = -INFINITY;
+        if (c + i < len) {
+          if constexpr (sizeof(Z) == 4) v[k][i] = zr[c + i];
+          else v[k][i] = __uint_as_float((uint32_t)zr[c + i] << 16);
+        }
+      }
+    }
   }
   if (a.past || a.K) {
-    for (int i = tid; i < (a.past ? SEG : 0) + (a.K ? SEG : 0); i += THREADS) lds[i] = 0u;
+    for (int i = tid; i < ((a.past ? SEG : 0) + (a.K ? SEG : 0)) / 4; i += THREADS) lds[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
     bool bad = false;
     if (a.past)
@@ -113,33 +155,71 @@ __global__ void __launch_bounds__(THREADS) k_rules(RulesNet a, int row0, const Z
   float nan = 0.f;
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
-    const int c = (k * THREADS + tid) * 8;
+    const int c = (k * THREADS + tid) * V;
     if (c >= len) continue;
-    const uint32_t bits = mask ? mask[c / 32] >> (c % 32) : 0xffu;
+    float(&x)[V] = v[k];
+    if (a.past) {
+      uint32_t n[V], any = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (c + i >= len) continue;
-      float x = v[k][i];
-      if (a.past) {
-        const uint32_t n = count[c + i];
-        if (n) {
-          x = x > 0.f ? x / r : x * r;
-          x = x - p;
-          x = x - f * (float)n;
-        }
+      for (int i = 0; i < V; i += 4) {
+        const uint4 q = *reinterpret_cast<const uint4*>(count + c + i);
+        n[i] = q.x, n[i + 1] = q.y, n[i + 2] = q.z, n[i + 3] = q.w;
+        any |= q.x | q.y | q.z | q.w;
       }
-      if (a.bias) x = x + a.bias[c0 + c + i];
-      if (a.K) x = x + own[c + i];
-      if (!(bits >> i & 1u)) x = -INFINITY;
-      if (a.temp) x = x / T;
-      v[k][i] = x;
-      top = higher(top, Top{x, c0 + c + i});
-      if (x != x) nan = x;
-      if (out) {
-        O* o = out + (size_t)row * a.C + c0 + c + i;
-        if constexpr (sizeof(O) == 4) *o = x;
-        else *o = f2bf(x);
+      if (any)
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+          if (n[i]) {
+            x[i] = x[i] > 0.f ? x[i] / r : x[i] * r;
+            x[i] = x[i] - p;
+            x[i] = x[i] - f * (float)n[i];
+          }
+    }
+    const bool whole = c + V <= len;
+    if (a.bias) {
+      const float* b = a.bias + c0 + c;
+      float y[V];
+      if (whole) {
+        load_any<float, V>(b, y);
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) y[i] = c + i < len ? b[i] : 0.f;
       }
+#pragma unroll
+      for (int i = 0; i < V; ++i) x[i] = x[i] + y[i];
+    }
+    if (a.K)
+#pragma unroll
+      for (int i = 0; i < V; i += 4) {
+        const float4 q = *reinterpret_cast<const float4*>(own + c + i);
+        x[i] = x[i] + q.x, x[i + 1] = x[i + 1] + q.y, x[i + 2] = x[i + 2] + q.z, x[i + 3] = x[i + 3] + q.w;
+      }
+    if (mask) {
+      const uint32_t bits = mask[c / 32] >> (c % 32);
+#pragma unroll
+      for (int i = 0; i < V; ++i) x[i] = bits >> i & 1u ? x[i] : -INFINITY;
+    }
+    if (a.temp)
+#pragma unroll
+      for (int i = 0; i < V; ++i) x[i] = x[i] / T;
+    if (out) {
+      O* o = out + (size_t)row * a.C + c0 + c;
+      if (whole) {
+        store_any<O, V>(o, x);
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+          if (c + i < len) {
+            if constexpr (sizeof(O) == 4) o[i] = x[i];
+            else o[i] = f2bf(x[i]);
+          }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      if (!whole && c + i >= len) x[i] = -INFINITY;
+      if (x[i] > top.v) top = Top{x[i], c0 + c + i};   // ascending words: the first one stays
+      nan += x[i] != x[i] ? x[i] : 0.f;
     }
   }
   if (!a.best && !a.lse) return;
@@ -153,7 +233,7 @@ __global__ void __launch_bounds__(THREADS) k_rules(RulesNet a, int row0, const Z
 #pragma unroll
     for (int k = 0; k < NV; ++k)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s += __builtin_amdgcn_exp2f((v[k][i] - top.v) * kLog2e);
+      for (int i = 0; i < V; ++i) s += __builtin_amdgcn_exp2f((v[k][i] - top.v) * kLog2e);
   s = wave_sum(s);
   if ((tid & 63) == 0) sums[tid >> 6] = s;
   __syncthreads();
