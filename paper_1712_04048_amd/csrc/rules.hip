@@ -23,29 +23,57 @@ struct RulesNet {
   const uint32_t* mask;
   int* best;
   float* lse;
-  float4* part;   // [n][segments]: largest, sum of exp(v - largest), its word
+  float4* part;   // [n][segments][wavefronts]: largest, sum of exp(v - largest), its word
   int segs;
   int* err;
 };
 
-// Largest value and its first word, over the workgroup.
+// A largest value and the first word that has it.
 struct Top {
   float v;
   int c;
 };
-__device__ __forceinline__ Top higher(Top a, Top b) {
-  return b.v > a.v || (b.v == a.v && b.c < a.c) ? b : a;
+
+// Over the wavefront, in every lane: sixteen lanes by rotation, then the four rows.
+template <class F>
+__device__ __forceinline__ float wave_all(float v, F f) {
+  auto ror = [](float x, auto n) {
+    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x120 + decltype(n)::value, 15, 15, true));
+  };
+  v = f(v, ror(v, std::integral_constant<int, 8>{}));
+  v = f(v, ror(v, std::integral_constant<int, 4>{}));
+  v = f(v, ror(v, std::integral_constant<int, 2>{}));
+  v = f(v, ror(v, std::integral_constant<int, 1>{}));
+  auto row = [&](int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), l)); };
+  return f(f(row(0), row(16)), f(row(32), row(48)));
 }
 __device__ __forceinline__ Top wave_top(Top t) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) t = higher(t, Top{__shfl_xor(t.v, o, kWave), __shfl_xor(t.c, o, kWave)});
-  return t;
+  const float v = wave_all(t.v, [](float x, float y) { return fmaxf(x, y); });
+  // words are below 2^20: as floats they are what they are
+  const float c = wave_all(t.v == v ? (float)t.c : INFINITY, [](float x, float y) { return fminf(x, y); });
+  return Top{v, (int)c};
+}
+__device__ __forceinline__ float wave_total(float s) {
+  return wave_all(s, [](float x, float y) { return x + y; });
 }
 
-__device__ __forceinline__ void rules_write(const RulesNet& a, int row, Top t, float sum) {
-  // sum is of exp(v - t.v); all words masked, or the largest is infinite: no sum
-  if (a.best) a.best[row] = t.v == -INFINITY ? -1 : t.c;
-  if (a.lse) a.lse[row] = sum != sum || fabsf(t.v) < INFINITY ? t.v + logf(sum) : t.v;
+// A wavefront joins n parts (largest, sum of exp(v - largest), its word) of a row.
+__device__ __forceinline__ void rules_join(const RulesNet& a, int row, const float4* part, int n) {
+  const int lane = threadIdx.x & 63;
+  Top top{-INFINITY, 1 << 20};
+  for (int k = lane; k < n; k += 64)   // ascending words
+    if (part[k].x > top.v) top = Top{part[k].x, __float_as_int(part[k].z)};
+  top = wave_top(top);
+  float s = 0.f;
+  for (int k = lane; k < n; k += 64)
+    // a part without a finite value adds what it has (nothing, or NaN)
+    s += fabsf(part[k].x) < INFINITY && fabsf(top.v) < INFINITY
+             ? part[k].y * __builtin_amdgcn_exp2f((part[k].x - top.v) * kLog2e) : part[k].y;
+  s = wave_total(s);
+  if (lane != 0) return;
+  if (a.best) a.best[row] = top.v == -INFINITY ? -1 : top.c;
+  // all words masked, or the largest is infinite: no sum, unless there is a NaN
+  if (a.lse) a.lse[row] = s != s || fabsf(top.v) < INFINITY ? top.v + logf(s) : top.v;
 }
 
 // V adjacent elements at any address that is aligned to them.
@@ -80,91 +108,118 @@ __device__ __forceinline__ void store_any(T* p, const float (&v)[V]) {
   }
 }
 
-// A workgroup takes kPer words a thread of one row, in pieces of V adjacent ones, 16
-// bytes of the narrower type.  Counts of the words so far and sums of the row's own
-// biases are kept in LDS for its words alone; whole numbers and a fixed order, so
-// that no run differs.
+// A workgroup takes a piece, kPer words a thread of one row, a thread vectors of V
+// adjacent ones, 16 bytes of the narrower type.  Everything that it reads is asked for
+// before anything is waited for.  Counts of the words so far and sums of the row's
+// own biases are kept in LDS for the piece's words alone; whole numbers and a fixed
+// order, so that no run differs.  Each wavefront leaves its largest v and its sum.
+// (Workgroups that go through pieces and ask for the next one ahead were slower: 256
+// x 128 000 in bf16 49 us, 39 with one for each piece.)
 template <class Z, class O, int THREADS>
 __global__ void __launch_bounds__(THREADS) k_rules(RulesNet a, int row0, const Z* z, O* out) {
 #pragma clang fp contract(off)
-  constexpr int SEG = THREADS * kPer, V = sizeof(Z) == 4 && sizeof(O) == 4 ? 4 : 8, NV = kPer / V;
+  constexpr int SEG = THREADS * kPer, V = sizeof(Z) == 4 && sizeof(O) == 4 ? 4 : 8, NV = kPer / V, W = THREADS / 64;
   extern __shared__ uint4 lds[];
-  __shared__ Top tops[THREADS / 64];
-  __shared__ float sums[THREADS / 64];
-  const int tid = threadIdx.x, row = row0 + blockIdx.x / a.segs, seg = blockIdx.x % a.segs;
-  const int c0 = seg * SEG, len = min(SEG, a.C - c0);
+  __shared__ float4 parts[W];
+  const int tid = threadIdx.x, row = row0 + blockIdx.x / a.segs, c0 = blockIdx.x % a.segs * SEG;
+  const int len = min(SEG, a.C - c0);
   uint32_t* count = reinterpret_cast<uint32_t*>(lds);
   float* own = reinterpret_cast<float*>(lds + (a.past ? SEG / 4 : 0));
-  float v[NV][V];
+  int* word = reinterpret_cast<int*>(own + (a.K ? SEG : 0));   // the row's own words and their biases
+  float* extra = reinterpret_cast<float*>(word + a.K);
+  typedef Z Raw __attribute__((ext_vector_type(V), aligned(sizeof(Z))));
+  Raw raw[NV];
   const Z* zr = z + (size_t)row * a.C + c0;
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     const int c = (k * THREADS + tid) * V;
-    if (c + V <= len) {
-      load_any<Z, V>(zr + c, v[k]);
-    } else {
+    if (c + V <= len) raw[k] = *reinterpret_cast<const Raw*>(zr + c);
+  }
+  constexpr int AHEAD = 2;
+  int said[AHEAD];
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        v[k][i] = -INFINITY;
-        if (c + i < len) {
-          if constexpr (sizeof(Z) == 4) v[k][i] = zr[c + i];
-          else v[k][i] = __uint_as_float((uint32_t)zr[c + i] << 16);
-        }
-      }
+  for (int k = 0; k < AHEAD; ++k)
+    said[k] = a.past && k * THREADS + tid < a.L ? a.past[(size_t)row * a.L + k * THREADS + tid] : -1;
+  const float r = a.repeat ? a.repeat[row] : 1.f, p = a.presence ? a.presence[row] : 0.f;
+  const float f = a.frequency ? a.frequency[row] : 0.f, T = a.temp ? a.temp[row] : 1.f;
+  uint32_t bits[NV];
+  if (a.mask) {
+    const int m = a.mask_row ? a.mask_row[row] : a.M == 1 ? 0 : row;
+    const bool there = (unsigned)m < (unsigned)a.M;
+    if (!there && m != -1 && tid == 0) a.err[1] = 1;
+    const uint32_t* mask = a.mask + (size_t)(there ? m : 0) * a.W32 + c0 / 32;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int c = (k * THREADS + tid) * V;
+      bits[k] = there && c < len ? mask[c / 32] >> (c % 32) : ~0u;
     }
   }
   if (a.past || a.K) {
+    bool bad = false;
+    for (int i = tid; i < a.K; i += THREADS) {
+      const int w = a.word[(size_t)row * a.K + i];
+      word[i] = w;
+      extra[i] = a.extra[(size_t)row * a.K + i];
+      bad |= (unsigned)(w + 1) > (unsigned)a.C;
+    }
     for (int i = tid; i < ((a.past ? SEG : 0) + (a.K ? SEG : 0)) / 4; i += THREADS) lds[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
-    bool bad = false;
-    if (a.past)
-      for (int i = tid; i < a.L; i += THREADS) {
-        const int w = a.past[(size_t)row * a.L + i];
+    if (a.past) {
+      auto one = [&](int w) {
         if ((unsigned)(w - c0) < (unsigned)len) atomicAdd(&count[w - c0], 1u);
         bad |= (unsigned)(w + 1) > (unsigned)a.C;
-      }
-    if (a.K) {
-      const int* word = a.word + (size_t)row * a.K;
-      const float* extra = a.extra + (size_t)row * a.K;
-      for (int i = tid; i < a.K; i += THREADS) {
-        const int w = word[i];
-        bad |= (unsigned)(w + 1) > (unsigned)a.C;
-        if ((unsigned)(w - c0) >= (unsigned)len) continue;
-        // the first of a word's places adds all of them
-        bool first = true;
-        for (int j = 0; j < i; ++j) first &= word[j] != w;
-        if (!first) continue;
-        float s = extra[i];
-        for (int j = i + 1; j < a.K; ++j)
-          if (word[j] == w) s += extra[j];
-        own[w - c0] = s;
-      }
+      };
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) one(said[k]);
+      for (int i = AHEAD * THREADS + tid; i < a.L; i += THREADS) one(a.past[(size_t)row * a.L + i]);
     }
-    if (bad && seg == 0) a.err[1] = 1;
+    for (int i = tid; i < a.K; i += THREADS) {
+      const int w = word[i];
+      if ((unsigned)(w - c0) >= (unsigned)len) continue;
+      // the first of a word's places adds all of them
+      bool first = true;
+      for (int j = 0; j < i; ++j) first &= word[j] != w;
+      if (!first) continue;
+      float s = extra[i];
+      for (int j = i + 1; j < a.K; ++j)
+        if (word[j] == w) s += extra[j];
+      own[w - c0] = s;
+    }
+    if (bad) a.err[1] = 1;
     __syncthreads();
   }
-  const float r = a.repeat ? a.repeat[row] : 1.f, p = a.presence ? a.presence[row] : 0.f;
-  const float f = a.frequency ? a.frequency[row] : 0.f, T = a.temp ? a.temp[row] : 1.f;
-  const uint32_t* mask = nullptr;
-  if (a.mask) {
-    const int m = a.mask_row ? a.mask_row[row] : a.M == 1 ? 0 : row;
-    if ((unsigned)m < (unsigned)a.M) mask = a.mask + (size_t)m * a.W32 + c0 / 32;
-    else if (m != -1 && tid == 0 && seg == 0) a.err[1] = 1;
-  }
-  Top top{-INFINITY, 0x7fffffff};
-  float nan = 0.f;
+  float v[NV][V];
+  Top top{-INFINITY, 1 << 20};
+  float sum = 0.f;
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     const int c = (k * THREADS + tid) * V;
-    if (c >= len) continue;
     float(&x)[V] = v[k];
+    const bool whole = c + V <= len;
+    if (whole) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        if constexpr (sizeof(Z) == 4) x[i] = raw[k][i];
+        else x[i] = __uint_as_float((uint32_t)raw[k][i] << 16);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        x[i] = -INFINITY;
+        if (c + i < len) {
+          if constexpr (sizeof(Z) == 4) x[i] = zr[c + i];
+          else x[i] = __uint_as_float((uint32_t)zr[c + i] << 16);
+        }
+      }
+      if (c >= len) continue;
+    }
     if (a.past) {
       uint32_t n[V], any = 0;
 #pragma unroll
       for (int i = 0; i < V; i += 4) {
-        const uint4 q = *reinterpret_cast<const uint4*>(count + c + i);
-        n[i] = q.x, n[i + 1] = q.y, n[i + 2] = q.z, n[i + 3] = q.w;
-        any |= q.x | q.y | q.z | q.w;
+        const uint4 y = *reinterpret_cast<const uint4*>(count + c + i);
+        n[i] = y.x, n[i + 1] = y.y, n[i + 2] = y.z, n[i + 3] = y.w;
+        any |= y.x | y.y | y.z | y.w;
       }
       if (any)
 #pragma unroll
@@ -175,7 +230,6 @@ __global__ void __launch_bounds__(THREADS) k_rules(RulesNet a, int row0, const Z
             x[i] = x[i] - f * (float)n[i];
           }
     }
-    const bool whole = c + V <= len;
     if (a.bias) {
       const float* b = a.bias + c0 + c;
       float y[V];
@@ -191,14 +245,12 @@ __global__ void __launch_bounds__(THREADS) k_rules(RulesNet a, int row0, const Z
     if (a.K)
 #pragma unroll
       for (int i = 0; i < V; i += 4) {
-        const float4 q = *reinterpret_cast<const float4*>(own + c + i);
-        x[i] = x[i] + q.x, x[i + 1] = x[i + 1] + q.y, x[i + 2] = x[i + 2] + q.z, x[i + 3] = x[i + 3] + q.w;
+        const float4 y = *reinterpret_cast<const float4*>(own + c + i);
+        x[i] = x[i] + y.x, x[i + 1] = x[i + 1] + y.y, x[i + 2] = x[i + 2] + y.z, x[i + 3] = x[i + 3] + y.w;
       }
-    if (mask) {
-      const uint32_t bits = mask[c / 32] >> (c % 32);
+    if (a.mask)
 #pragma unroll
-      for (int i = 0; i < V; ++i) x[i] = bits >> i & 1u ? x[i] : -INFINITY;
-    }
+      for (int i = 0; i < V; ++i) x[i] = bits[k] >> i & 1u ? x[i] : -INFINITY;
     if (a.temp)
 #pragma unroll
       for (int i = 0; i < V; ++i) x[i] = x[i] / T;
@@ -219,46 +271,29 @@ __global__ void __launch_bounds__(THREADS) k_rules(RulesNet a, int row0, const Z
     for (int i = 0; i < V; ++i) {
       if (!whole && c + i >= len) x[i] = -INFINITY;
       if (x[i] > top.v) top = Top{x[i], c0 + c + i};   // ascending words: the first one stays
-      nan += x[i] != x[i] ? x[i] : 0.f;
+      sum += x[i] != x[i] ? x[i] : 0.f;
     }
   }
   if (!a.best && !a.lse) return;
   top = wave_top(top);
-  if ((tid & 63) == 0) tops[tid >> 6] = top;
-  __syncthreads();
-#pragma unroll
-  for (int k = 0; k < THREADS / 64; ++k) top = higher(top, tops[k]);
-  float s = nan;
   if (fabsf(top.v) < INFINITY)
 #pragma unroll
     for (int k = 0; k < NV; ++k)
 #pragma unroll
-      for (int i = 0; i < V; ++i) s += __builtin_amdgcn_exp2f((v[k][i] - top.v) * kLog2e);
-  s = wave_sum(s);
-  if ((tid & 63) == 0) sums[tid >> 6] = s;
-  __syncthreads();
-  if (tid == 0) {
-    s = 0.f;
-    for (int k = 0; k < THREADS / 64; ++k) s += sums[k];
-    if (a.segs == 1) rules_write(a, row, top, s);
-    else a.part[(size_t)row * a.segs + seg] = make_float4(top.v, s, __int_as_float(top.c), 0.f);
+      for (int i = 0; i < V; ++i) sum += __builtin_amdgcn_exp2f((v[k][i] - top.v) * kLog2e);
+  sum = wave_total(sum);
+  const float4 mine = make_float4(top.v, sum, __int_as_float(top.c), 0.f);
+  if (a.segs > 1) {
+    if ((tid & 63) == 0) a.part[((size_t)row * a.segs + c0 / SEG) * W + tid / 64] = mine;
+  } else {
+    if ((tid & 63) == 0) parts[tid / 64] = mine;
+    __syncthreads();
+    if (tid < 64) rules_join(a, row, parts, W);
   }
 }
 
-// A wavefront joins a row's segments.
-__global__ void __launch_bounds__(64) k_rules_join(RulesNet a, int row0) {
-  const int row = row0 + blockIdx.x, lane = threadIdx.x;
-  const float4* part = a.part + (size_t)row * a.segs;
-  Top top{-INFINITY, 0x7fffffff};
-  for (int k = lane; k < a.segs; k += 64) top = higher(top, Top{part[k].x, __float_as_int(part[k].z)});
-  top = wave_top(top);
-  float s = 0.f;
-  for (int k = lane; k < a.segs; k += 64)
-    // a segment without a finite word adds what it has (nothing, or NaN)
-    s += fabsf(part[k].x) < INFINITY && fabsf(top.v) < INFINITY
-             ? part[k].y * __builtin_amdgcn_exp2f((part[k].x - top.v) * kLog2e) : part[k].y;
-  s = wave_sum(s);
-  if (lane == 0) rules_write(a, row, top, s);
+__global__ void __launch_bounds__(64) k_rules_join(RulesNet a, int n) {
+  rules_join(a, blockIdx.x, a.part + (size_t)blockIdx.x * n, n);
 }
 
 cavs_status rules_args(cavs_ctx* ctx, const cavs_rules* r) {
@@ -277,7 +312,7 @@ cavs_status rules_args(cavs_ctx* ctx, const cavs_rules* r) {
 
 size_t adjust_ws_bytes(int n, int C) {
   if (n < 0 || C <= 0 || n > kRulesMaxN || C > kRulesMaxC) return 0;
-  return std::max<size_t>(256, (size_t)n * cdiv(C, 256 * kPer) * sizeof(float4));
+  return std::max<size_t>(256, (size_t)n * cdiv(C, 256 * kPer) * 4 * sizeof(float4));
 }
 
 cavs_status adjust_run(cavs_ctx* ctx, const cavs_rules* r, const void* z, void* out, int* best, float* lse,
@@ -320,7 +355,7 @@ cavs_status adjust_run(cavs_ctx* ctx, const cavs_rules* r, const void* z, void* 
     if (((uintptr_t)ws & 15) != 0) return fail(ctx, CAVS_ERR_ARG, "ws must be aligned to 16 bytes");
   }
   const int threads = wide ? 1024 : 256;
-  const size_t shmem = (size_t)threads * kPer * 4 * ((a.past ? 1 : 0) + (a.K ? 1 : 0));
+  const size_t shmem = (size_t)threads * kPer * 4 * ((a.past ? 1 : 0) + (a.K ? 1 : 0)) + 8 * (size_t)a.K;
   // a launch has fewer than 2^32 threads
   const int step = std::max(1, (int)std::min<long>(r->n, (1l << 30) / threads / a.segs));
   for (int i = 0; i < r->n; i += step) {
@@ -328,16 +363,21 @@ cavs_status adjust_run(cavs_ctx* ctx, const cavs_rules* r, const void* z, void* 
     auto go = [&](auto zt, auto ot) {
       using Z = decltype(zt);
       using O = decltype(ot);
+      if (wide && shmem > 64 << 10)
+        (void)hipFuncSetAttribute((const void*)k_rules<Z, O, 1024>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                  (int)shmem);
       if (wide)
-        CAVS_LAUNCH("k_rules<1024>", (k_rules<Z, O, 1024>), grid, dim3(1024), shmem, ctx->stream, a, i, (const Z*)z, (O*)out);
+        CAVS_LAUNCH("k_rules<1024>", (k_rules<Z, O, 1024>), grid, dim3(1024), shmem, ctx->stream, a, i, (const Z*)z,
+                    (O*)out);
       else
-        CAVS_LAUNCH("k_rules<256>", (k_rules<Z, O, 256>), grid, dim3(256), shmem, ctx->stream, a, i, (const Z*)z, (O*)out);
+        CAVS_LAUNCH("k_rules<256>", (k_rules<Z, O, 256>), grid, dim3(256), shmem, ctx->stream, a, i, (const Z*)z,
+                    (O*)out);
     };
     if (zs == 2) os == 2 ? go(u16{}, u16{}) : go(u16{}, float{});
     else os == 2 ? go(float{}, u16{}) : go(float{}, float{});
   }
   if ((best || lse) && a.segs > 1)
-    CAVS_LAUNCH("k_rules_join", k_rules_join, dim3(r->n), dim3(64), 0, ctx->stream, a, 0);
+    CAVS_LAUNCH("k_rules_join", k_rules_join, dim3(r->n), dim3(64), 0, ctx->stream, a, 4 * a.segs);
   CAVS_LAUNCH_CHECK(ctx);
   return CAVS_OK;
 }
