@@ -422,6 +422,12 @@ _TYPES = {torch.float32: T_F32, torch.bfloat16: T_BF16}
 
 def _operand(name: str, t: Optional[torch.Tensor], shape, dtypes, device) -> Optional[int]:
     """The address of a tensor after the checks that the C ABI cannot make."""
+    try:   # all of them at once, as most calls pass them
+        if (t.dtype in dtypes and t.shape == shape and (device is None or t.device == device)
+                and t.is_contiguous() and isinstance(t, torch.Tensor)):
+            return t.data_ptr() or None
+    except AttributeError:
+        pass
     if not isinstance(t, torch.Tensor):
         raise CavsError(ERR_ARG, "%s: a tensor is required" % name)
     if t.dtype not in dtypes:
@@ -655,12 +661,20 @@ def quant_product(ctx: Context, q: QuantWeights, x: torch.Tensor, y: torch.Tenso
     """cavs_quant_product (asynchronous): y [n, C] = x [n, H] What + bias [C]."""
     dev = ctx.torch_device
     r = q.raw(dev)
-    if not isinstance(x, torch.Tensor) or x.dim() != 2:
-        raise CavsError(ERR_ARG, "x: a matrix is required")
+    _columns("x", x)
     n = int(x.shape[0])
     px, py = _operand("x", x, (n, q.H), _TYPES, dev), _operand("y", y, (n, q.C), _TYPES, dev)
     pb = None if bias is None else _operand("bias", bias, (q.C,), (torch.float32,), dev)
     ctx.check(lib().cavs_quant_product(ctx._h, ct.byref(r), _TYPES[x.dtype], px, n, pb, _TYPES[y.dtype], py))
+
+
+_FLOAT, _INT = (torch.float32,), (torch.int32,)
+
+
+def _columns(name: str, t: torch.Tensor) -> int:
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+        raise CavsError(ERR_ARG, "%s: a matrix is required" % name)
+    return int(t.shape[1])
 
 
 @dataclass
@@ -682,31 +696,35 @@ class LogitRules:
     temp: Optional[torch.Tensor] = None
 
     def raw(self, n: int, C: int, z_type: int, out_type: int, device=None) -> cavs_rules:
-        f, i = (torch.float32,), (torch.int32,)
-
-        def columns(name, t):
-            if t is None:
-                return 0
-            if not isinstance(t, torch.Tensor) or t.dim() != 2:
-                raise CavsError(ERR_ARG, "%s: a matrix is required" % name)
-            return int(t.shape[1])
-
-        def p(name, shape, types):
-            t = getattr(self, name)
-            return None if t is None else _operand(name, t, shape, types, device)
-
-        L, K = columns("past", self.past), columns("extra_word", self.extra_word)
-        columns("mask", self.mask)
-        M = 0 if self.mask is None else int(self.mask.shape[0])
-        if self.past is None and any(t is not None for t in (self.repeat, self.presence, self.frequency)):
+        r = cavs_rules(z_type, out_type, n, C)
+        if self.past is not None:
+            r.L = _columns("past", self.past)
+            r.past = _operand("past", self.past, (n, r.L), _INT, device)
+        elif self.repeat is not None or self.presence is not None or self.frequency is not None:
             raise CavsError(ERR_ARG, "repeat, presence and frequency need past")
-        if (self.extra_word is None) != (self.extra is None):
-            raise CavsError(ERR_ARG, "extra_word and extra [n, K] go together")
-        return cavs_rules(
-            z_type, out_type, n, C, L, p("past", (n, L), i), p("repeat", (n,), f), p("presence", (n,), f),
-            p("frequency", (n,), f), p("bias", (C,), f), K, p("extra_word", (n, K), i),
-            p("extra", (n, K), f), M, p("mask", (M, -(-C // 32)), i), p("mask_row", (n,), i),
-            p("temp", (n,), f))
+        if self.repeat is not None:
+            r.repeat = _operand("repeat", self.repeat, (n,), _FLOAT, device)
+        if self.presence is not None:
+            r.presence = _operand("presence", self.presence, (n,), _FLOAT, device)
+        if self.frequency is not None:
+            r.frequency = _operand("frequency", self.frequency, (n,), _FLOAT, device)
+        if self.bias is not None:
+            r.bias = _operand("bias", self.bias, (C,), _FLOAT, device)
+        if self.extra_word is not None or self.extra is not None:
+            if self.extra_word is None or self.extra is None:
+                raise CavsError(ERR_ARG, "extra_word and extra [n, K] go together")
+            r.K = _columns("extra_word", self.extra_word)
+            r.extra_word = _operand("extra_word", self.extra_word, (n, r.K), _INT, device)
+            r.extra = _operand("extra", self.extra, (n, r.K), _FLOAT, device)
+        if self.mask is not None:
+            _columns("mask", self.mask)
+            r.M = int(self.mask.shape[0])
+            r.mask = _operand("mask", self.mask, (r.M, -(-C // 32)), _INT, device)
+        if self.mask_row is not None:
+            r.mask_row = _operand("mask_row", self.mask_row, (n,), _INT, device)
+        if self.temp is not None:
+            r.temp = _operand("temp", self.temp, (n,), _FLOAT, device)
+        return r
 
 
 def adjust_workspace_bytes(n: int, C: int) -> int:
@@ -717,13 +735,11 @@ def adjust_logits(ctx: Context, rules: LogitRules, z: torch.Tensor, out: Optiona
                   best: Optional[torch.Tensor], lse: Optional[torch.Tensor], ws: torch.Tensor) -> None:
     """cavs_adjust_logits (asynchronous): out [n, C] (may be z), best [n] int32,
     lse [n] float32; what is None is not written."""
-    dev = ctx.torch_device
-    if not isinstance(z, torch.Tensor) or z.dim() != 2:
-        raise CavsError(ERR_ARG, "z: a matrix is required")
-    n, C = int(z.shape[0]), int(z.shape[1])
+    dev, C = ctx.torch_device, _columns("z", z)
+    n = int(z.shape[0])
     pz = _operand("z", z, (n, C), _TYPES, dev)
     po = None if out is None else _operand("out", out, (n, C), _TYPES, dev)
     r = rules.raw(n, C, _TYPES[z.dtype], _TYPES[(z if out is None else out).dtype], dev)
-    ctx.check(lib().cavs_adjust_logits(
-        ctx._h, ct.byref(r), pz, po, None if best is None else _operand("best", best, (n,), (torch.int32,), dev),
-        None if lse is None else _operand("lse", lse, (n,), (torch.float32,), dev), *_workspace(ws, dev)))
+    pb = None if best is None else _operand("best", best, (n,), _INT, dev)
+    pl = None if lse is None else _operand("lse", lse, (n,), _FLOAT, dev)
+    ctx.check(lib().cavs_adjust_logits(ctx._h, ct.byref(r), pz, po, pb, pl, *_workspace(ws, dev)))

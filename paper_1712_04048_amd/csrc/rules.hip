@@ -14,7 +14,9 @@ namespace cavs {
 namespace {
 
 constexpr int kRulesMaxN = 1 << 20, kRulesMaxC = 1 << 20, kRulesMaxL = 1 << 20, kRulesMaxK = 1024;
-constexpr int kPer = 16;   // words of a thread
+// Words of a thread: 16, or 8 where pieces of 16 are too few to have eight on every CU
+// (64 x 50 001, every rule: 12.8 us with 16, 11.0 with 8; 256 x 128 000: 32 and 40).
+constexpr int kPer = 16, kPerFew = 8;
 
 struct RulesNet {
   int n, C, L, K, M, W32;   // W32 words of 32 bits to a mask
@@ -108,17 +110,17 @@ __device__ __forceinline__ void store_any(T* p, const float (&v)[V]) {
   }
 }
 
-// A workgroup takes a piece, kPer words a thread of one row, a thread vectors of V
+// A workgroup takes a piece, PER words a thread of one row, a thread vectors of V
 // adjacent ones, 16 bytes of the narrower type.  Everything that it reads is asked for
 // before anything is waited for.  Counts of the words so far and sums of the row's
 // own biases are kept in LDS for the piece's words alone; whole numbers and a fixed
 // order, so that no run differs.  Each wavefront leaves its largest v and its sum.
 // (Workgroups that go through pieces and ask for the next one ahead were slower: 256
 // x 128 000 in bf16 49 us, 39 with one for each piece.)
-template <class Z, class O, int THREADS>
+template <class Z, class O, int THREADS, int PER>
 __global__ void __launch_bounds__(THREADS) k_rules(RulesNet a, int row0, const Z* z, O* out) {
 #pragma clang fp contract(off)
-  constexpr int SEG = THREADS * kPer, V = sizeof(Z) == 4 && sizeof(O) == 4 ? 4 : 8, NV = kPer / V, W = THREADS / 64;
+  constexpr int SEG = THREADS * PER, V = sizeof(Z) == 4 && sizeof(O) == 4 ? 4 : 8, NV = PER / V, W = THREADS / 64;
   extern __shared__ uint4 lds[];
   __shared__ float4 parts[W];
   const int tid = threadIdx.x, row = row0 + blockIdx.x / a.segs, c0 = blockIdx.x % a.segs * SEG;
@@ -178,11 +180,14 @@ __global__ void __launch_bounds__(THREADS) k_rules(RulesNet a, int row0, const Z
       if ((unsigned)(w - c0) >= (unsigned)len) continue;
       // the first of a word's places adds all of them
       bool first = true;
-      for (int j = 0; j < i; ++j) first &= word[j] != w;
-      if (!first) continue;
       float s = extra[i];
-      for (int j = i + 1; j < a.K; ++j)
-        if (word[j] == w) s += extra[j];
+#pragma unroll 8
+      for (int j = 0; j < a.K; ++j) {
+        const bool same = word[j] == w;
+        first &= !same || j >= i;
+        s = same && j > i ? s + extra[j] : s;
+      }
+      if (!first) continue;
       own[w - c0] = s;
     }
     if (bad) a.err[1] = 1;
@@ -312,7 +317,7 @@ cavs_status rules_args(cavs_ctx* ctx, const cavs_rules* r) {
 
 size_t adjust_ws_bytes(int n, int C) {
   if (n < 0 || C <= 0 || n > kRulesMaxN || C > kRulesMaxC) return 0;
-  return std::max<size_t>(256, (size_t)n * cdiv(C, 256 * kPer) * 4 * sizeof(float4));
+  return std::max<size_t>(256, (size_t)n * cdiv(C, 256 * kPerFew) * 4 * sizeof(float4));
 }
 
 cavs_status adjust_run(cavs_ctx* ctx, const cavs_rules* r, const void* z, void* out, int* best, float* lse,
@@ -348,14 +353,16 @@ cavs_status adjust_run(cavs_ctx* ctx, const cavs_rules* r, const void* z, void* 
   a.part = (float4*)ws;
   // a row of up to 16 384 words in one workgroup, without a join
   const bool wide = r->C <= 1024 * kPer && r->C > 256 * kPer && !(a.past && a.K);
-  a.segs = cdiv(r->C, (wide ? 1024 : 256) * kPer);
+  const int threads = wide ? 1024 : 256;
+  const bool few = !wide && (long)r->n * cdiv(r->C, 256 * kPer) < 2048 && r->C > 256 * kPer;
+  const int per = few ? kPerFew : kPer;
+  a.segs = cdiv(r->C, threads * per);
   a.err = ctx->dev_err_dev;
   if ((best || lse) && a.segs > 1) {
     if (!ws || ws_bytes < need) return fail(ctx, CAVS_ERR_WORKSPACE, "workspace too small: %zu < %zu", ws_bytes, need);
     if (((uintptr_t)ws & 15) != 0) return fail(ctx, CAVS_ERR_ARG, "ws must be aligned to 16 bytes");
   }
-  const int threads = wide ? 1024 : 256;
-  const size_t shmem = (size_t)threads * kPer * 4 * ((a.past ? 1 : 0) + (a.K ? 1 : 0)) + 8 * (size_t)a.K;
+  const size_t shmem = (size_t)threads * per * 4 * ((a.past ? 1 : 0) + (a.K ? 1 : 0)) + 8 * (size_t)a.K;
   // a launch has fewer than 2^32 threads
   const int step = std::max(1, (int)std::min<long>(r->n, (1l << 30) / threads / a.segs));
   for (int i = 0; i < r->n; i += step) {
@@ -363,15 +370,14 @@ cavs_status adjust_run(cavs_ctx* ctx, const cavs_rules* r, const void* z, void* 
     auto go = [&](auto zt, auto ot) {
       using Z = decltype(zt);
       using O = decltype(ot);
-      if (wide && shmem > 64 << 10)
-        (void)hipFuncSetAttribute((const void*)k_rules<Z, O, 1024>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                                  (int)shmem);
-      if (wide)
-        CAVS_LAUNCH("k_rules<1024>", (k_rules<Z, O, 1024>), grid, dim3(1024), shmem, ctx->stream, a, i, (const Z*)z,
-                    (O*)out);
-      else
-        CAVS_LAUNCH("k_rules<256>", (k_rules<Z, O, 256>), grid, dim3(256), shmem, ctx->stream, a, i, (const Z*)z,
-                    (O*)out);
+      auto launch = [&](const char* name, auto kernel) {
+        if (shmem > 64 << 10)
+          (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)shmem);
+        CAVS_LAUNCH(name, kernel, grid, dim3(threads), shmem, ctx->stream, a, i, (const Z*)z, (O*)out);
+      };
+      if (wide) launch("k_rules<1024, 16>", k_rules<Z, O, 1024, kPer>);
+      else if (few) launch("k_rules<256, 8>", k_rules<Z, O, 256, kPerFew>);
+      else launch("k_rules<256, 16>", k_rules<Z, O, 256, kPer>);
     };
     if (zs == 2) os == 2 ? go(u16{}, u16{}) : go(u16{}, float{});
     else os == 2 ? go(float{}, u16{}) : go(float{}, float{});
