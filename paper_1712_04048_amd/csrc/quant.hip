@@ -47,92 +47,157 @@ __device__ __forceinline__ u16 round_twice(double v) {
   return f2bf(f);
 }
 
-// The code of w: the whole number nearest to (w - m) / s, the even one of two, in
-// -8 .. 7.  t is off by a few roundings (of 1 / s, of the difference and of the
-// product: `near` bounds them), so what is that close to a border is divided in 64
-// bits, where every such quotient of a float less a bf16 and a bf16 falls on the
-// right side.
-__device__ __forceinline__ int quant_code(float w, float s, float m, float inv, float near) {
-  const float t = (w - m) * inv, r = rintf(t);
-  float q = r;
-  if (!(fabsf(fabsf(t - r) - 0.5f) > near)) q = (float)rint(((double)w - (double)m) / (double)s);
-  return (int)fminf(fmaxf(q, -8.f), 7.f);
+// The whole number nearest to (w - m) / s, the even one of two, in -8 .. 7, by the
+// definition: where fp32 does not hold 1 / s, or what is multiplied with it.
+__device__ __noinline__ float quant_code_wide(float w, float s, float m) {
+  return fminf(fmaxf((float)rint(((double)w - (double)m) / (double)s), -8.f), 7.f);
 }
 
-// 64 columns of a block of 128 rows to a workgroup: wavefront b has rows 32 b ..
-// of them in registers, so that W is read once; groups of more than 32 rows join
-// their ends through LDS.  The dwords are turned into the layout's order in LDS.
-// Bound by memory: W once in, 4 bits a weight out.
-template <class T, int G, bool SHIFT>
-__global__ void __launch_bounds__(256) k_quant_pack(QuantNet q, const T* __restrict__ W, uint4* code,
-                                                    u16* scale) {
-  __shared__ float ends[2][4][64];
-  __shared__ uint32_t dw[4][4][4][16];   // [tile][j][column][b], 16 bytes a lane of the layout
-  const int lane = threadIdx.x & 63, b = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kb = blockIdx.y, c = blockIdx.x * 64 + lane, k0 = kb * kQB + 32 * b;
-  const int rows = min(32, q.H - k0);   // may be negative
-  const bool in = c < q.C;
-  float w[32];
+// The same for a scale well inside fp32's range, inv = 1 / s.  d = w - m is rounded
+// once, which leaves it on its side of each border b s (b half way between two codes):
+// b s is a float of at most 13 bits.  t2 is d / s rounded once (a quotient within two
+// steps of it, corrected by its own remainder, which the fused product has exactly);
+// a float d other than b s is at least 2^-23 / (its mantissa) of b s away from it, more
+// than half a step of t2 at b, so t2 is b for d = b s alone.  With m = 0 d is w and
+// the even one is right; with a shift d may have been rounded to b s, and w - m, which
+// 64 bits hold, decides.
+template <bool SHIFT>
+__device__ __forceinline__ float quant_code(float w, float s, float m, float inv) {
+  const float d = SHIFT ? w - m : w, t = d * inv, t2 = fmaf(fmaf(-t, s, d), inv, t);
+  float q = rintf(t2);
+  if (SHIFT && fabsf(t2 - q) == 0.5f) {
+    const double over = fma(-(double)t2, (double)s, (double)w - (double)m);
+    if (over != 0.0) q = (over > 0.0) == (s > 0.f) ? t2 + 0.5f : t2 - 0.5f;
+  }
+  return __builtin_amdgcn_fmed3f(q, -8.f, 7.f);
+}
+
+// Eight codes plus 8 in the order of a dword: the even places are nibbles 0 .. 3, the
+// odd ones 4 .. 7, summed as floats, which hold four of them; 8 in each is 0x8888.
+template <bool SHIFT>
+__device__ __forceinline__ uint32_t quant_codes(const float (&w)[8], float s, float m, float inv) {
+  float q[8];
+  if (fabsf(s) > 0x1p-100f && fabsf(s) < 0x1p100f) {
 #pragma unroll
-  for (int i = 0; i < 32; ++i) w[i] = in && i < rows ? load_one(W + (size_t)(k0 + i) * q.C + c) : 0.f;
-  float lo = INFINITY, hi = -INFINITY;
-  bool fine = true;
+    for (int i = 0; i < 8; ++i) q[i] = quant_code<SHIFT>(w[i], s, m, inv);
+  } else {
 #pragma unroll
-  for (int i = 0; i < 32; ++i)
-    if (i < rows) {
-      lo = fminf(lo, w[i]);
-      hi = fmaxf(hi, w[i]);
-      fine &= fabsf(w[i]) < INFINITY;
-    }
-  if (!fine) lo = -INFINITY, hi = INFINITY;
-  if (G > 32) {
-    ends[0][b][lane] = lo;
-    ends[1][b][lane] = hi;
-    __syncthreads();
-    const int b0 = b & ~(G / 32 - 1);
+    for (int i = 0; i < 8; ++i) q[i] = quant_code_wide(w[i], s, m);
+  }
+  const float even = fmaf(fmaf(fmaf(q[6], 16.f, q[4]), 16.f, q[2]), 16.f, q[0]) + 34952.f;
+  const float odd = fmaf(fmaf(fmaf(q[7], 16.f, q[5]), 16.f, q[3]), 16.f, q[1]) + 34952.f;
+  return (uint32_t)even | (uint32_t)odd << 16;
+}
+
+// NC adjacent elements at any address that is aligned to them, as they are in memory.
+template <class T, int NC>
+struct Columns {
+  typedef T type __attribute__((ext_vector_type(NC), aligned(sizeof(T))));
+};
+template <class T>
+struct Columns<T, 1> {
+  typedef T type;
+};
+template <class T, int NC>
+__device__ __forceinline__ float column(const typename Columns<T, NC>::type& v, int n) {
+  T x;
+  if constexpr (NC == 1) x = v;
+  else x = v[n];
+  if constexpr (sizeof(T) == 4) return x;
+  else return bf2f(x);
+}
+
+// 64 NC columns of a block of 128 rows to a workgroup, NC adjacent ones to a lane and
+// sixteen rows to a wavefront, in registers, so that W is read once; a group's ends
+// are joined through LDS.  The dwords are put into the layout's order in LDS.
+// Bound by memory: W once in, 4 bits a weight out.  What it reaches depends on how
+// much of a row a load takes: 1024 x 50 001 in bf16, groups of 64 with shifts, 101 us
+// with a column a lane.
+template <class T, int G, bool SHIFT, int NC>
+__global__ void __launch_bounds__(512) k_quant_pack(QuantNet q, const T* __restrict__ W, uint4* code, u16* scale) {
+  constexpr int CW = 64 * NC, GW = G / 16;   // columns; wavefronts of a group
+  __shared__ float ends[2][8][CW];
+  __shared__ uint32_t dw[4][4 * NC][4][16];   // [b][tile][j][column]
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kb = blockIdx.y, l0 = lane * NC, c0 = blockIdx.x * CW + l0, k0 = kb * kQB + 16 * w;
+  const int rows = min(16, q.H - k0);   // may be negative
+  typedef typename Columns<T, NC>::type Row;
+  Row x[16];
+  if (c0 + NC <= q.C) {
 #pragma unroll
-    for (int i = 0; i < G / 32; ++i) {
-      lo = fminf(lo, ends[0][b0 + i][lane]);
-      hi = fmaxf(hi, ends[1][b0 + i][lane]);
+    for (int i = 0; i < 16; ++i)
+      if (i < rows) x[i] = *reinterpret_cast<const Row*>(W + (size_t)(k0 + i) * q.C + c0);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      x[i] = Row{};
+      if constexpr (NC > 1)
+#pragma unroll
+        for (int n = 0; n < NC; ++n)
+          if (i < rows && c0 + n < q.C) x[i][n] = W[(size_t)(k0 + i) * q.C + c0 + n];
     }
   }
-  u16 s16 = 0, m16 = 0;
-  if (in && lo <= hi) {   // the group has rows
-    if (hi == INFINITY) {
-      s16 = 0x7fc0;
-    } else if (SHIFT) {
-      s16 = round_twice(((double)hi - (double)lo) / 15.0);
-      m16 = round_twice(0.5 * ((double)lo + (double)hi) + 0.5 * (double)bf2f(s16));
-    } else {
-      // the end that is further from 0 (the lower of two alike) becomes -8
-      s16 = f2bf(-0.125f * (hi > -lo ? hi : lo));
-    }
-  }
-  const float s = bf2f(s16), m = SHIFT ? bf2f(m16) : 0.f, inv = 1.f / s;
-  const float near = 1e-5f + fabsf(m * inv) * 0x1p-21f;
-  const bool some = s != 0.f && s == s;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    uint32_t d = 0;
+  for (int n = 0; n < NC; ++n) {
+    float lo = INFINITY, hi = -INFINITY, odd = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int v = some && 8 * j + i < rows ? quant_code(w[8 * j + i], s, m, inv, near) + 8 : 8;
-      d |= (uint32_t)v << (4 * (i & 1 ? 4 + i / 2 : i / 2));
-    }
-    dw[lane >> 4][j][b][lane & 15] = d;
-  }
-  constexpr int NS = kQB / G, W16 = NS * (SHIFT ? 2 : 1);
-  const int tile = blockIdx.x * 4 + (lane >> 4);
-  if (tile < q.T && (b & (G / 32 - 1)) == 0) {
-    u16* at = scale + (((size_t)tile * q.KB + kb) * 16 + (lane & 15)) * W16 + b / (G / 32) * (SHIFT ? 2 : 1);
-    at[0] = s16;
-    if (SHIFT) at[1] = m16;
+    for (int i = 0; i < 16; ++i)
+      if (i < rows) {
+        const float v = column<T, NC>(x[i], n);
+        lo = fminf(lo, v);
+        hi = fmaxf(hi, v);
+        odd = fmaf(v, 0.f, odd);   // NaN where v is not finite
+      }
+    ends[0][w][l0 + n] = odd == 0.f ? lo : -INFINITY;
+    ends[1][w][l0 + n] = odd == 0.f ? hi : INFINITY;
   }
   __syncthreads();
-  const int t = threadIdx.x >> 6, j = lane >> 4, col = lane & 15;
-  if (blockIdx.x * 4 + t < q.T)
-    code[((size_t)(blockIdx.x * 4 + t) * q.KB + kb) * 64 + lane] =
-        make_uint4(dw[t][j][0][col], dw[t][j][1][col], dw[t][j][2][col], dw[t][j][3][col]);
+  const int w0 = w & ~(GW - 1), tile0 = blockIdx.x * 4 * NC;
+#pragma unroll
+  for (int n = 0; n < NC; ++n) {
+    float lo = INFINITY, hi = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < GW; ++i) {
+      lo = fminf(lo, ends[0][w0 + i][l0 + n]);
+      hi = fmaxf(hi, ends[1][w0 + i][l0 + n]);
+    }
+    u16 s16 = 0, m16 = 0;
+    if (c0 + n < q.C && lo <= hi) {   // the group has rows
+      if (hi == INFINITY) {
+        s16 = 0x7fc0;
+      } else if (SHIFT) {
+        s16 = round_twice(((double)hi - (double)lo) / 15.0);
+        m16 = round_twice(0.5 * ((double)lo + (double)hi) + 0.5 * (double)bf2f(s16));
+      } else {
+        // the end that is further from 0 (the lower of two alike) becomes -8
+        s16 = f2bf(-0.125f * (hi > -lo ? hi : lo));
+      }
+    }
+    const float s = bf2f(s16), m = SHIFT ? bf2f(m16) : 0.f, inv = 1.f / s;
+    const bool some = s != 0.f && s == s;
+#pragma unroll
+    for (int jj = 0; jj < 2; ++jj) {
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = 8 * jj + i < rows ? column<T, NC>(x[8 * jj + i], n) : m;
+      const uint32_t d = some ? quant_codes<SHIFT>(v, s, m, inv) : 0x88888888u;
+      dw[w / 2][(l0 + n) / 16][w % 2 * 2 + jj][(l0 + n) % 16] = d;
+    }
+    const int tile = tile0 + (l0 + n) / 16;
+    if (tile < q.T && w == w0) {
+      constexpr int W16 = kQB / G * (SHIFT ? 2 : 1);
+      u16* at = scale + (((size_t)tile * q.KB + kb) * 16 + (l0 + n) % 16) * W16 + w / GW * (SHIFT ? 2 : 1);
+      at[0] = s16;
+      if (SHIFT) at[1] = m16;
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 4 * NC * 64; i += 512) {
+    const int tile = i / 64, at = i % 64;
+    if (tile0 + tile < q.T)
+      code[((size_t)(tile0 + tile) * q.KB + kb) * 64 + at] =
+          make_uint4((&dw[0][tile][0][0])[at], (&dw[1][tile][0][0])[at], (&dw[2][tile][0][0])[at], (&dw[3][tile][0][0])[at]);
+  }
 }
 
 // What in rows: the same split, a dword of eight rows at a time.
@@ -453,8 +518,14 @@ cavs_status quant_pack_run(cavs_ctx* ctx, const cavs_quant* q, int w_type, const
   by_group(q, [&](auto g, auto shift) {
     by_element(w_type, [&](auto t) {
       using T = decltype(t);
-      CAVS_LAUNCH("k_quant_pack", (k_quant_pack<T, g(), shift()>), dim3(cdiv(n.T, 4), n.KB), dim3(256), 0,
-                  ctx->stream, n, (const T*)W, (uint4*)data, (u16*)((char*)data + code_bytes(q)));
+      auto launch = [&](auto nc) {
+        CAVS_LAUNCH("k_quant_pack", (k_quant_pack<T, g(), shift(), nc()>), dim3(cdiv(n.C, 64 * nc()), n.KB), dim3(512),
+                    0, ctx->stream, n, (const T*)W, (uint4*)data, (u16*)((char*)data + code_bytes(q)));
+      };
+      const int nc = (long)cdiv(n.C, 256) * n.KB >= 512 ? 4 : (long)cdiv(n.C, 128) * n.KB >= 512 ? 2 : 1;
+      if (nc == 4) launch(std::integral_constant<int, 4>{});
+      else if (nc == 2) launch(std::integral_constant<int, 2>{});
+      else launch(std::integral_constant<int, 1>{});
     });
   });
   CAVS_LAUNCH_CHECK(ctx);
