@@ -14,6 +14,7 @@
 #include <algorithm>
 
 #include "vocab.h"
+#include "xcd_map.h"
 
 namespace cavs {
 namespace {
@@ -89,122 +90,94 @@ __device__ __forceinline__ uint32_t quant_codes(const float (&w)[8], float s, fl
   return (uint32_t)even | (uint32_t)odd << 16;
 }
 
-// NC adjacent elements at any address that is aligned to them, as they are in memory.
-template <class T, int NC>
-struct Columns {
-  typedef T type __attribute__((ext_vector_type(NC), aligned(sizeof(T))));
-};
-template <class T>
-struct Columns<T, 1> {
-  typedef T type;
-};
-template <class T, int NC>
-__device__ __forceinline__ float column(const typename Columns<T, NC>::type& v, int n) {
-  T x;
-  if constexpr (NC == 1) x = v;
-  else x = v[n];
-  if constexpr (sizeof(T) == 4) return x;
-  else return bf2f(x);
-}
-
-// 64 NC columns of a block of 128 rows to a workgroup, NC adjacent ones to a lane and
-// sixteen rows to a wavefront, in registers, so that W is read once; a group's ends
-// are joined through LDS.  The dwords are put into the layout's order in LDS.
-// Bound by memory: W once in, 4 bits a weight out.  What it reaches depends on how
-// much of a row a load takes: 1024 x 50 001 in bf16, groups of 64 with shifts, 101 us
-// with a column a lane.
-template <class T, int G, bool SHIFT, int NC>
+// 64 columns of a block of 128 rows to a workgroup, sixteen rows to a wavefront, in
+// registers, so that W is read once; a group's ends are joined through LDS, and the
+// dwords are put into the layout's order there.  Bound by memory: W once in, 4 bits a
+// weight out.  Each XCD takes adjacent columns: rows of any length then share the
+// lines at a workgroup's ends in its cache (1024 x 50 001: bf16 with shifts 42 us with
+// neighbours on other XCDs and 35 here, 3.8 TB/s; fp32 86 and 71).  Two or four
+// columns a lane were no faster (38 and 48).
+template <class T, int G, bool SHIFT>
 __global__ void __launch_bounds__(512) k_quant_pack(QuantNet q, const T* __restrict__ W, uint4* code, u16* scale) {
-  constexpr int CW = 64 * NC, GW = G / 16;   // columns; wavefronts of a group
-  __shared__ float ends[2][8][CW];
-  __shared__ uint32_t dw[4][4 * NC][4][16];   // [b][tile][j][column]
+  constexpr int GW = G / 16;   // wavefronts of a group
+  __shared__ float ends[2][8][64];
+  __shared__ uint32_t dw[4][4][4][16];   // [b][tile][j][column]
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kb = blockIdx.y, l0 = lane * NC, c0 = blockIdx.x * CW + l0, k0 = kb * kQB + 16 * w;
+  const int nx = cdiv_dev(q.C, 64), item = xcd_item(blockIdx.x, nx * q.KB);
+  if (item < 0) return;
+  const int kb = item / nx, bx = item - kb * nx, c = bx * 64 + lane, k0 = kb * kQB + 16 * w;
   const int rows = min(16, q.H - k0);   // may be negative
-  typedef typename Columns<T, NC>::type Row;
-  Row x[16];
-  if (c0 + NC <= q.C) {
+  const bool in = c < q.C;
+  // past the last row it again, which changes no group's ends
+  float x[16];
+  if (in) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (i < rows) x[i] = *reinterpret_cast<const Row*>(W + (size_t)(k0 + i) * q.C + c0);
+    for (int i = 0; i < 16; ++i) x[i] = load_one(W + (size_t)min(k0 + i, q.H - 1) * q.C + c);
   } else {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      x[i] = Row{};
-      if constexpr (NC > 1)
+    for (int i = 0; i < 16; ++i) x[i] = 0.f;
+  }
+  float lo = INFINITY, hi = -INFINITY, odd = 0.f;
 #pragma unroll
-        for (int n = 0; n < NC; ++n)
-          if (i < rows && c0 + n < q.C) x[i][n] = W[(size_t)(k0 + i) * q.C + c0 + n];
+  for (int i = 0; i < 16; ++i) {
+    lo = fminf(lo, x[i]);
+    hi = fmaxf(hi, x[i]);
+    odd = fmaf(x[i], 0.f, odd);   // NaN where one is not finite
+  }
+  ends[0][w][lane] = odd == 0.f ? lo : -INFINITY;
+  ends[1][w][lane] = odd == 0.f ? hi : INFINITY;
+  __syncthreads();
+  const int w0 = w & ~(GW - 1), tile = bx * 4 + lane / 16;
+#pragma unroll
+  for (int i = 0; i < GW; ++i) {
+    lo = fminf(lo, ends[0][w0 + i][lane]);
+    hi = fmaxf(hi, ends[1][w0 + i][lane]);
+  }
+  u16 s16 = 0, m16 = 0;
+  if (in && kb * kQB + 16 * w0 < q.H) {   // the group has rows
+    if (hi == INFINITY) {
+      s16 = 0x7fc0;
+    } else if (SHIFT) {
+      s16 = round_twice(((double)hi - (double)lo) / 15.0);
+      m16 = round_twice(0.5 * ((double)lo + (double)hi) + 0.5 * (double)bf2f(s16));
+    } else {
+      // the end that is further from 0 (the lower of two alike) becomes -8
+      s16 = f2bf(-0.125f * (hi > -lo ? hi : lo));
     }
   }
+  const float s = bf2f(s16), m = SHIFT ? bf2f(m16) : 0.f, inv = 1.f / s;
+  if (rows < 16)
 #pragma unroll
-  for (int n = 0; n < NC; ++n) {
-    float lo = INFINITY, hi = -INFINITY, odd = 0.f;
+    for (int i = 0; i < 16; ++i) x[i] = i < rows ? x[i] : m;
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (i < rows) {
-        const float v = column<T, NC>(x[i], n);
-        lo = fminf(lo, v);
-        hi = fmaxf(hi, v);
-        odd = fmaf(v, 0.f, odd);   // NaN where v is not finite
-      }
-    ends[0][w][l0 + n] = odd == 0.f ? lo : -INFINITY;
-    ends[1][w][l0 + n] = odd == 0.f ? hi : INFINITY;
+  for (int jj = 0; jj < 2; ++jj) {
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = x[8 * jj + i];
+    dw[w / 2][lane / 16][w % 2 * 2 + jj][lane % 16] =
+        s != 0.f && s == s ? quant_codes<SHIFT>(v, s, m, inv) : 0x88888888u;
+  }
+  if (tile < q.T && w == w0) {
+    constexpr int W16 = kQB / G * (SHIFT ? 2 : 1);
+    u16* at = scale + (((size_t)tile * q.KB + kb) * 16 + lane % 16) * W16 + w / GW * (SHIFT ? 2 : 1);
+    at[0] = s16;
+    if (SHIFT) at[1] = m16;
   }
   __syncthreads();
-  const int w0 = w & ~(GW - 1), tile0 = blockIdx.x * 4 * NC;
-#pragma unroll
-  for (int n = 0; n < NC; ++n) {
-    float lo = INFINITY, hi = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < GW; ++i) {
-      lo = fminf(lo, ends[0][w0 + i][l0 + n]);
-      hi = fmaxf(hi, ends[1][w0 + i][l0 + n]);
-    }
-    u16 s16 = 0, m16 = 0;
-    if (c0 + n < q.C && lo <= hi) {   // the group has rows
-      if (hi == INFINITY) {
-        s16 = 0x7fc0;
-      } else if (SHIFT) {
-        s16 = round_twice(((double)hi - (double)lo) / 15.0);
-        m16 = round_twice(0.5 * ((double)lo + (double)hi) + 0.5 * (double)bf2f(s16));
-      } else {
-        // the end that is further from 0 (the lower of two alike) becomes -8
-        s16 = f2bf(-0.125f * (hi > -lo ? hi : lo));
-      }
-    }
-    const float s = bf2f(s16), m = SHIFT ? bf2f(m16) : 0.f, inv = 1.f / s;
-    const bool some = s != 0.f && s == s;
-#pragma unroll
-    for (int jj = 0; jj < 2; ++jj) {
-      float v[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = 8 * jj + i < rows ? column<T, NC>(x[8 * jj + i], n) : m;
-      const uint32_t d = some ? quant_codes<SHIFT>(v, s, m, inv) : 0x88888888u;
-      dw[w / 2][(l0 + n) / 16][w % 2 * 2 + jj][(l0 + n) % 16] = d;
-    }
-    const int tile = tile0 + (l0 + n) / 16;
-    if (tile < q.T && w == w0) {
-      constexpr int W16 = kQB / G * (SHIFT ? 2 : 1);
-      u16* at = scale + (((size_t)tile * q.KB + kb) * 16 + (l0 + n) % 16) * W16 + w / GW * (SHIFT ? 2 : 1);
-      at[0] = s16;
-      if (SHIFT) at[1] = m16;
-    }
-  }
-  __syncthreads();
-  for (int i = threadIdx.x; i < 4 * NC * 64; i += 512) {
-    const int tile = i / 64, at = i % 64;
-    if (tile0 + tile < q.T)
-      code[((size_t)(tile0 + tile) * q.KB + kb) * 64 + at] =
-          make_uint4((&dw[0][tile][0][0])[at], (&dw[1][tile][0][0])[at], (&dw[2][tile][0][0])[at], (&dw[3][tile][0][0])[at]);
-  }
+  const int t = threadIdx.x / 64;
+  if (t < 4 && bx * 4 + t < q.T)
+    code[((size_t)(bx * 4 + t) * q.KB + kb) * 64 + lane] =
+        make_uint4((&dw[0][t][0][0])[lane], (&dw[1][t][0][0])[lane], (&dw[2][t][0][0])[lane], (&dw[3][t][0][0])[lane]);
 }
 
-// What in rows: the same split, a dword of eight rows at a time.
+// What in rows, a dword of eight rows at a time; XCDs as above (1024 x 50 001 bf16: 44
+// and 27 us).
 template <class T, int G, bool SHIFT>
 __global__ void __launch_bounds__(256) k_quant_unpack(QuantNet q, T* W) {
   const int lane = threadIdx.x & 63, b = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kb = blockIdx.y, c = blockIdx.x * 64 + lane, k0 = kb * kQB + 32 * b;
+  const int nx = cdiv_dev(q.C, 64), item = xcd_item(blockIdx.x, nx * q.KB);
+  if (item < 0) return;
+  const int kb = item / nx, c = (item - kb * nx) * 64 + lane, k0 = kb * kQB + 32 * b;
   if (c >= q.C) return;
   constexpr int W16 = kQB / G * (SHIFT ? 2 : 1);
   const size_t block = (size_t)(c >> 4) * q.KB + kb;
@@ -518,14 +491,8 @@ cavs_status quant_pack_run(cavs_ctx* ctx, const cavs_quant* q, int w_type, const
   by_group(q, [&](auto g, auto shift) {
     by_element(w_type, [&](auto t) {
       using T = decltype(t);
-      auto launch = [&](auto nc) {
-        CAVS_LAUNCH("k_quant_pack", (k_quant_pack<T, g(), shift(), nc()>), dim3(cdiv(n.C, 64 * nc()), n.KB), dim3(512),
-                    0, ctx->stream, n, (const T*)W, (uint4*)data, (u16*)((char*)data + code_bytes(q)));
-      };
-      const int nc = (long)cdiv(n.C, 256) * n.KB >= 512 ? 4 : (long)cdiv(n.C, 128) * n.KB >= 512 ? 2 : 1;
-      if (nc == 4) launch(std::integral_constant<int, 4>{});
-      else if (nc == 2) launch(std::integral_constant<int, 2>{});
-      else launch(std::integral_constant<int, 1>{});
+      CAVS_LAUNCH("k_quant_pack", (k_quant_pack<T, g(), shift()>), dim3(xcd_grid(cdiv(n.C, 64) * n.KB)), dim3(512), 0,
+                  ctx->stream, n, (const T*)W, (uint4*)data, (u16*)((char*)data + code_bytes(q)));
     });
   });
   CAVS_LAUNCH_CHECK(ctx);
@@ -541,7 +508,7 @@ cavs_status quant_unpack_run(cavs_ctx* ctx, const cavs_quant* q, int w_type, voi
   by_group(q, [&](auto g, auto shift) {
     by_element(w_type, [&](auto t) {
       using T = decltype(t);
-      CAVS_LAUNCH("k_quant_unpack", (k_quant_unpack<T, g(), shift()>), dim3(cdiv(n.T, 4), n.KB), dim3(256), 0,
+      CAVS_LAUNCH("k_quant_unpack", (k_quant_unpack<T, g(), shift()>), dim3(xcd_grid(cdiv(n.C, 64) * n.KB)), dim3(256), 0,
                   ctx->stream, n, (T*)W);
     });
   });
