@@ -8,26 +8,40 @@
 // once for the sum and once more to be scaled.
 #include <algorithm>
 #include <cmath>
+#include <iterator>
 
 #include "vocab.h"
 
 namespace cavs {
 namespace {
 
-constexpr int kSlots = 1024;    // workgroups of a launch, each with a partial sum
-constexpr int kSet = 120;       // gradients of a launch: their list is its argument
-constexpr int kChunk = 8192;    // elements that a workgroup takes at a time
+constexpr int kSlots = 1024;     // workgroups of a launch, each with a partial sum
+constexpr int kThreads = 512;
+constexpr int kChunk = kThreads * 8;   // elements that a workgroup takes at a time
+constexpr int kSet = 160;        // gradients whose list is an argument of a launch
+constexpr int kTable = 4096;     // gradients of a table in the workspace
 
-// Gradients of a launch; chunks[k] is the number of chunks up to and with the k-th.
+// Gradients of a launch; end[k]: chunks up to and with the k-th's.
 struct ClipSet {
   const void* g[kSet];
   void* out[kSet];
-  long long n[kSet];
-  uint32_t chunks[kSet];
-  uint32_t gbf[(kSet + 31) / 32], obf[(kSet + 31) / 32];
+  uint32_t n[kSet];    // 0: 2^32
+  uint32_t end[kSet];
+  uint32_t gbf[kSet / 32], obf[kSet / 32];
   int count;
 };
-static_assert(sizeof(ClipSet) <= 3584, "kernel arguments");
+static_assert(sizeof(ClipSet) <= 3968, "kernel arguments");
+
+// The same in the workspace, of all gradients, which the norm's launches leave for the
+// one that scales.
+struct ClipEntry {
+  const void* g;
+  void* out;
+  long long n;
+  uint32_t end, types;   // bit 0: g is bf16, 1: out is
+};
+
+__device__ __forceinline__ long long clip_size(uint32_t n) { return n ? n : 1ll << 32; }
 
 // Vectors at any address that is aligned to its elements.
 template <class T, int V>
@@ -35,20 +49,26 @@ struct Vec {
   typedef T type __attribute__((ext_vector_type(V), aligned(sizeof(T))));
 };
 
+// Eight adjacent elements as they are in memory.
 template <class T>
-__device__ __forceinline__ void load8(const T* p, float (&v)[8]) {
-  if constexpr (sizeof(T) == 4) {
-    typedef typename Vec<float, 4>::type f4;
-    const f4 a = *reinterpret_cast<const f4*>(p), b = *reinterpret_cast<const f4*>(p + 4);
+struct Vec8 {
+  typedef typename Vec<T, 16 / sizeof(T)>::type part;
+  part x[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
-  } else {
-    typedef typename Vec<u16, 8>::type s8;
-    const s8 a = *reinterpret_cast<const s8*>(p);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float((uint32_t)a[i] << 16);
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) x[i] = reinterpret_cast<const part*>(p)[i];
   }
-}
+  __device__ __forceinline__ void floats(float (&v)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (sizeof(T) == 4) v[i] = x[i / 4][i % 4];
+      else v[i] = __uint_as_float((uint32_t)x[0][i] << 16);
+    }
+  }
+};
+__device__ __forceinline__ float one_float(float v) { return v; }
+__device__ __forceinline__ float one_float(u16 v) { return __uint_as_float((uint32_t)v << 16); }
+
 template <class T>
 __device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
   if constexpr (sizeof(T) == 4) {
@@ -73,123 +93,168 @@ __device__ __forceinline__ double wave_sum64(double v) {
 // The workgroup's sum, in every thread.
 __device__ __forceinline__ double group_sum64(double v, double* lds) {
   v = wave_sum64(v);
-  __syncthreads();
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
   __syncthreads();
-  return (lds[0] + lds[1]) + (lds[2] + lds[3]);
+  v = 0.0;
+#pragma unroll
+  for (int i = 0; i < kThreads / 64; ++i) v += lds[i];
+  return v;
 }
 
-// The gradient that a chunk belongs to: the number of those that end before it.
-__device__ __forceinline__ int clip_owner(const ClipSet& a, uint32_t chunk) {
-  const int lane = threadIdx.x & 63;
-  const bool b0 = lane < a.count && a.chunks[lane] <= chunk;
-  const bool b1 = 64 + lane < a.count && a.chunks[min(64 + lane, kSet - 1)] <= chunk;
-  return __popcll(__ballot(b0)) + __popcll(__ballot(b1));
+// f(v, i) of eight elements at a time, v their values, of [from, to); four steps'
+// loads are in flight where there are that many.
+template <class T, class F>
+__device__ __forceinline__ void clip_each(const T* g, long long from, long long to, F f) {
+  long long at = from;
+  const int mine = threadIdx.x * 8;
+  for (; at + 4 * kChunk <= to; at += 4 * kChunk) {
+    Vec8<T> x[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) x[u].load(g + at + u * kChunk + mine);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) f(x[u], at + u * kChunk + mine);
+  }
+  for (; at + kChunk <= to; at += kChunk) {
+    Vec8<T> x;
+    x.load(g + at + mine);
+    f(x, at + mine);
+  }
+  const long long i = at + mine;
+  if (i + 8 <= to) {
+    Vec8<T> x;
+    x.load(g + i);
+    f(x, i);
+  }
+}
+// Elements that are in none of those: fewer than eight, of one thread.
+template <class F>
+__device__ __forceinline__ void clip_rest(long long from, long long to, F f) {
+  const long long at = from + (to - from) / kChunk * kChunk + threadIdx.x * 8;
+  if (at < to && at + 8 > to)
+    for (long long i = at; i < to; ++i) f(i);
 }
 
 template <class T>
-__device__ __forceinline__ double clip_squares(const T* g, int n) {
-  double s = 0.0;
-  for (int i = threadIdx.x * 8; i < n; i += 256 * 8) {
-    if (i + 8 <= n) {
-      float v[8];
-      load8(g + i, v);
+__device__ __forceinline__ double clip_squares(const T* g, long long from, long long to) {
+  double s[4] = {};   // four sums: one would wait for itself
+  clip_each(g, from, to, [&](const Vec8<T>& x, long long) {
+    float v[8];
+    x.floats(v);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) s = fma((double)v[k], (double)v[k], s);
-    } else {
-      for (int k = i; k < n; ++k) {
-        float v;
-        if constexpr (sizeof(T) == 4) v = g[k];
-        else v = __uint_as_float((uint32_t)g[k] << 16);
-        s = fma((double)v, (double)v, s);
-      }
-    }
-  }
-  return s;
+    for (int k = 0; k < 8; ++k) s[k & 3] = fma((double)v[k], (double)v[k], s[k & 3]);
+  });
+  clip_rest(from, to, [&](long long i) {
+    const double v = one_float(g[i]);
+    s[0] = fma(v, v, s[0]);
+  });
+  return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
-// Workgroup b's share of the sum is added to slot b, or is its first value.
-__global__ void __launch_bounds__(256) k_clip_norm(ClipSet a, uint32_t total, int written, double* slots) {
-  __shared__ double lds[4];
+// Workgroup b's share of the sum, a run of chunks, is added to slot b or is its first
+// value.  The first workgroup writes the set's part of the table.
+__global__ void __launch_bounds__(kThreads) k_clip_norm(ClipSet a, uint32_t total, int written, uint32_t base,
+                                                        double* slots, ClipEntry* table) {
+  __shared__ double lds[kThreads / 64];
+  const int lane = threadIdx.x & 63;
+  if (table && blockIdx.x == 0)
+    for (int k = threadIdx.x; k < a.count; k += kThreads)
+      table[k] = ClipEntry{a.g[k], a.out[k], clip_size(a.n[k]), base + a.end[k],
+                           (a.gbf[k >> 5] >> (k & 31) & 1) | (a.obf[k >> 5] >> (k & 31) & 1) << 1};
+  if (!slots) return;
+  const uint32_t per = (total + gridDim.x - 1) / gridDim.x;
+  uint32_t c = blockIdx.x * per;
+  const uint32_t stop = min(c + per, total);
+  // the gradient of the first chunk: the number of those that end before it
+  int k = 0;
+#pragma unroll
+  for (int i = 0; i < kSet; i += 64)
+    k += __popcll(__ballot(i + lane < a.count && a.end[min(i + lane, kSet - 1)] <= c));
+  k = __builtin_amdgcn_readfirstlane(k);
   double s = 0.0;
-  for (uint32_t chunk = blockIdx.x; chunk < total; chunk += gridDim.x) {
-    const int k = __builtin_amdgcn_readfirstlane(clip_owner(a, chunk));
-    const long long at = (long long)(chunk - (k ? a.chunks[k - 1] : 0u)) * kChunk;
-    const int n = (int)min((long long)kChunk, a.n[k] - at);
-    s += a.gbf[k >> 5] >> (k & 31) & 1 ? clip_squares((const u16*)a.g[k] + at, n)
-                                       : clip_squares((const float*)a.g[k] + at, n);
+  for (; c < stop; ++k) {
+    const uint32_t first = k ? a.end[k - 1] : 0u, last = min(a.end[k], stop);
+    const long long from = (long long)(c - first) * kChunk;
+    const long long to = min((long long)(last - first) * kChunk, clip_size(a.n[k]));
+    s += a.gbf[k >> 5] >> (k & 31) & 1 ? clip_squares((const u16*)a.g[k], from, to)
+                                       : clip_squares((const float*)a.g[k], from, to);
+    c = last;
   }
   s = group_sum64(s, lds);
   if (threadIdx.x == 0) slots[blockIdx.x] = (int)blockIdx.x < written ? slots[blockIdx.x] + s : s;
 }
 
 template <class T, class O>
-__device__ __forceinline__ void clip_scale(const T* g, O* out, int n, float a, float f) {
-  for (int i = threadIdx.x * 8; i < n; i += 256 * 8) {
-    if (i + 8 <= n) {
-      float v[8];
-      load8(g + i, v);
+__device__ __forceinline__ void clip_scale(const T* g, O* out, long long from, long long to, float a, float f) {
+  clip_each(g, from, to, [&](const Vec8<T>& x, long long i) {
+    float v[8];
+    x.floats(v);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = v[k] * a * f;
-      store8(out + i, v);
-    } else {
-      for (int k = i; k < n; ++k) {
-        float v;
-        if constexpr (sizeof(T) == 4) v = g[k];
-        else v = __uint_as_float((uint32_t)g[k] << 16);
-        if constexpr (sizeof(O) == 4) out[k] = v * a * f;
-        else out[k] = f2bf(v * a * f);
-      }
-    }
-  }
+    for (int k = 0; k < 8; ++k) v[k] = v[k] * a * f;
+    store8(out + i, v);
+  });
+  clip_rest(from, to, [&](long long i) {
+    const float v = one_float(g[i]) * a * f;
+    if constexpr (sizeof(O) == 4) out[i] = v;
+    else out[i] = f2bf(v);
+  });
 }
 
-// Every workgroup adds up the slots by itself, in one order.  A norm that is not
-// finite clips nothing.
-__global__ void __launch_bounds__(256) k_clip_scale(ClipSet a, uint32_t total, int slots_n, const double* slots,
-                                                    float scale, float max_norm, float* norm_out) {
-  __shared__ double lds[4];
+// Every workgroup adds up the slots by itself, in one order, and scales a run of
+// chunks: the last ones first, which the norm read last and the cache still holds.  A
+// norm that is not finite clips nothing.
+__global__ void __launch_bounds__(kThreads) k_clip_scale(const ClipEntry* table, int count, uint32_t total, int slots_n,
+                                                         const double* slots, float scale, float max_norm,
+                                                         float* norm_out) {
+  __shared__ double lds[kThreads / 64];
+  const int lane = threadIdx.x & 63;
+  const uint32_t per = (total + gridDim.x - 1) / gridDim.x;
+  uint32_t c = (gridDim.x - 1 - blockIdx.x) * per;
+  const uint32_t stop = min(c + per, total);
+  // the gradient of the first chunk, first among 64 times 64
+  int k = 64 * __popcll(__ballot(64 * lane + 63 < count && table[min(64 * lane + 63, count - 1)].end <= c));
+  k += __popcll(__ballot(k + lane < count && table[min(k + lane, count - 1)].end <= c));
+  k = __builtin_amdgcn_readfirstlane(k);
   double s = 0.0;
-  for (int i = threadIdx.x; i < slots_n; i += 256) s += slots[i];
+  for (int i = threadIdx.x; i < slots_n; i += kThreads) s += slots[i];
   s = group_sum64(s, lds);
   const double norm = sqrt(s) * fabs((double)scale);
   if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
   const double factor = norm > (double)max_norm && norm < INFINITY ? (double)scale * ((double)max_norm / norm) : scale;
   // a factor that fp32 holds only as a subnormal is two: the first loses nothing
-  const float a2 = fabs(factor) < 0x1p-100 ? 0x1p-64f : 1.f, f = (float)(a2 == 1.f ? factor : factor * 0x1p64);
-  for (uint32_t chunk = blockIdx.x; chunk < total; chunk += gridDim.x) {
-    const int k = __builtin_amdgcn_readfirstlane(clip_owner(a, chunk));
-    const long long at = (long long)(chunk - (k ? a.chunks[k - 1] : 0u)) * kChunk;
-    const int n = (int)min((long long)kChunk, a.n[k] - at);
-    const bool gb = a.gbf[k >> 5] >> (k & 31) & 1, ob = a.obf[k >> 5] >> (k & 31) & 1;
-    if (a.out[k] == a.g[k] && factor == 1.0) continue;
-    if (gb) ob ? clip_scale((const u16*)a.g[k] + at, (u16*)a.out[k] + at, n, a2, f)
-               : clip_scale((const u16*)a.g[k] + at, (float*)a.out[k] + at, n, a2, f);
-    else ob ? clip_scale((const float*)a.g[k] + at, (u16*)a.out[k] + at, n, a2, f)
-            : clip_scale((const float*)a.g[k] + at, (float*)a.out[k] + at, n, a2, f);
+  const float a = fabs(factor) < 0x1p-100 ? 0x1p-64f : 1.f, f = (float)(a == 1.f ? factor : factor * 0x1p64);
+  for (; c < stop; ++k) {
+    const ClipEntry e = table[k];
+    const uint32_t first = k ? table[k - 1].end : 0u, last = min(e.end, stop);
+    const long long from = (long long)(c - first) * kChunk, to = min((long long)(last - first) * kChunk, e.n);
+    c = last;
+    if (!e.out || (e.out == e.g && factor == 1.0)) continue;
+    if (e.types & 1) e.types & 2 ? clip_scale((const u16*)e.g, (u16*)e.out, from, to, a, f)
+                                 : clip_scale((const u16*)e.g, (float*)e.out, from, to, a, f);
+    else e.types & 2 ? clip_scale((const float*)e.g, (u16*)e.out, from, to, a, f)
+                     : clip_scale((const float*)e.g, (float*)e.out, from, to, a, f);
   }
 }
 
 struct ClipFill {
   ClipSet set;
-  uint32_t total;
+  uint32_t total;   // its chunks
 };
-// The next set of gradients from `at` on; out: only those that are written.
-int clip_fill(const cavs_grad* grads, int count, int at, bool out, ClipFill& f) {
+// The next set of gradients from `at` on; returns where the one after it begins.
+int clip_fill(const cavs_grad* grads, int count, int at, ClipFill& f) {
   ClipSet& a = f.set;
   a.count = 0;
   f.total = 0;
-  for (uint32_t& w : a.gbf) w = 0;
-  for (uint32_t& w : a.obf) w = 0;
+  std::fill(std::begin(a.gbf), std::end(a.gbf), 0u);
+  std::fill(std::begin(a.obf), std::end(a.obf), 0u);
   for (; at < count && a.count < kSet; ++at) {
     const cavs_grad& g = grads[at];
-    if (g.n == 0 || (out && !g.out)) continue;
+    if (g.n == 0) continue;
     const int k = a.count++;
     a.g[k] = g.g;
     a.out[k] = g.out;
-    a.n[k] = g.n;
+    a.n[k] = (uint32_t)g.n;
     f.total += (uint32_t)((g.n + kChunk - 1) / kChunk);
-    a.chunks[k] = f.total;
+    a.end[k] = f.total;
     if (g.g_type == CAVS_T_BF16) a.gbf[k >> 5] |= 1u << (k & 31);
     if (g.out_type == CAVS_T_BF16) a.obf[k >> 5] |= 1u << (k & 31);
   }
@@ -198,7 +263,7 @@ int clip_fill(const cavs_grad* grads, int count, int at, bool out, ClipFill& f) 
 
 }  // namespace
 
-size_t clip_ws_bytes() { return kSlots * sizeof(double); }
+size_t clip_ws_bytes() { return kSlots * sizeof(double) + kTable * sizeof(ClipEntry); }
 
 cavs_status clip_run(cavs_ctx* ctx, const cavs_grad* grads, int count, float scale, float max_norm, float* norm,
                      void* ws, size_t ws_bytes) {
@@ -221,21 +286,61 @@ cavs_status clip_run(cavs_ctx* ctx, const cavs_grad* grads, int count, float sca
     return fail(ctx, CAVS_ERR_WORKSPACE, "workspace too small: %zu < %zu", ws_bytes, clip_ws_bytes());
   if (((uintptr_t)ws & 7) != 0) return fail(ctx, CAVS_ERR_ARG, "ws must be aligned to 8 bytes");
   double* slots = (double*)ws;
-  int written = 0;
+  ClipEntry* table = (ClipEntry*)(slots + kSlots);
   ClipFill f;
+  // a round of gradients that share a table: where it begins, its gradients and chunks
+  struct Round {
+    int from, entries;
+    uint32_t chunks;
+  };
+  auto fits = [&](const Round& r) { return r.entries + f.set.count <= kTable && r.chunks + (uint64_t)f.total < 1u << 31; };
+  int written = 0;
+  Round first{0, 0, 0};
+  bool open = true;   // the first round takes this set
+  int second = count;
   for (int at = 0; at < count;) {
-    at = clip_fill(grads, count, at, false, f);
+    const int from = at;
+    at = clip_fill(grads, count, at, f);
     if (f.total == 0) continue;
+    if (open && !fits(first)) {
+      open = false;
+      second = from;
+    }
     const int blocks = (int)std::min<uint32_t>(f.total, kSlots);
-    CAVS_LAUNCH("k_clip_norm", k_clip_norm, dim3(blocks), dim3(256), 0, ctx->stream, f.set, f.total, written, slots);
+    CAVS_LAUNCH("k_clip_norm", k_clip_norm, dim3(blocks), dim3(kThreads), 0, ctx->stream, f.set, f.total, written,
+                first.chunks, slots, open ? table + first.entries : nullptr);
     written = std::max(written, blocks);
+    if (open) {
+      first.entries += f.set.count;
+      first.chunks += f.total;
+    }
   }
-  int at = 0;
-  for (bool first = true; first || at < count; first = false) {
-    at = clip_fill(grads, count, at, true, f);
-    if (!first && f.total == 0) continue;
-    CAVS_LAUNCH("k_clip_scale", k_clip_scale, dim3(std::max(1u, std::min<uint32_t>(f.total, 2 * kSlots))), dim3(256), 0,
-                ctx->stream, f.set, f.total, written, (const double*)slots, scale, max_norm, first ? norm : nullptr);
+  auto scaled = [&](const Round& r, float* to) {
+    CAVS_LAUNCH("k_clip_scale", k_clip_scale, dim3(std::max(1u, std::min<uint32_t>(r.chunks, kSlots))), dim3(kThreads),
+                0, ctx->stream, (const ClipEntry*)table, r.entries, r.chunks, written, (const double*)slots, scale,
+                max_norm, to);
+  };
+  bool any = false;
+  for (int i = 0; i < count; ++i) any |= grads[i].out && grads[i].n > 0;
+  if (!any) first = Round{0, 0, 0};
+  scaled(first, norm);
+  // what the table could not hold, a table at a time
+  for (int at = second; any && at < count;) {
+    Round r{at, 0, 0};
+    while (at < count) {
+      const int from = at;
+      at = clip_fill(grads, count, at, f);
+      if (f.total == 0) continue;
+      if (!fits(r)) {
+        at = from;
+        break;
+      }
+      CAVS_LAUNCH("k_clip_norm", k_clip_norm, dim3(1), dim3(kThreads), 0, ctx->stream, f.set, f.total, 0, r.chunks,
+                  (double*)nullptr, table + r.entries);
+      r.entries += f.set.count;
+      r.chunks += f.total;
+    }
+    scaled(r, nullptr);
   }
   CAVS_LAUNCH_CHECK(ctx);
   return CAVS_OK;

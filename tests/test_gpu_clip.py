@@ -38,8 +38,9 @@ def _call(ctx, grads, limit, out=None, scale=1.0):
 
 SIZES = {
     "one": [1], "few": [7, 0, 8, 1, 9], "odd": [8191, 8192, 8193, 3, 100001], "large": [3000001, 5],
-    "many": [(37 * k) % 501 for k in range(500)], "same": [4096] * 121, "set": [10] * 120, "sets": [5000] * 240,
+    "many": [(37 * k) % 501 for k in range(500)], "same": [4096] * 121, "set": [10] * 160, "sets": [5000] * 321,
 }
+THOUSANDS = [(k % 7) * (k % 3) for k in range(4000)] + [4099, 1] * 1500 + [0] * 50 + [20000]
 
 
 @pytest.mark.parametrize("sizes", list(SIZES))
@@ -61,6 +62,16 @@ def test_clipped(ctx, sizes, types, limit, scale):
     if types[0] == types[1]:
         again = _call(ctx, grads, limit, scale=scale)
         assert torch.equal(again, norm) and all(torch.equal(x, y) for x, y in zip(grads, out))
+
+
+def test_more_gradients_than_a_table_holds(ctx):
+    flat = torch.randn(sum(THOUSANDS), generator=torch.Generator().manual_seed(2)).cuda()
+    grads, kept = list(flat.split(THOUSANDS)), flat.clone()
+    out = torch.full_like(flat, float("nan"))
+    norm = _call(ctx, grads, 2.0, list(out.split(THOUSANDS)))
+    want, nb, [(w, b)] = R.clip([kept], 1.0, 2.0, [F32])
+    assert abs(float(norm) - want) <= nb and R.outside(out, w, b) <= 1.0 and torch.equal(flat, kept)
+    assert torch.equal(_call(ctx, grads, 2.0), norm) and torch.equal(flat, out)
 
 
 def test_shapes_types_and_places_together(ctx):
