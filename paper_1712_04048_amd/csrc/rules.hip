@@ -95,18 +95,24 @@ __device__ __forceinline__ void load_any(const T* p, float (&v)[V]) {
     for (int i = 0; i < V; ++i) v[i] = __uint_as_float((uint32_t)a[i] << 16);
   }
 }
-template <class T, int V>
+// FAR: past the caches.
+template <bool FAR, class T, int V>
 __device__ __forceinline__ void store_any(T* p, const float (&v)[V]) {
   if constexpr (sizeof(T) == 4) {
     typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
 #pragma unroll
-    for (int i = 0; i < V; i += 4) *reinterpret_cast<f4*>(p + i) = f4{v[i], v[i + 1], v[i + 2], v[i + 3]};
+    for (int i = 0; i < V; i += 4) {
+      const f4 a = {v[i], v[i + 1], v[i + 2], v[i + 3]};
+      if constexpr (FAR) __builtin_nontemporal_store(a, reinterpret_cast<f4*>(p + i));
+      else *reinterpret_cast<f4*>(p + i) = a;
+    }
   } else {
     typedef uint32_t w __attribute__((ext_vector_type(V / 2), aligned(2)));
     w a;
 #pragma unroll
     for (int i = 0; i < V / 2; ++i) a[i] = f2bf2(v[2 * i], v[2 * i + 1]);
-    *reinterpret_cast<w*>(p) = a;
+    if constexpr (FAR) __builtin_nontemporal_store(a, reinterpret_cast<w*>(p));
+    else *reinterpret_cast<w*>(p) = a;
   }
 }
 
@@ -117,7 +123,7 @@ __device__ __forceinline__ void store_any(T* p, const float (&v)[V]) {
 // order, so that no run differs.  Each wavefront leaves its largest v and its sum.
 // (Workgroups that go through pieces and ask for the next one ahead were slower: 256
 // x 128 000 in bf16 49 us, 39 with one for each piece.)
-template <class Z, class O, int THREADS, int PER>
+template <class Z, class O, int THREADS, int PER, bool FAR>
 __global__ void __launch_bounds__(THREADS) k_rules(RulesNet a, int row0, const Z* z, O* out) {
 #pragma clang fp contract(off)
   constexpr int SEG = THREADS * PER, V = sizeof(Z) == 4 && sizeof(O) == 4 ? 4 : 8, NV = PER / V, W = THREADS / 64;
@@ -262,7 +268,7 @@ __global__ void __launch_bounds__(THREADS) k_rules(RulesNet a, int row0, const Z
     if (out) {
       O* o = out + (size_t)row * a.C + c0 + c;
       if (whole) {
-        store_any<O, V>(o, x);
+        store_any<FAR, O, V>(o, x);
       } else {
 #pragma unroll
         for (int i = 0; i < V; ++i)
@@ -358,6 +364,9 @@ cavs_status adjust_run(cavs_ctx* ctx, const cavs_rules* r, const void* z, void* 
   const int per = few ? kPerFew : kPer;
   a.segs = cdiv(r->C, threads * per);
   a.err = ctx->dev_err_dev;
+  // what is read next does not find 32 MB in the caches (256 x 128 000 in bf16: 32 us
+  // through them, 29 past them)
+  const bool far = (size_t)r->n * r->C * os >= 32u << 20;
   if ((best || lse) && a.segs > 1) {
     if (!ws || ws_bytes < need) return fail(ctx, CAVS_ERR_WORKSPACE, "workspace too small: %zu < %zu", ws_bytes, need);
     if (((uintptr_t)ws & 15) != 0) return fail(ctx, CAVS_ERR_ARG, "ws must be aligned to 16 bytes");
@@ -375,9 +384,10 @@ cavs_status adjust_run(cavs_ctx* ctx, const cavs_rules* r, const void* z, void* 
           (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)shmem);
         CAVS_LAUNCH(name, kernel, grid, dim3(threads), shmem, ctx->stream, a, i, (const Z*)z, (O*)out);
       };
-      if (wide) launch("k_rules<1024, 16>", k_rules<Z, O, 1024, kPer>);
-      else if (few) launch("k_rules<256, 8>", k_rules<Z, O, 256, kPerFew>);
-      else launch("k_rules<256, 16>", k_rules<Z, O, 256, kPer>);
+      if (wide) launch("k_rules<1024, 16>", k_rules<Z, O, 1024, kPer, false>);
+      else if (few) launch("k_rules<256, 8>", k_rules<Z, O, 256, kPerFew, false>);
+      else if (far) launch("k_rules<256, 16, far>", k_rules<Z, O, 256, kPer, true>);
+      else launch("k_rules<256, 16>", k_rules<Z, O, 256, kPer, false>);
     };
     if (zs == 2) os == 2 ? go(u16{}, u16{}) : go(u16{}, float{});
     else os == 2 ? go(float{}, u16{}) : go(float{}, float{});
