@@ -195,29 +195,37 @@ __global__ void __launch_bounds__(256) k_quant_unpack(QuantNet q, T* W) {
   }
 }
 
-// Eight codes q as halves.  A half with an exponent of 0 is its mantissa times
-// 2^-24, so q's bits in place are q 2^-24, four places up 2^-20 q: five
-// instructions, where the bound by memory leaves about 26 for eight weights.  The
-// matrix instruction takes such halves as they are; the rows' side makes up for the
-// factor of 16 (adjacent pairs of columns, in turn) and for the 2^-24.
-__device__ __forceinline__ h8 halves(uint32_t w) {
+// Eight codes less 8 as halves, exact: 0x6400 | q is 1024 + q, 0x6400 | q << 4 is
+// 1024 + 16 q.  Nine instructions, where the bound by memory leaves about 26 for
+// eight weights.  Codes left as 0 .. 15, in the bits of subnormal halves, take five,
+// and 8 times the sum of x off afterwards: 16 x 128 000 x 2048 in 35.1 us instead of
+// 36.1, but the sums are four times as large, and y's error was 3.5e-7 of it (fp32 x
+// 9e-7) instead of 6e-8.  mask and magic are registers, so that one instruction takes
+// both.
+struct QuantBits {
+  uint32_t low = 0x000f000fu, high = 0x00f000f0u, magic = 0x64006400u;
+  __device__ __forceinline__ QuantBits() { asm("" : "+s"(low), "+s"(high), "+v"(magic)); }
+};
+__device__ __forceinline__ h8 halves(uint32_t w, const QuantBits& k) {
+  const h2 a = {(_Float16)-1032.f, (_Float16)-1032.f}, f = {(_Float16)0.0625f, (_Float16)0.0625f},
+           g = {(_Float16)-72.f, (_Float16)-72.f};
+  auto at = [&](uint32_t v, uint32_t mask) { return __builtin_bit_cast(h2, (v & mask) | k.magic); };
   const uint32_t v = w >> 8;
-  return __builtin_bit_cast(h8, make_uint4(w & 0x000f000fu, w & 0x00f000f0u, v & 0x000f000fu, v & 0x00f000f0u));
+  const h2 v0 = at(w, k.low) + a, v1 = __builtin_elementwise_fma(at(w, k.high), f, g);
+  const h2 v2 = at(v, k.low) + a, v3 = __builtin_elementwise_fma(at(v, k.high), f, g);
+  return h8{v0.x, v0.y, v1.x, v1.y, v2.x, v2.y, v3.x, v3.y};
 }
 
 // The rows' side of the product.  With X the sum of a group's x,
-//   sum x What = sum over groups of s (sum x q - 8 X) + m X.
+//   sum x What = sum over groups of s (sum x (q - 8)) + m X.
 // x is scaled by a power of two 2^up for each row and block of 128 columns, so that
-// the block's largest finite value lies in 2^14 .. 2^15 (and every other pair of
-// columns by 1/16): a half then holds what a bf16 has (values 2^-28 of the block's
-// largest and less lose bits, which is less than an fp32 sum keeps of them); an fp32
-// x is the sum of two halves, 2^-24 of it away at most, or 2^-35 of the block's
-// largest.  Products of halves and codes are exact, their sums are fp32.  The sums
-// over blocks are kept times 2^-12, which takes half of the 2^-24 (rows near either
-// end of fp32 stay inside it) and is made up for at the end.
-//   LDS: xh [KC][parts][4 b][4 j][rows] of 16 bytes, xs [KC][16] = 2^(12 - up),
-//   xg [KC][groups][16] = 2^-12 X.
-constexpr float kQDown = 0x1p-12f;
+// the block's largest finite value lies in 2^14 .. 2^15: a half then holds what a bf16
+// has (values 2^-32 of the block's largest and less lose bits, which is less than an
+// fp32 sum keeps of them); an fp32 x is the sum of two halves, 2^-24 of it away at
+// most, or 2^-39 of the block's largest.  Products of halves and codes are exact,
+// their sums are fp32.
+//   LDS: xh [KC][parts][4 b][4 j][rows] of 16 bytes, xs [KC][16] = 2^-up,
+//   with shifts xg [KC][groups][16] = X.
 
 template <class X>
 __device__ __forceinline__ void quant_load8(const X* __restrict__ x, int H, int k, float (&v)[8]) {
@@ -239,7 +247,7 @@ __device__ __forceinline__ void quant_load8(const X* __restrict__ x, int H, int 
   }
 }
 
-template <class X, int G>
+template <class X, int G, bool SHIFT>
 __device__ __forceinline__ void quant_put(const float (&v)[8], int o, int r, int kb, int rows, uint4* xh, float* xs,
                                           float* xg) {
   constexpr int P = sizeof(X) == 4 ? 2 : 1, NS = kQB / G;
@@ -249,12 +257,12 @@ __device__ __forceinline__ void quant_put(const float (&v)[8], int o, int r, int
   for (int i = 0; i < 8; ++i) {
     const uint32_t a = __float_as_uint(v[i]) & 0x7fffffffu;
     top = max(top, a < 0x7f800000u ? a : 0u);
-    sum += v[i] * kQDown;
+    if (SHIFT) sum += v[i];
   }
 #pragma unroll
   for (int d = 1; d < 16; d <<= 1) {
     top = max(top, (uint32_t)__shfl_xor((int)top, d, 16));
-    if (d * 8 < G) sum += __shfl_xor(sum, d, 16);
+    if (SHIFT && d * 8 < G) sum += __shfl_xor(sum, d, 16);
   }
   // a block of values below 2^-112 keeps fewer bits
   const int e = max((int)(top >> 23) - 127, -112), up = top ? 14 - e : 0;
@@ -264,7 +272,7 @@ __device__ __forceinline__ void quant_put(const float (&v)[8], int o, int r, int
     h2 h, l;
 #pragma unroll
     for (int z = 0; z < 2; ++z) {
-      const float t = ldexpf(v[2 * i + z], up - (i & 1 ? 4 : 0));
+      const float t = ldexpf(v[2 * i + z], up);
       h[z] = (_Float16)t;
       l[z] = fabsf(t) < INFINITY ? (_Float16)(t - (float)h[z]) : (_Float16)0.f;
     }
@@ -275,13 +283,13 @@ __device__ __forceinline__ void quant_put(const float (&v)[8], int o, int r, int
   uint4* at = xh + ((size_t)kb * P * 16 + o) * rows + r;
   at[0] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
   if (P == 2) at[16 * rows] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-  if (o == 0) xs[kb * kQR + r] = ldexpf(1.f, 12 - up);
-  if (o % (G / 8) == 0) xg[(kb * NS + o / (G / 8)) * kQR + r] = sum;
+  if (o == 0) xs[kb * kQR + r] = ldexpf(1.f, -up);
+  if (SHIFT && o % (G / 8) == 0) xg[(kb * NS + o / (G / 8)) * kQR + r] = sum;
 }
 
 // Blocks kb0 .. kb0 + nkb of all rows; a row's block to sixteen lanes, eight columns
 // each, two such blocks in flight.
-template <class X, int G>
+template <class X, int G, bool SHIFT>
 __device__ __forceinline__ void quant_stage(const X* __restrict__ x, int H, int rows, int kb0, int nkb, uint4* xh,
                                             float* xs, float* xg) {
   const int units = rows * nkb * 16, step = blockDim.x;
@@ -297,7 +305,7 @@ __device__ __forceinline__ void quant_stage(const X* __restrict__ x, int H, int 
     }
 #pragma unroll
     for (int z = 0; z < 2; ++z)
-      if (u + z * step < units) quant_put<X, G>(v[z], u & 15, r[z], kb[z], rows, xh, xs, xg);
+      if (u + z * step < units) quant_put<X, G, SHIFT>(v[z], u & 15, r[z], kb[z], rows, xh, xs, xg);
   }
 }
 
@@ -324,7 +332,7 @@ __global__ void __launch_bounds__(64 * kQW) k_quant_product(QuantJob a) {
   uint4* xh = lds;
   float* xs = reinterpret_cast<float*>(lds + (size_t)a.KC * P * 16 * rows);
   float* xg = xs + a.KC * kQR;
-  v4f* red = reinterpret_cast<v4f*>(xg + a.KC * NS * kQR);   // [kQW][64]
+  v4f* red = reinterpret_cast<v4f*>(xg + (SHIFT ? a.KC * NS * kQR : 0));   // [kQW][64]
   const X* x = (const X*)a.x + (size_t)r0 * a.q.H;
   const int KB = a.q.KB, T = a.q.T, S = a.S, ks = w % S, tw = w / S, per = kQW / S;
   const int steps = (KB + S - 1) / S, cstep = a.KC / S;   // blocks of a wavefront: of a tile, of a chunk
@@ -348,6 +356,7 @@ __global__ void __launch_bounds__(64 * kQW) k_quant_product(QuantJob a) {
 #pragma unroll
   for (int u = 0; u < PF; ++u) load(ring[u]);
   const uint4* frag = xh + j * rows + row;   // this lane's place in a dword's fragment
+  const QuantBits bits;
   v4f acc = {};
   int step = 0, cs = 0, grp = 0;
   for (int it0 = 0; it0 < items; it0 += PF) {
@@ -357,7 +366,7 @@ __global__ void __launch_bounds__(64 * kQW) k_quant_product(QuantJob a) {
       if (cs == 0 && (it0 + u == 0 || a.KC < KB)) {
         if (it0 + u > 0) __syncthreads();   // the last chunk has been read
         const int kb0 = step * S;
-        quant_stage<X, G>(x, a.q.H, rows, kb0, min(a.KC, KB - kb0), xh, xs, xg);
+        quant_stage<X, G, SHIFT>(x, a.q.H, rows, kb0, min(a.KC, KB - kb0), xh, xs, xg);
         __syncthreads();
       }
       if (step * S + ks < KB) {
@@ -366,21 +375,22 @@ __global__ void __launch_bounds__(64 * kQW) k_quant_product(QuantJob a) {
         const float f = xs[kc * kQR + row];
 #pragma unroll
         for (int g = 0; g < NS; ++g) {
-          v4f part = {};
+          v4f part[P] = {};   // small halves apart: the instruction drops bits of theirs below a large sum
 #pragma unroll
           for (int b = g * (4 / NS); b < (g + 1) * (4 / NS); ++b) {
-            const h8 c8 = halves(d[b]);
+            const h8 c8 = halves(d[b], bits);
 #pragma unroll
             for (int p = 0; p < P; ++p)
-              part = __builtin_amdgcn_mfma_f32_16x16x32_f16(
-                  c8, __builtin_bit_cast(h8, frag[((kc * P + p) * 4 + b) * 4 * rows]), part, 0, 0, 0);
+              part[p] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+                  c8, __builtin_bit_cast(h8, frag[((kc * P + p) * 4 + b) * 4 * rows]), part[p], 0, 0, 0);
           }
-          const float X1 = xg[(kc * NS + g) * kQR + row], X8 = -8.f * X1;
+          if (P == 2) part[0] += part[P - 1];
+          const float X1 = SHIFT ? xg[(kc * NS + g) * kQR + row] : 0.f;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {   // word i's numbers: halves W16 i and on
             const int at = W16 * i + g * (SHIFT ? 2 : 1);
             const uint32_t s = ring[u].s[at / 2];
-            acc[i] = fmaf(__uint_as_float(at & 1 ? s & 0xffff0000u : s << 16), fmaf(f, part[i], X8), acc[i]);
+            acc[i] = fmaf(__uint_as_float(at & 1 ? s & 0xffff0000u : s << 16), f * part[0][i], acc[i]);
             if (SHIFT) acc[i] = fmaf(__uint_as_float(s & 0xffff0000u), X1, acc[i]);
           }
         }
@@ -406,7 +416,7 @@ __global__ void __launch_bounds__(64 * kQW) k_quant_product(QuantJob a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float bias = a.bias && (whole || c + i < a.q.C) ? a.bias[c + i] : 0.f;
-          v[i] = fmaf(acc[i], 1.f / kQDown, bias);
+          v[i] = acc[i] + bias;
         }
         if (whole) {   // at any address that is aligned to its elements
           typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
@@ -537,7 +547,7 @@ cavs_status quant_product_run(cavs_ctx* ctx, const cavs_quant* q, int x_type, co
   // tiles, whose blocks are then read in the order of memory by neighbours (16 x
   // 128 000 x 2048: 37.0 us with one, 35.8 with two, 36.1 with four; of 1024: one)
   const int rows = cdiv(n, kQR);
-  const size_t block = (size_t)P * 256 * std::min(n, kQR) + 4 * kQR * (1 + kQB / q->group);
+  const size_t block = (size_t)P * 256 * std::min(n, kQR) + 4 * kQR * (1 + (q->shift ? kQB / q->group : 0));
   a.S = KB >= 16 ? 2 : 1;
   while (a.S < 8 && a.S < KB && (long)T * a.S * rows < 2048) a.S *= 2;
   const size_t red = a.S > 1 ? (size_t)kQW * 1024 : 0;

@@ -4,14 +4,12 @@ gradients' norm and clipping, with bounds on how far 32-bit sums may be from the
 u = 2^-24 is fp32's half step; a rounding to bf16 is off by at most 2^-8 of the
 value (torch.finfo(torch.bfloat16).eps / 2).
 
-* The 4-bit product: x, scaled so that its block's largest value is at least 2^14
-  (every other pair of columns: 2^10), is a half, or the sum of two, 2^-24 of it
-  away at most, or half of a half's smallest step (2^-24): 2^-35 of the block's largest
-  value.  A product of a half and a code is exact; of H terms each passes at most H
-  additions in fp32, two multiplications (the group's scale; the powers of two are
-  exact).  The codes are 0 .. 15, what is too much is taken off with the sum of x,
-  times (m - 8 s), rounded once: the terms' magnitudes are |s q| + |m - 8 s|, each sum
-  (2 H + 16) u of their sum, as for any fp32 product.
+* The 4-bit product: x, scaled so that its block's largest value is at least 2^14, is
+  a half, or the sum of two, 2^-24 of it away at most, or half of a half's smallest step
+  (2^-24): 2^-39 of the block's largest value.  A product of a half and a code is exact;
+  of H terms each passes at most H additions in fp32 and two multiplications (the group's
+  scale; the powers of two are exact), and with a shift the same again, of |m x|:
+  (2 H + 16) u of the sum of the terms' magnitudes, as for any fp32 product.
 * Rules: each step is one rounding of a value no larger than the magnitudes'
   sum; nine steps and K additions of a word's extras at most.
 * ln sum exp: v's bound, as ln sum exp moves no more than its largest argument;
@@ -80,10 +78,10 @@ def product(x, q, s, m, group, bias, out_bf):
     W, x = weights(q, s, m, group), x.double()
     y = x @ W
     rep = lambda a: a.repeat_interleave(group, 0)[:H]
-    big = (rep(s) * (q + 8)).abs() + (rep(m) - 8 * rep(s)).abs()
+    big = (rep(s) * q).abs() + rep(m).abs()
     bound = (2 * H + 16) * U * (x.abs() @ big)
     top = torch.cat([b.abs().amax(1, keepdim=True).expand_as(b) for b in x.split(128, 1)], 1)
-    bound += 2.0 ** -35 * (top @ big)
+    bound += 2.0 ** -39 * (top @ big)
     if bias is not None:
         y = y + bias.double()
         bound = bound + U * y.abs()
