@@ -526,7 +526,8 @@ typedef struct {
   const float* temp;        /* [n] */
 } cavs_rules;
 
-/* Bytes of device workspace cavs_adjust_logits needs.  0 on bad args. */
+/* Bytes of device workspace cavs_adjust_logits needs (aligned to 16; not read or
+   written without best and lse).  0 on bad args. */
 size_t cavs_adjust_workspace_bytes(int32_t n, int32_t C);
 
 /* out [n, C] (may be z itself, of one type then, or NULL) the v; best [n] (or

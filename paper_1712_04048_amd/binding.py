@@ -422,12 +422,9 @@ _TYPES = {torch.float32: T_F32, torch.bfloat16: T_BF16}
 
 def _operand(name: str, t: Optional[torch.Tensor], shape, dtypes, device) -> Optional[int]:
     """The address of a tensor after the checks that the C ABI cannot make."""
-    try:   # all of them at once, as most calls pass them
-        if (t.dtype in dtypes and t.shape == shape and (device is None or t.device == device)
-                and t.is_contiguous() and isinstance(t, torch.Tensor)):
-            return t.data_ptr() or None
-    except AttributeError:
-        pass
+    if (isinstance(t, torch.Tensor) and t.dtype in dtypes and t.shape == shape
+            and (device is None or t.device == device) and t.is_contiguous()):
+        return t.data_ptr() or None   # as most calls pass them, all at once
     if not isinstance(t, torch.Tensor):
         raise CavsError(ERR_ARG, "%s: a tensor is required" % name)
     if t.dtype not in dtypes:
@@ -588,6 +585,9 @@ class GradList:
             q = None if o is None else _operand("out %d" % k, o, g.shape, _TYPES, device)
             self.raw[k] = cavs_grad(p, q, g.numel(), _TYPES[g.dtype], _TYPES[(g if o is None else o).dtype])
         self.device = device
+        written = [r.out for r in self.raw if r.out]
+        if len(set(written)) != len(written):
+            raise CavsError(ERR_ARG, "out: the same memory twice")
 
 
 def clip_workspace_bytes() -> int:

@@ -367,7 +367,7 @@ cavs_status adjust_run(cavs_ctx* ctx, const cavs_rules* r, const void* z, void* 
   // what is read next does not find 32 MB in the caches (256 x 128 000 in bf16: 32 us
   // through them, 29 past them)
   const bool far = (size_t)r->n * r->C * os >= 32u << 20;
-  if ((best || lse) && a.segs > 1) {
+  if (best || lse) {
     if (!ws || ws_bytes < need) return fail(ctx, CAVS_ERR_WORKSPACE, "workspace too small: %zu < %zu", ws_bytes, need);
     if (((uintptr_t)ws & 15) != 0) return fail(ctx, CAVS_ERR_ARG, "ws must be aligned to 16 bytes");
   }

@@ -222,11 +222,12 @@ class LmBatch(Batch):
         """The likeliest word at each of ``vertices`` (int32 [n], on the device: the
         last ones of the sequences, as a rule) under the rules, -1 where they allow
         none: the states, their rows, the head in 4 bits, the rules.  ``logits``
-        [n, C] and ``lse`` [n] hold what the words were taken from."""
+        [n, C] and ``lse`` [n] hold what the words were taken from.  After alloc()."""
         n, C, dev = int(vertices.shape[0]), int(self.Ws.shape[1]), self.dev
         if self.quant is None:
             self.quantise()
         if getattr(self, "best", None) is None or self.best.shape[0] != n:
+            self.ctx.sync()   # an earlier call may still be using what is replaced
             self.rows = torch.empty(n, self.wl.H, dtype=torch.float32, device=dev)
             self.logits = torch.empty(n, C, dtype=torch.float32, device=dev)
             self.best = torch.empty(n, dtype=torch.int32, device=dev)

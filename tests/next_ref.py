@@ -14,8 +14,9 @@ value (torch.finfo(torch.bfloat16).eps / 2).
   sum; nine steps and K additions of a word's extras at most.
 * ln sum exp: v's bound, as ln sum exp moves no more than its largest argument;
   exp of a rounded x: (2 |x| + 4) 2 u of each term, averaged by the terms; 16 terms
-  of a thread, 6 + 4 (or 16) additions in a workgroup, 4 + 6 of up to 256 segments,
-  each scaled once (9 u): 64 u; the logarithm 4 u of its value, the last sum u.
+  of a thread, 6 additions in a wavefront, up to 16 parts in a lane of the join and 6
+  additions there, each part scaled once (9 u): 64 u; the logarithm 4 u of its value,
+  the last sum u.
 * Norm and clipping: sums in 64 bits (2^-53 times the number of terms at most,
   2^-23 of the value at 2^30 of them, far less than that in pairs: u covers it) and one
   rounding; the factor's rounding, the product's, and that to bf16.

@@ -141,3 +141,20 @@ def test_a_norm_that_is_not_finite_clips_nothing(ctx, bad):
     out = [torch.empty_like(x), torch.empty_like(y)]
     _call(ctx, [x, y], 1.0, out, scale=2.0)
     assert torch.equal(out[0], 2 * x)
+
+
+@pytest.mark.parametrize("types", [(BF16, BF16), (F32, BF16), (BF16, F32)])
+def test_many_elements_at_odd_places(ctx, types):
+    """Enough of them that they are written past the caches, from any element on."""
+    g = torch.Generator(device="cuda").manual_seed(9)
+    n = [5000001, 17, 4000003]
+    for off in (0, 1, 3):
+        src = torch.randn(sum(n) + off, generator=g, device="cuda").to(types[0])
+        room = torch.full((sum(n) + off + 8,), 9.0, dtype=types[1], device="cuda")
+        grads, out = list(src[off:].split(n)), list(room[off:off + sum(n)].split(n))
+        want, nb, outs = R.clip(grads, 1.0, 2.0, [types[1]] * 3)
+        norm = _call(ctx, grads, 2.0, out)
+        assert abs(float(norm) - want) <= nb
+        for o, (w, b) in zip(out, outs):
+            assert R.outside(o, w, b) <= 1.0
+        assert (room[:off] == 9.0).all() and (room[off + sum(n):] == 9.0).all()

@@ -123,11 +123,12 @@ def _outputs(s):
     return [s[k].clone() for k in ("x", "z", "best", "lse", "norm")] + [o.clone() for o in s["out"]]
 
 
-def test_captured_and_replayed(ctx):
+@pytest.mark.parametrize("n,H,C", [(5, 256, 20000), (16, 2048, 5000), (1, 64, 300)])
+def test_captured_and_replayed(ctx, n, H, C):
     """Replays on changed inputs, with eager work between them, equal eager calls."""
     stream = torch.cuda.Stream()
     c = B.Context(0, stream)
-    s = _state(c, 1)
+    s = _state(c, 1, n, H, C)
     _step(c, s)
     c.sync()
     graph = torch.cuda.CUDAGraph()
@@ -137,7 +138,7 @@ def test_captured_and_replayed(ctx):
     for k in range(4):
         s["word"].copy_(torch.randint(0, 40, s["word"].shape, generator=g, device="cuda"))
         s["src"][0].mul_(0.9 + 0.1 * k)
-        s["rules"].past.copy_(torch.randint(-1, 20000, s["rules"].past.shape, generator=g, device="cuda"))
+        s["rules"].past.copy_(torch.randint(-1, C, s["rules"].past.shape, generator=g, device="cuda"))
         torch.cuda.synchronize()
         graph.replay()
         torch.cuda.synchronize()

@@ -222,3 +222,26 @@ def test_logits_inside_an_allocation(ctx):
 def test_no_rows(ctx):
     z = torch.empty(0, 50, device="cuda")
     _call(ctx, {}, z)
+
+
+@pytest.mark.parametrize("types", [(BF16, BF16), (F32, F32), (F32, BF16), (BF16, F32)])
+def test_many_logits_at_odd_places(ctx, types):
+    """Enough of them that they are written past the caches: the same bits as row by row."""
+    g = torch.Generator(device="cuda").manual_seed(15)
+    n, C, off = 41, 420001, 1
+    src = torch.randn(n * C + off, generator=g, device="cuda").to(types[0])
+    z = src[off:].view(n, C)
+    room = torch.full((n * C + off + 8,), 9.0, dtype=types[1], device="cuda")
+    out = room[off:off + n * C].view(n, C)
+    cpu = torch.Generator().manual_seed(15)
+    rules = _rules(cpu, n, C, "rpfbemt")
+    ws = torch.empty(B.adjust_workspace_bytes(n, C), dtype=torch.uint8, device="cuda")
+    best, lse = torch.empty(n, dtype=torch.int32, device="cuda"), torch.empty(n, device="cuda")
+    B.adjust_logits(ctx, B.LogitRules(**rules), z, out, best, lse, ws)
+    ctx.sync()
+    assert (room[:off] == 9.0).all() and (room[off + n * C:] == 9.0).all()
+    for i in (0, 1, 20, n - 1):
+        one = {k: v if k in ("bias", "mask") else v[i:i + 1] for k, v in rules.items()}
+        o, b, l = _call(ctx, one, z[i:i + 1].contiguous(), types[1])
+        assert torch.equal(o[0], out[i]) and torch.equal(b[0], best[i])
+        assert abs(float(l) - float(lse[i])) <= 128 * R.U * (1 + abs(float(l)))   # other pieces, other sums
