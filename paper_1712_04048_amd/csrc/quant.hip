@@ -247,7 +247,7 @@ __device__ __forceinline__ void quant_load8(const X* __restrict__ x, int H, int 
   }
 }
 
-template <class X, int G, bool SHIFT>
+template <class X, int G, bool SHIFT, int R>
 __device__ __forceinline__ void quant_put(const float (&v)[8], int o, int r, int kb, int rows, uint4* xh, float* xs,
                                           float* xg) {
   constexpr int P = sizeof(X) == 4 ? 2 : 1, NS = kQB / G;
@@ -283,13 +283,13 @@ __device__ __forceinline__ void quant_put(const float (&v)[8], int o, int r, int
   uint4* at = xh + ((size_t)kb * P * 16 + o) * rows + r;
   at[0] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
   if (P == 2) at[16 * rows] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-  if (o == 0) xs[kb * kQR + r] = ldexpf(1.f, -up);
-  if (SHIFT && o % (G / 8) == 0) xg[(kb * NS + o / (G / 8)) * kQR + r] = sum;
+  if (o == 0) xs[kb * R + r] = ldexpf(1.f, -up);
+  if (SHIFT && o % (G / 8) == 0) xg[(kb * NS + o / (G / 8)) * R + r] = sum;
 }
 
 // Blocks kb0 .. kb0 + nkb of all rows; a row's block to sixteen lanes, eight columns
 // each, two such blocks in flight.
-template <class X, int G, bool SHIFT>
+template <class X, int G, bool SHIFT, int R>
 __device__ __forceinline__ void quant_stage(const X* __restrict__ x, int H, int rows, int kb0, int nkb, uint4* xh,
                                             float* xs, float* xg) {
   const int units = rows * nkb * 16, step = blockDim.x;
@@ -305,16 +305,20 @@ __device__ __forceinline__ void quant_stage(const X* __restrict__ x, int H, int 
     }
 #pragma unroll
     for (int z = 0; z < 2; ++z)
-      if (u + z * step < units) quant_put<X, G, SHIFT>(v[z], u & 15, r[z], kb[z], rows, xh, xs, xg);
+      if (u + z * step < units) quant_put<X, G, SHIFT, R>(v[z], u & 15, r[z], kb[z], rows, xh, xs, xg);
   }
 }
 
-// y[rows, C] = x What + bias.  A workgroup of sixteen wavefronts has up to sixteen
-// rows of x (KC blocks of them at a time) in LDS and goes through groups of tiles; S
+// y[rows, C] = x What + bias.  A workgroup of sixteen wavefronts has up to 16 RT rows
+// of x (KC blocks of them at a time) in LDS and goes through groups of tiles; S
 // wavefronts share a tile, each S-th block to one, and join their sums in LDS.  Each
 // wavefront keeps PF blocks of codes in flight, over the ends of tiles.  The words
 // are the rows of the matrix instruction's result, so that a lane has four adjacent
-// ones of one row of y.
+// ones of a row of y, one store: with four stores of a word each, the next blocks
+// waited for them (16 x 128 000 x 2048: 43 us, 37 so).
+// Bound by memory, the codes once: 16 x 128 000 x 2048 in 36 us (143 MB, 4.0 TB/s), of
+// which reading the codes alone takes 28; 4 x 50 001 x 1024 in 10 (30 MB); below some
+// 10 MB by latency (1 x 10 000 x 512 in 4).
 struct QuantJob {
   QuantNet q;
   const void* x;
@@ -323,21 +327,24 @@ struct QuantJob {
   int n, KC, S, groups, ybf;
 };
 
-template <class X, int G, bool SHIFT>
+template <class X, int G, bool SHIFT, int RT>
 __global__ void __launch_bounds__(64 * kQW) k_quant_product(QuantJob a) {
-  constexpr int P = sizeof(X) == 4 ? 2 : 1, NS = kQB / G, W16 = NS * (SHIFT ? 2 : 1), PF = 2;
+  constexpr int P = sizeof(X) == 4 ? 2 : 1, NS = kQB / G, W16 = NS * (SHIFT ? 2 : 1), PF = 2, R = kQR * RT;
   extern __shared__ uint4 lds[];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int r0 = blockIdx.y * kQR, rows = min(kQR, a.n - r0);
+  const int r0 = blockIdx.y * R, rows = min(R, a.n - r0);
   uint4* xh = lds;
   float* xs = reinterpret_cast<float*>(lds + (size_t)a.KC * P * 16 * rows);
-  float* xg = xs + a.KC * kQR;
-  v4f* red = reinterpret_cast<v4f*>(xg + (SHIFT ? a.KC * NS * kQR : 0));   // [kQW][64]
+  float* xg = xs + a.KC * R;
+  v4f* red = reinterpret_cast<v4f*>(xg + (SHIFT ? a.KC * NS * R : 0));   // [kQW][RT][64]
   const X* x = (const X*)a.x + (size_t)r0 * a.q.H;
   const int KB = a.q.KB, T = a.q.T, S = a.S, ks = w % S, tw = w / S, per = kQW / S;
   const int steps = (KB + S - 1) / S, cstep = a.KC / S;   // blocks of a wavefront: of a tile, of a chunk
   const int mine = (a.groups - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x;   // groups of tiles
-  const int items = mine * steps, j = lane >> 4, row = min(lane & 15, rows - 1);
+  const int items = mine * steps, j = lane >> 4;
+  int row[RT];
+#pragma unroll
+  for (int k = 0; k < RT; ++k) row[k] = min(k * kQR + (lane & 15), rows - 1);
   struct Block {
     uint4 c;
     uint32_t s[2 * W16];   // of this lane's four words
@@ -355,9 +362,11 @@ __global__ void __launch_bounds__(64 * kQW) k_quant_product(QuantJob a) {
   };
 #pragma unroll
   for (int u = 0; u < PF; ++u) load(ring[u]);
-  const uint4* frag = xh + j * rows + row;   // this lane's place in a dword's fragment
+  const uint4* frag[RT];   // this lane's place in a dword's fragment of each sixteen rows
+#pragma unroll
+  for (int k = 0; k < RT; ++k) frag[k] = xh + j * rows + row[k];
   const QuantBits bits;
-  v4f acc = {};
+  v4f acc[RT] = {};
   int step = 0, cs = 0, grp = 0;
   for (int it0 = 0; it0 < items; it0 += PF) {
 #pragma unroll
@@ -366,32 +375,39 @@ __global__ void __launch_bounds__(64 * kQW) k_quant_product(QuantJob a) {
       if (cs == 0 && (it0 + u == 0 || a.KC < KB)) {
         if (it0 + u > 0) __syncthreads();   // the last chunk has been read
         const int kb0 = step * S;
-        quant_stage<X, G, SHIFT>(x, a.q.H, rows, kb0, min(a.KC, KB - kb0), xh, xs, xg);
+        quant_stage<X, G, SHIFT, R>(x, a.q.H, rows, kb0, min(a.KC, KB - kb0), xh, xs, xg);
         __syncthreads();
       }
       if (step * S + ks < KB) {
         const int kc = cs * S + ks;
         const uint32_t d[4] = {ring[u].c.x, ring[u].c.y, ring[u].c.z, ring[u].c.w};
-        const float f = xs[kc * kQR + row];
+        float f[RT];
+#pragma unroll
+        for (int k = 0; k < RT; ++k) f[k] = xs[kc * R + row[k]];
 #pragma unroll
         for (int g = 0; g < NS; ++g) {
-          v4f part[P] = {};   // small halves apart: the instruction drops bits of theirs below a large sum
+          v4f part[RT][P] = {};   // small halves apart: the instruction drops bits of theirs below a large sum
 #pragma unroll
           for (int b = g * (4 / NS); b < (g + 1) * (4 / NS); ++b) {
             const h8 c8 = halves(d[b], bits);
 #pragma unroll
             for (int p = 0; p < P; ++p)
-              part[p] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
-                  c8, __builtin_bit_cast(h8, frag[((kc * P + p) * 4 + b) * 4 * rows]), part[p], 0, 0, 0);
-          }
-          if (P == 2) part[0] += part[P - 1];
-          const float X1 = SHIFT ? xg[(kc * NS + g) * kQR + row] : 0.f;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {   // word i's numbers: halves W16 i and on
-            const int at = W16 * i + g * (SHIFT ? 2 : 1);
-            const uint32_t s = ring[u].s[at / 2];
-            acc[i] = fmaf(__uint_as_float(at & 1 ? s & 0xffff0000u : s << 16), f * part[0][i], acc[i]);
-            if (SHIFT) acc[i] = fmaf(__uint_as_float(s & 0xffff0000u), X1, acc[i]);
+              for (int k = 0; k < RT; ++k)
+                part[k][p] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+                    c8, __builtin_bit_cast(h8, frag[k][((kc * P + p) * 4 + b) * 4 * rows]), part[k][p], 0, 0, 0);
+          }
+#pragma unroll
+          for (int k = 0; k < RT; ++k) {
+            if (P == 2) part[k][0] += part[k][P - 1];
+            const float X1 = SHIFT ? xg[(kc * NS + g) * R + row[k]] : 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {   // word i's numbers: halves W16 i and on
+              const int at = W16 * i + g * (SHIFT ? 2 : 1);
+              const uint32_t s = ring[u].s[at / 2];
+              acc[k][i] = fmaf(__uint_as_float(at & 1 ? s & 0xffff0000u : s << 16), f[k] * part[k][0][i], acc[k][i]);
+              if (SHIFT) acc[k][i] = fmaf(__uint_as_float(s & 0xffff0000u), X1, acc[k][i]);
+            }
           }
         }
       }
@@ -403,33 +419,42 @@ __global__ void __launch_bounds__(64 * kQW) k_quant_product(QuantJob a) {
       const int t = ((int)blockIdx.x + grp++ * (int)gridDim.x) * per + tw;
       if (S > 1) {
         __syncthreads();
-        if (ks > 0) red[w * 64 + lane] = acc;
+        if (ks > 0)
+#pragma unroll
+          for (int k = 0; k < RT; ++k) red[(w * RT + k) * 64 + lane] = acc[k];
         __syncthreads();
         if (ks == 0)
-          for (int o = 1; o < S; ++o) acc += red[(w + o) * 64 + lane];
+          for (int o = 1; o < S; ++o)
+#pragma unroll
+            for (int k = 0; k < RT; ++k) acc[k] += red[((w + o) * RT + k) * 64 + lane];
       }
       const int c = t * 16 + 4 * j;
-      if (ks == 0 && t < T && (lane & 15) < rows && c < a.q.C) {
-        const size_t at = (size_t)(r0 + row) * a.q.C + c;
+      if (ks == 0 && t < T && c < a.q.C) {
         const bool whole = c + 4 <= a.q.C;
-        float v[4];
+        float bias[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float bias = a.bias && (whole || c + i < a.q.C) ? a.bias[c + i] : 0.f;
-          v[i] = acc[i] + bias;
-        }
-        if (whole) {   // at any address that is aligned to its elements
-          typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
-          typedef uint32_t u2 __attribute__((ext_vector_type(2), aligned(2)));
-          if (a.ybf) *reinterpret_cast<u2*>((u16*)a.y + at) = u2{f2bf2(v[0], v[1]), f2bf2(v[2], v[3])};
-          else *reinterpret_cast<f4*>((float*)a.y + at) = f4{v[0], v[1], v[2], v[3]};
-        } else {
+        for (int i = 0; i < 4; ++i) bias[i] = a.bias && (whole || c + i < a.q.C) ? a.bias[c + i] : 0.f;
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (c + i < a.q.C) a.ybf ? store_one((u16*)a.y + at + i, v[i]) : store_one((float*)a.y + at + i, v[i]);
+        for (int k = 0; k < RT; ++k) {
+          if (k * kQR + (lane & 15) >= rows) continue;
+          const size_t at = (size_t)(r0 + row[k]) * a.q.C + c;
+          float v[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = acc[k][i] + bias[i];
+          if (whole) {   // at any address that is aligned to its elements
+            typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
+            typedef uint32_t u2 __attribute__((ext_vector_type(2), aligned(2)));
+            if (a.ybf) *reinterpret_cast<u2*>((u16*)a.y + at) = u2{f2bf2(v[0], v[1]), f2bf2(v[2], v[3])};
+            else *reinterpret_cast<f4*>((float*)a.y + at) = f4{v[0], v[1], v[2], v[3]};
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (c + i < a.q.C) a.ybf ? store_one((u16*)a.y + at + i, v[i]) : store_one((float*)a.y + at + i, v[i]);
+          }
         }
       }
-      acc = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < RT; ++k) acc[k] = v4f{0.f, 0.f, 0.f, 0.f};
     }
   }
 }
@@ -543,27 +568,41 @@ cavs_status quant_product_run(cavs_ctx* ctx, const cavs_quant* q, int x_type, co
   QuantJob a{quant_net(q, q->data), x, bias, y, n};
   a.ybf = y_type == CAVS_T_BF16;
   const int P = x_type == CAVS_T_F32 ? 2 : 1, T = a.q.T, KB = a.q.KB;
+  size_t shmem;
+  dim3 grid;
   // wavefronts of a tile: as many as leave each of 2048 something to do; two of long
   // tiles, whose blocks are then read in the order of memory by neighbours (16 x
   // 128 000 x 2048: 37.0 us with one, 35.8 with two, 36.1 with four; of 1024: one)
-  const int rows = cdiv(n, kQR);
-  const size_t block = (size_t)P * 256 * std::min(n, kQR) + 4 * kQR * (1 + (q->shift ? kQB / q->group : 0));
-  a.S = KB >= 16 ? 2 : 1;
-  while (a.S < 8 && a.S < KB && (long)T * a.S * rows < 2048) a.S *= 2;
-  const size_t red = a.S > 1 ? (size_t)kQW * 1024 : 0;
-  a.KC = std::min(cdiv(KB, a.S), (int)((kQLds - red) / block) / a.S) * a.S;
-  a.groups = cdiv(T, kQW / a.S);
-  const size_t shmem = a.KC * block + red;
-  // a workgroup per CU; the groups of rows of a tile on one XCD
-  const dim3 grid(std::min(a.groups, (int)align_up(cdiv(256, rows), 8)), rows);
+  auto plan = [&](int rt) {
+    const int rows = cdiv(n, kQR * rt);
+    const size_t block = (size_t)P * 256 * std::min(n, kQR * rt) + 4 * kQR * rt * (1 + (q->shift ? kQB / q->group : 0));
+    a.S = KB >= 16 ? 2 : 1;
+    const size_t sums = (size_t)kQW * rt * 1024;
+    while (a.S < 8 && a.S < KB && (long)T * a.S * rows < 2048 && 2 * a.S * block + sums <= kQLds) a.S *= 2;
+    const size_t red = a.S > 1 ? sums : 0;
+    a.KC = std::min(cdiv(KB, a.S), (int)((kQLds - red) / block) / a.S) * a.S;
+    a.groups = cdiv(T, kQW / a.S);
+    shmem = a.KC * block + red;
+    // a workgroup per CU; the groups of rows of a tile on one XCD
+    grid = dim3(std::min(a.groups, (int)align_up(cdiv(256, rows), 8)), rows);
+  };
+  // 32 rows of x to a workgroup where there are tiles for all wavefronts without
+  // sharing them and the rows are short enough to be in LDS once for all tiles: the
+  // codes become halves once for them (64 x 50 001 x 1024 in bf16 27 us with 16 rows and
+  // 21 with 32, 64 x 30 000 16.8 and 14.9; but 64 x 10 000 x 512 in fp32 8.6 and 9.5,
+  // 64 x 32 000 x 2048 32 and 38)
+  plan(2);
+  const bool two = n > kQR && KB < 16 && a.S == 1 && a.KC == KB;
+  if (!two) plan(1);
   by_group(q, [&](auto g, auto shift) {
     by_element(x_type, [&](auto t) {
       using X = decltype(t);
-      if (shmem > 64 << 10)
-        (void)hipFuncSetAttribute((const void*)k_quant_product<X, g(), shift()>,
-                                  hipFuncAttributeMaxDynamicSharedMemorySize, (int)shmem);
-      CAVS_LAUNCH("k_quant_product", (k_quant_product<X, g(), shift()>), grid, dim3(64 * kQW), shmem, ctx->stream,
-                  a);
+      auto launch = [&](auto kernel) {
+        if (shmem > 64 << 10)
+          (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)shmem);
+        CAVS_LAUNCH("k_quant_product", kernel, grid, dim3(64 * kQW), shmem, ctx->stream, a);
+      };
+      two ? launch(k_quant_product<X, g(), shift(), 2>) : launch(k_quant_product<X, g(), shift(), 1>);
     });
   });
   CAVS_LAUNCH_CHECK(ctx);
