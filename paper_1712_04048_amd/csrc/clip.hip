@@ -110,28 +110,31 @@ __device__ __forceinline__ double group_sum64(double v, double* lds) {
 }
 
 // f(v, i) of eight elements at a time, v their values, of [from, to); four steps'
-// loads are in flight where there are that many.
-template <class T, class F>
+// loads are in flight where there are that many.  DOWN: the last ones first.
+template <bool DOWN, class T, class F>
 __device__ __forceinline__ void clip_each(const T* g, long long from, long long to, F f) {
-  long long at = from;
   const int mine = threadIdx.x * 8;
-  for (; at + 4 * kChunk <= to; at += 4 * kChunk) {
-    Vec8<T> x[4];
+  auto steps = [&](auto count, long long at) {
+    Vec8<T> x[count];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) x[u].load(g + at + u * kChunk + mine);
+    for (int u = 0; u < count; ++u) x[u].load(g + at + u * kChunk + mine);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) f(x[u], at + u * kChunk + mine);
-  }
-  for (; at + kChunk <= to; at += kChunk) {
-    Vec8<T> x;
-    x.load(g + at + mine);
-    f(x, at + mine);
-  }
-  const long long i = at + mine;
-  if (i + 8 <= to) {
-    Vec8<T> x;
-    x.load(g + i);
-    f(x, i);
+    for (int u = 0; u < count; ++u) f(x[u], at + u * kChunk + mine);
+  };
+  const std::integral_constant<int, 4> four{};
+  const std::integral_constant<int, 1> one{};
+  const long long whole = (to - from) / kChunk, fours = whole / 4, rest = from + whole * kChunk;
+  auto last = [&] {
+    if (rest + mine + 8 <= to) steps(one, rest);
+  };
+  if (DOWN) {
+    last();
+    for (long long k = whole; k > fours * 4; --k) steps(one, from + (k - 1) * kChunk);
+    for (long long k = fours; k > 0; --k) steps(four, from + (k - 1) * 4 * kChunk);
+  } else {
+    for (long long k = 0; k < fours; ++k) steps(four, from + k * 4 * kChunk);
+    for (long long k = fours * 4; k < whole; ++k) steps(one, from + k * kChunk);
+    last();
   }
 }
 // Elements that are in none of those: fewer than eight, of one thread.
@@ -145,7 +148,7 @@ __device__ __forceinline__ void clip_rest(long long from, long long to, F f) {
 template <class T>
 __device__ __forceinline__ double clip_squares(const T* g, long long from, long long to) {
   double s[4] = {};   // four sums: one would wait for itself
-  clip_each(g, from, to, [&](const Vec8<T>& x, long long) {
+  clip_each<false>(g, from, to, [&](const Vec8<T>& x, long long) {
     float v[8];
     x.floats(v);
 #pragma unroll
@@ -193,7 +196,7 @@ __global__ void __launch_bounds__(kThreads) k_clip_norm(ClipSet a, uint32_t tota
 
 template <bool FAR, class T, class O>
 __device__ __forceinline__ void clip_scale(const T* g, O* out, long long from, long long to, float a, float f) {
-  clip_each(g, from, to, [&](const Vec8<T>& x, long long i) {
+  clip_each<true>(g, from, to, [&](const Vec8<T>& x, long long i) {
     float v[8];
     x.floats(v);
 #pragma unroll
@@ -208,8 +211,11 @@ __device__ __forceinline__ void clip_scale(const T* g, O* out, long long from, l
 }
 
 // Every workgroup adds up the slots by itself, in one order, and scales a run of
-// chunks: the last ones first, which the norm read last and the cache still holds.  A
-// norm that is not finite clips nothing.
+// chunks: the last runs first, each from its end on, and on the XCD whose workgroup
+// read it for the norm, so that what was read last is found in its cache (12 million
+// fp32 gradients in both launches: 30.2 us with runs on any XCD, 28.2 on their own,
+// 26.8 from their ends on; 111 million bf16 ones 111.8, 111.6 and 108.3).  A norm that
+// is not finite clips nothing.
 template <bool FAR>
 __global__ void __launch_bounds__(kThreads) k_clip_scale(const ClipEntry* table, int count, uint32_t total, int slots_n,
                                                          const double* slots, float scale, float max_norm,
@@ -217,9 +223,11 @@ __global__ void __launch_bounds__(kThreads) k_clip_scale(const ClipEntry* table,
   __shared__ double lds[kThreads / 64];
   const int lane = threadIdx.x & 63;
   const uint32_t per = (total + gridDim.x - 1) / gridDim.x;
-  uint32_t c = (gridDim.x - 1 - blockIdx.x) * per;
-  const uint32_t stop = min(c + per, total);
-  // the gradient of the first chunk, first among 64 times 64
+  const uint32_t eights = gridDim.x / 8, b = blockIdx.x;
+  const uint32_t start = (b / 8 < eights ? (eights - 1 - b / 8) * 8 + b % 8 : b) * per;
+  uint32_t stop = min(start + per, total);
+  // the gradient of the last chunk, first among 64 times 64
+  const uint32_t c = stop - 1;
   int k = 64 * __popcll(__ballot(64 * lane + 63 < count && table[min(64 * lane + 63, count - 1)].end <= c));
   k += __popcll(__ballot(k + lane < count && table[min(k + lane, count - 1)].end <= c));
   k = __builtin_amdgcn_readfirstlane(k);
@@ -231,11 +239,11 @@ __global__ void __launch_bounds__(kThreads) k_clip_scale(const ClipEntry* table,
   const double factor = norm > (double)max_norm && norm < INFINITY ? (double)scale * ((double)max_norm / norm) : scale;
   // a factor that fp32 holds only as a subnormal is two: the first loses nothing
   const float a = fabs(factor) < 0x1p-100 ? 0x1p-64f : 1.f, f = (float)(a == 1.f ? factor : factor * 0x1p64);
-  for (; c < stop; ++k) {
+  for (; start < stop; --k) {
     const ClipEntry e = table[k];
-    const uint32_t first = k ? table[k - 1].end : 0u, last = min(e.end, stop);
-    const long long from = (long long)(c - first) * kChunk, to = min((long long)(last - first) * kChunk, e.n);
-    c = last;
+    const uint32_t first = k ? table[k - 1].end : 0u, at = max(first, start);
+    const long long from = (long long)(at - first) * kChunk, to = min((long long)(stop - first) * kChunk, e.n);
+    stop = at;
     if (!e.out || (e.out == e.g && factor == 1.0)) continue;
     if (e.types & 1) e.types & 2 ? clip_scale<FAR>((const u16*)e.g, (u16*)e.out, from, to, a, f)
                                  : clip_scale<FAR>((const u16*)e.g, (float*)e.out, from, to, a, f);
