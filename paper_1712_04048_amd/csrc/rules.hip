@@ -7,6 +7,7 @@
 // and of each row the first of its largest v and ln sum exp v.  One pass over the
 // logits: bound by memory, the row in and out once.
 #include <algorithm>
+#include <utility>
 
 #include "vocab.h"
 
@@ -116,11 +117,18 @@ __device__ __forceinline__ void store_any(T* p, const float (&v)[V]) {
   }
 }
 
+// x[at] += e where `here`, at the same for the wavefront: one branch of many.
+template <int NV, int V, unsigned... S>
+__device__ __forceinline__ void add_at(float (&x)[NV][V], unsigned at, bool here, float e,
+                                       std::integer_sequence<unsigned, S...>) {
+  (void)((at == S && (x[S / V][S % V] = here ? x[S / V][S % V] + e : x[S / V][S % V], true)) || ...);
+}
+
 // A workgroup takes a piece, PER words a thread of one row, a thread vectors of V
 // adjacent ones, 16 bytes of the narrower type.  Everything that it reads is asked for
-// before anything is waited for.  Counts of the words so far and sums of the row's
-// own biases are kept in LDS for the piece's words alone; whole numbers and a fixed
-// order, so that no run differs.  Each wavefront leaves its largest v and its sum.
+// before anything is waited for.  Counts of the words so far are kept in LDS for the
+// piece's words alone; whole numbers, so that no run differs.  Each wavefront leaves
+// its largest v and its sum.
 // (Workgroups that go through pieces and ask for the next one ahead were slower: 256
 // x 128 000 in bf16 49 us, 39 with one for each piece.)
 template <class Z, class O, int THREADS, int PER, bool FAR>
@@ -132,9 +140,6 @@ __global__ void __launch_bounds__(THREADS) k_rules(RulesNet a, int row0, const Z
   const int tid = threadIdx.x, row = row0 + blockIdx.x / a.segs, c0 = blockIdx.x % a.segs * SEG;
   const int len = min(SEG, a.C - c0);
   uint32_t* count = reinterpret_cast<uint32_t*>(lds);
-  float* own = reinterpret_cast<float*>(lds + (a.past ? SEG / 4 : 0));
-  int* word = reinterpret_cast<int*>(own + (a.K ? SEG : 0));   // the row's own words and their biases
-  float* extra = reinterpret_cast<float*>(word + a.K);
   typedef Z Raw __attribute__((ext_vector_type(V), aligned(sizeof(Z))));
   Raw raw[NV];
   const Z* zr = z + (size_t)row * a.C + c0;
@@ -143,11 +148,24 @@ __global__ void __launch_bounds__(THREADS) k_rules(RulesNet a, int row0, const Z
     const int c = (k * THREADS + tid) * V;
     if (c + V <= len) raw[k] = *reinterpret_cast<const Raw*>(zr + c);
   }
-  constexpr int AHEAD = 2;
-  int said[AHEAD];
-#pragma unroll
-  for (int k = 0; k < AHEAD; ++k)
-    said[k] = a.past && k * THREADS + tid < a.L ? a.past[(size_t)row * a.L + k * THREADS + tid] : -1;
+  const int* past = a.past + (size_t)row * a.L;
+  auto ask = [&](int at, auto& w) {   // a thread's words of the past from `at` on
+    int k = 0;
+    for (int& x : w) {
+      x = at + k < a.L ? past[at + k] : -1;
+      k += THREADS;
+    }
+  };
+  int said[2];
+  if (a.past) ask(tid, said);
+  const int lane = tid & 63;
+  int word = -1;       // a wavefront's next 64 of the row's own words, and their biases
+  float extra = 0.f;
+  auto ask_own = [&](int at) {
+    word = at + lane < a.K ? a.word[(size_t)row * a.K + at + lane] : -1;
+    extra = at + lane < a.K ? a.extra[(size_t)row * a.K + at + lane] : 0.f;
+  };
+  if (a.K) ask_own(0);
   const float r = a.repeat ? a.repeat[row] : 1.f, p = a.presence ? a.presence[row] : 0.f;
   const float f = a.frequency ? a.frequency[row] : 0.f, T = a.temp ? a.temp[row] : 1.f;
   uint32_t bits[NV];
@@ -162,43 +180,53 @@ __global__ void __launch_bounds__(THREADS) k_rules(RulesNet a, int row0, const Z
       bits[k] = there && c < len ? mask[c / 32] >> (c % 32) : ~0u;
     }
   }
-  if (a.past || a.K) {
-    bool bad = false;
-    for (int i = tid; i < a.K; i += THREADS) {
-      const int w = a.word[(size_t)row * a.K + i];
-      word[i] = w;
-      extra[i] = a.extra[(size_t)row * a.K + i];
-      bad |= (unsigned)(w + 1) > (unsigned)a.C;
-    }
-    for (int i = tid; i < ((a.past ? SEG : 0) + (a.K ? SEG : 0)) / 4; i += THREADS) lds[i] = make_uint4(0, 0, 0, 0);
+  bool bad = false;
+  if (a.past) {
+    for (int i = tid; i < SEG / 4; i += THREADS) lds[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
-    if (a.past) {
-      auto one = [&](int w) {
+    auto count_in = [&](const auto& words) {
+      for (const int w : words) {
         if ((unsigned)(w - c0) < (unsigned)len) atomicAdd(&count[w - c0], 1u);
         bad |= (unsigned)(w + 1) > (unsigned)a.C;
-      };
-#pragma unroll
-      for (int k = 0; k < AHEAD; ++k) one(said[k]);
-      for (int i = AHEAD * THREADS + tid; i < a.L; i += THREADS) one(a.past[(size_t)row * a.L + i]);
-    }
-    for (int i = tid; i < a.K; i += THREADS) {
-      const int w = word[i];
-      if ((unsigned)(w - c0) >= (unsigned)len) continue;
-      // the first of a word's places adds all of them
-      bool first = true;
-      float s = extra[i];
-#pragma unroll 8
-      for (int j = 0; j < a.K; ++j) {
-        const bool same = word[j] == w;
-        first &= !same || j >= i;
-        s = same && j > i ? s + extra[j] : s;
       }
-      if (!first) continue;
-      own[w - c0] = s;
+    };
+    count_in(said);
+    for (int at = 2 * THREADS; at < a.L; at += 8 * THREADS) {
+      int more[8];
+      ask(at + tid, more);
+      count_in(more);
     }
-    if (bad) a.err[1] = 1;
     __syncthreads();
   }
+  // The row's own biases: each wavefront looks for those of its words and adds them up,
+  // in the list's order, in the registers of the lane that has the word.  (Through a
+  // table of the piece's words in LDS, 126 x 130 000 with 64 of them took 45 us, 24
+  // without any.)
+  float own[NV][V];
+  if (a.K) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int i = 0; i < V; ++i) own[k][i] = 0.f;
+    for (int at = 0; at < a.K; at += 64) {
+      const int c = word - c0;
+      const float e = extra;
+      bad |= (unsigned)(word + 1) > (unsigned)a.C;
+      unsigned long long mine =
+          __ballot((unsigned)c < (unsigned)len && (unsigned)c / V % THREADS / 64 == (unsigned)tid / 64);
+      if (at + 64 < a.K) ask_own(at + 64);
+      while (mine) {
+        const int l = __ffsll(mine) - 1;
+        mine &= mine - 1;
+        const unsigned cl = __builtin_amdgcn_readlane(c, l);
+        const float el = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(e), l));
+        const bool here = lane == (int)(cl / V % 64);
+        const unsigned slot = cl / V / THREADS * V + cl % V;
+        add_at(own, slot, here, el, std::make_integer_sequence<unsigned, PER>{});
+      }
+    }
+  }
+  if (bad) a.err[1] = 1;
   float v[NV][V];
   Top top{-INFINITY, 1 << 20};
   float sum = 0.f;
@@ -255,10 +283,7 @@ __global__ void __launch_bounds__(THREADS) k_rules(RulesNet a, int row0, const Z
     }
     if (a.K)
 #pragma unroll
-      for (int i = 0; i < V; i += 4) {
-        const float4 y = *reinterpret_cast<const float4*>(own + c + i);
-        x[i] = x[i] + y.x, x[i + 1] = x[i + 1] + y.y, x[i + 2] = x[i + 2] + y.z, x[i + 3] = x[i + 3] + y.w;
-      }
+      for (int i = 0; i < V; ++i) x[i] = x[i] + own[k][i];
     if (a.mask)
 #pragma unroll
       for (int i = 0; i < V; ++i) x[i] = bits[k] >> i & 1u ? x[i] : -INFINITY;
@@ -358,7 +383,7 @@ cavs_status adjust_run(cavs_ctx* ctx, const cavs_rules* r, const void* z, void* 
   a.lse = lse;
   a.part = (float4*)ws;
   // a row of up to 16 384 words in one workgroup, without a join
-  const bool wide = r->C <= 1024 * kPer && r->C > 256 * kPer && !(a.past && a.K);
+  const bool wide = r->C <= 1024 * kPer && r->C > 256 * kPer;
   const int threads = wide ? 1024 : 256;
   const bool few = !wide && (long)r->n * cdiv(r->C, 256 * kPer) < 2048 && r->C > 256 * kPer;
   const int per = few ? kPerFew : kPer;
@@ -371,7 +396,7 @@ cavs_status adjust_run(cavs_ctx* ctx, const cavs_rules* r, const void* z, void* 
     if (!ws || ws_bytes < need) return fail(ctx, CAVS_ERR_WORKSPACE, "workspace too small: %zu < %zu", ws_bytes, need);
     if (((uintptr_t)ws & 15) != 0) return fail(ctx, CAVS_ERR_ARG, "ws must be aligned to 16 bytes");
   }
-  const size_t shmem = (size_t)threads * per * 4 * ((a.past ? 1 : 0) + (a.K ? 1 : 0)) + 8 * (size_t)a.K;
+  const size_t shmem = a.past ? (size_t)threads * per * 4 : 0;
   // a launch has fewer than 2^32 threads
   const int step = std::max(1, (int)std::min<long>(r->n, (1l << 30) / threads / a.segs));
   for (int i = 0; i < r->n; i += step) {
@@ -380,8 +405,6 @@ cavs_status adjust_run(cavs_ctx* ctx, const cavs_rules* r, const void* z, void* 
       using Z = decltype(zt);
       using O = decltype(ot);
       auto launch = [&](const char* name, auto kernel) {
-        if (shmem > 64 << 10)
-          (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)shmem);
         CAVS_LAUNCH(name, kernel, grid, dim3(threads), shmem, ctx->stream, a, i, (const Z*)z, (O*)out);
       };
       if (wide) launch("k_rules<1024, 16>", k_rules<Z, O, 1024, kPer, false>);

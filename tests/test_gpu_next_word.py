@@ -105,7 +105,9 @@ def _state(c, seed, n=5, H=256, C=20000):
              x=torch.empty(n, H, device="cuda"), z=torch.empty(n, C, device="cuda"), b=randn(C),
              best=torch.empty(n, dtype=torch.int32, device="cuda"), lse=torch.empty(n, device="cuda"))
     s["q"] = B.QuantWeights(torch.empty(B.quant_bytes(H, C), dtype=torch.uint8, device="cuda"), H, C)
-    B.quant_pack(c, s["q"], randn(H, C) / 16)
+    s["W"] = randn(H, C) / 16
+    torch.cuda.synchronize()   # made on torch's stream, read on the context's
+    B.quant_pack(c, s["q"], s["W"])
     s["rules"] = B.LogitRules(past=torch.randint(-1, C, (n, 50), generator=g, device="cuda").int(),
                               frequency=torch.rand(n, generator=g, device="cuda"))
     s["ws"] = torch.empty(B.adjust_workspace_bytes(n, C), dtype=torch.uint8, device="cuda")
