@@ -509,6 +509,52 @@ void by_element(int type, F f) {
   type == CAVS_T_BF16 ? f(u16{}) : f(float{});
 }
 
+// At most kQuantStep rows of x, whose groups of sixteen are a grid's second dimension.
+constexpr int kQuantStep = 1 << 19;
+void quant_product_launch(cavs_ctx* ctx, const cavs_quant* q, int x_type, const void* x, int n, const float* bias,
+                          int y_type, void* y) {
+  QuantJob a{quant_net(q, q->data), x, bias, y, n};
+  a.ybf = y_type == CAVS_T_BF16;
+  const int P = x_type == CAVS_T_F32 ? 2 : 1, T = a.q.T, KB = a.q.KB;
+  size_t shmem;
+  dim3 grid;
+  // wavefronts of a tile: as many as leave each of 2048 something to do; two of long
+  // tiles, whose blocks are then read in the order of memory by neighbours (16 x
+  // 128 000 x 2048: 37.0 us with one, 35.8 with two, 36.1 with four; of 1024: one)
+  auto plan = [&](int rt) {
+    const int rows = cdiv(n, kQR * rt);
+    const size_t block = (size_t)P * 256 * std::min(n, kQR * rt) + 4 * kQR * rt * (1 + (q->shift ? kQB / q->group : 0));
+    a.S = KB >= 16 ? 2 : 1;
+    const size_t sums = (size_t)kQW * rt * 1024;
+    while (a.S < 8 && a.S < KB && (long)T * a.S * rows < 2048 && 2 * a.S * block + sums <= kQLds) a.S *= 2;
+    const size_t red = a.S > 1 ? sums : 0;
+    a.KC = std::min(cdiv(KB, a.S), (int)((kQLds - red) / block) / a.S) * a.S;
+    a.groups = cdiv(T, kQW / a.S);
+    shmem = a.KC * block + red;
+    // a workgroup per CU; the groups of rows of a tile on one XCD
+    grid = dim3(std::min(a.groups, (int)align_up(cdiv(256, rows), 8)), rows);
+  };
+  // 32 rows of x to a workgroup where there are tiles for all wavefronts without
+  // sharing them and the rows are short enough to be in LDS once for all tiles: the
+  // codes become halves once for them (64 x 50 001 x 1024 in bf16 27 us with 16 rows and
+  // 21 with 32, 64 x 30 000 16.8 and 14.9; but 64 x 10 000 x 512 in fp32 8.6 and 9.5,
+  // 64 x 32 000 x 2048 32 and 38)
+  plan(2);
+  const bool two = n > kQR && KB < 16 && a.S == 1 && a.KC == KB;
+  if (!two) plan(1);
+  by_group(q, [&](auto g, auto shift) {
+    by_element(x_type, [&](auto t) {
+      using X = decltype(t);
+      auto launch = [&](auto kernel) {
+        if (shmem > 64 << 10)
+          (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)shmem);
+        CAVS_LAUNCH("k_quant_product", kernel, grid, dim3(64 * kQW), shmem, ctx->stream, a);
+      };
+      two ? launch(k_quant_product<X, g(), shift(), 2>) : launch(k_quant_product<X, g(), shift(), 1>);
+    });
+  });
+}
+
 }  // namespace
 
 size_t quant_bytes(const cavs_quant* q) {
@@ -565,46 +611,10 @@ cavs_status quant_product_run(cavs_ctx* ctx, const cavs_quant* q, int x_type, co
   if (st == CAVS_OK) st = quant_data(ctx, q->data);
   if (st != CAVS_OK) return st;
   if (((uintptr_t)bias & 3) != 0) return fail(ctx, CAVS_ERR_ARG, "bias is not aligned to its elements");
-  QuantJob a{quant_net(q, q->data), x, bias, y, n};
-  a.ybf = y_type == CAVS_T_BF16;
-  const int P = x_type == CAVS_T_F32 ? 2 : 1, T = a.q.T, KB = a.q.KB;
-  size_t shmem;
-  dim3 grid;
-  // wavefronts of a tile: as many as leave each of 2048 something to do; two of long
-  // tiles, whose blocks are then read in the order of memory by neighbours (16 x
-  // 128 000 x 2048: 37.0 us with one, 35.8 with two, 36.1 with four; of 1024: one)
-  auto plan = [&](int rt) {
-    const int rows = cdiv(n, kQR * rt);
-    const size_t block = (size_t)P * 256 * std::min(n, kQR * rt) + 4 * kQR * rt * (1 + (q->shift ? kQB / q->group : 0));
-    a.S = KB >= 16 ? 2 : 1;
-    const size_t sums = (size_t)kQW * rt * 1024;
-    while (a.S < 8 && a.S < KB && (long)T * a.S * rows < 2048 && 2 * a.S * block + sums <= kQLds) a.S *= 2;
-    const size_t red = a.S > 1 ? sums : 0;
-    a.KC = std::min(cdiv(KB, a.S), (int)((kQLds - red) / block) / a.S) * a.S;
-    a.groups = cdiv(T, kQW / a.S);
-    shmem = a.KC * block + red;
-    // a workgroup per CU; the groups of rows of a tile on one XCD
-    grid = dim3(std::min(a.groups, (int)align_up(cdiv(256, rows), 8)), rows);
-  };
-  // 32 rows of x to a workgroup where there are tiles for all wavefronts without
-  // sharing them and the rows are short enough to be in LDS once for all tiles: the
-  // codes become halves once for them (64 x 50 001 x 1024 in bf16 27 us with 16 rows and
-  // 21 with 32, 64 x 30 000 16.8 and 14.9; but 64 x 10 000 x 512 in fp32 8.6 and 9.5,
-  // 64 x 32 000 x 2048 32 and 38)
-  plan(2);
-  const bool two = n > kQR && KB < 16 && a.S == 1 && a.KC == KB;
-  if (!two) plan(1);
-  by_group(q, [&](auto g, auto shift) {
-    by_element(x_type, [&](auto t) {
-      using X = decltype(t);
-      auto launch = [&](auto kernel) {
-        if (shmem > 64 << 10)
-          (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)shmem);
-        CAVS_LAUNCH("k_quant_product", kernel, grid, dim3(64 * kQW), shmem, ctx->stream, a);
-      };
-      two ? launch(k_quant_product<X, g(), shift(), 2>) : launch(k_quant_product<X, g(), shift(), 1>);
-    });
-  });
+  const size_t xs = (size_t)q->H * (x_type == CAVS_T_BF16 ? 2 : 4), ys = (size_t)q->C * (y_type == CAVS_T_BF16 ? 2 : 4);
+  for (int at = 0; at < n; at += kQuantStep)
+    quant_product_launch(ctx, q, x_type, (const char*)x + at * xs, std::min(n - at, kQuantStep), bias, y_type,
+                         (char*)y + at * ys);
   CAVS_LAUNCH_CHECK(ctx);
   return CAVS_OK;
 }

@@ -58,8 +58,25 @@ def test_weights_past_2_32(ctx):
     assert R.outside(y[:, C - 300:], w, bound) <= 1.0
 
 
+@pytest.mark.parametrize("H", [64, 2000])
+def test_the_most_rows(ctx, H):
+    """2^20 rows, in groups of 32 and of 16; the first, the last and those between."""
+    n, C = 1 << 20, 21
+    x = _fill((n, H), 4)
+    W = torch.randn(H, C, generator=torch.Generator("cuda").manual_seed(5), device="cuda")
+    q = B.QuantWeights(torch.empty(B.quant_bytes(H, C, 64), dtype=torch.uint8, device="cuda"), H, C, 64)
+    B.quant_pack(ctx, q, W)
+    y = torch.full((n, C), float("nan"), device="cuda")
+    B.quant_product(ctx, q, x, y)
+    ctx.sync()
+    assert not torch.isnan(y).any()
+    for at in (0, (1 << 19) - 40, n - 80):
+        w, b = R.product(x[at:at + 80], *R.quantise(W, 64, False), 64, None, False)
+        assert R.outside(y[at:at + 80], w, b) <= 1.0
+
+
 def test_logits_past_2_32(ctx):
-    """2049 rows of 2^20 + .. words: scored and adjusted, the last rows looked at."""
+    """4100 rows of 2^20 words: scored and adjusted, rows on both sides looked at."""
     H, C, n = 32, 1 << 20, 4100
     g = torch.Generator("cuda").manual_seed(3)
     W = torch.randn(H, C, generator=g, device="cuda")
