@@ -461,8 +461,9 @@ cavs_status cavs_clip_grads(cavs_ctx* ctx, const cavs_grad* grads, int32_t count
  * q - 8 the nearest whole number to (w - m) / s (the even one of two), kept in
  * -8 .. 7.  Without shifts m = 0 and s = -e / 8, e the group's end that is further
  * from 0 (the lower of two alike); with them s = (highest - lowest) / 15 and m =
- * (highest + lowest + s) / 2.  Both are rounded to fp32 and that to bf16 before q is taken; a group
- * of zeros has s = 0; one with a weight that is not finite has s = NaN.
+ * (highest + lowest + s) / 2.  Both are rounded to fp32 and that to bf16 before q is taken; where
+ * s = 0, as in a group of zeros or, with shifts, of one value, q = 8; a group with a weight
+ * that is not finite has s = NaN, m = 0, q = 8.
  *
  * `data` is cavs_quant_bytes(q) bytes, aligned to 16, that cavs_quant_pack writes
  * and a program may keep in files.  With T = ceil(C / 16) and KB = ceil(H / 128):
@@ -492,8 +493,10 @@ cavs_status cavs_quant_unpack(cavs_ctx* ctx, const cavs_quant* q, int32_t w_type
 
 /* y [n, C] = x [n, H] What + bias (bias [C] or NULL), n <= 2^20, made for the few
    rows of a decoding step.  x is not rounded (an fp32 x by 2^-24 of it at most);
-   products are exact, sums fp32, y is rounded once.  A row of x that is not finite
-   gives infinities or NaN in that row alone. */
+   products are exact, sums fp32, y is rounded once.  Of the 128 columns from a
+   multiple of 128 on, values below 2^-32 of a row's largest, and all below 2^-112,
+   keep fewer bits; values of 2^115 and more may give infinities where y has none.
+   A row of x that is not finite gives infinities or NaN in that row alone. */
 cavs_status cavs_quant_product(cavs_ctx* ctx, const cavs_quant* q, int32_t x_type, const void* x,
                                int32_t n, const float* bias, int32_t y_type, void* y);
 

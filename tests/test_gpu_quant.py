@@ -167,6 +167,24 @@ def test_rows_of_very_different_magnitudes(ctx, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("shift", [False, True])
+def test_the_largest_and_smallest_values_of_x(ctx, dtype, shift):
+    """Just below 2^115, all codes -8 and of one sign, so that a group's sum is the
+    largest there is; and 2^-112."""
+    W = torch.full((256, 20), 0.125)
+    W[::2, 10:] = -0.125
+    x = torch.full((2, 256), 2.0 ** 115 * (1 - 2.0 ** -8))
+    x[1] = 2.0 ** -112
+    x, W = x.to(dtype).cuda(), W.cuda()
+    q = _packed(ctx, W, 128, shift)
+    y = torch.empty(2, 20, device="cuda")
+    B.quant_product(ctx, q, x, y)
+    ctx.sync()
+    want, bound = R.product(x, *R.quantise(W, 128, shift), 128, None, False)
+    assert R.outside(y, want, bound) <= 1.0
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("n", [3, 40])
 def test_rows_that_are_not_finite_stay_alone(ctx, dtype, n):
     g = torch.Generator().manual_seed(5)
