@@ -214,6 +214,8 @@ class LmBatch(Batch):
     def quantise(self, group: int = 128, shift: bool = False):
         """The head in 4 bits, which next_words scores with (cavs_quant_pack)."""
         H, C = self.Ws.shape
+        if self.quant is not None:
+            self.ctx.sync()   # an earlier call may still be reading what is replaced
         data = torch.empty(B.quant_bytes(H, C, group, shift), dtype=torch.uint8, device=self.dev)
         self.quant = B.QuantWeights(data, H, C, group, shift)
         B.quant_pack(self.ctx, self.quant, self.Ws)
@@ -222,7 +224,8 @@ class LmBatch(Batch):
         """The likeliest word at each of ``vertices`` (int32 [n], on the device: the
         last ones of the sequences, as a rule) under the rules, -1 where they allow
         none: the states, their rows, the head in 4 bits, the rules.  ``logits``
-        [n, C] and ``lse`` [n] hold what the words were taken from.  After alloc()."""
+        [n, C] and ``lse`` [n] hold what the words were taken from.  After alloc().
+        Holds the vertices and rules of its last call: wait (ctx.sync()) before others."""
         n, C, dev = int(vertices.shape[0]), int(self.Ws.shape[1]), self.dev
         if self.quant is None:
             self.quantise()

@@ -83,3 +83,11 @@ def test_next_words(made):
     assert b.next_words(last) is best and b.ctx.synced == waits and seen[-1][1][1] is b.rules
     assert [s[0] for s in seen].count("quant_pack") == 1
     assert b.next_words(last[:1].clone()) is not best and b.ctx.synced == waits + 1
+
+
+def test_a_head_is_quantised_again_after_a_wait(made):
+    b, seen = made()
+    b.quantise(64)
+    waits, first = b.ctx.synced, b.quant
+    b.quantise(32, True)
+    assert b.ctx.synced == waits + 1 and b.quant is not first and (b.quant.group, b.quant.shift) == (32, True)
