@@ -158,6 +158,7 @@ class LmBatch(Batch):
         self.head: Optional[B.VocabHead] = None
         self.max_norm = max_norm
         self.quant: Optional[B.QuantWeights] = None
+        self.rounded = (None, None, None)   # what quantise() made, of which weights, torch's count of their changes
 
     def alloc(self):
         super().alloc()
@@ -193,6 +194,7 @@ class LmBatch(Batch):
                      self.ws_head)
 
     def backward(self):
+        self.rounded = (self.rounded[0], None, None)   # what the gradients change may be the head
         super().backward()
         B.embed_grad(self.ctx, self.emb, self.words, self.grads["dX"], self.grads["dE"], self.ws_emb)
         if self.max_norm is not None:
@@ -211,24 +213,40 @@ class LmBatch(Batch):
         self._states()
         B.vocab_loss(self.ctx, self.head, self.loss, self.row_loss, self.ws_head)
 
+    def _head_now(self):
+        """The head's weights and torch's count of their changes (None: not counted)."""
+        return self.Ws, None if self.Ws.is_inference() else self.Ws._version
+
     def quantise(self, group: int = 128, shift: bool = False):
-        """The head in 4 bits, which next_words scores with (cavs_quant_pack)."""
+        """The head in 4 bits, which next_words scores with (cavs_quant_pack): the
+        weights as they are now, into the memory of the last call where that had the
+        same form (so a captured next_words finds them there)."""
         H, C = self.Ws.shape
-        if self.quant is not None:
-            self.ctx.sync()   # an earlier call may still be reading what is replaced
-        data = torch.empty(B.quant_bytes(H, C, group, shift), dtype=torch.uint8, device=self.dev)
-        self.quant = B.QuantWeights(data, H, C, group, shift)
-        B.quant_pack(self.ctx, self.quant, self.Ws)
+        (Ws, count), q = self._head_now(), self.quant
+        mine = q is not None and q is self.rounded[0]
+        if not mine or (q.H, q.C, q.group, q.shift) != (H, C, group, bool(shift)):
+            if q is not None:
+                self.ctx.sync()   # an earlier call may still be reading what is replaced
+            data = torch.empty(B.quant_bytes(H, C, group, shift), dtype=torch.uint8, device=self.dev)
+            q = self.quant = B.QuantWeights(data, H, C, group, bool(shift))
+        B.quant_pack(self.ctx, q, Ws)
+        self.rounded = (q, Ws, count)
 
     def next_words(self, vertices: torch.Tensor, rules: Optional[B.LogitRules] = None) -> torch.Tensor:
         """The likeliest word at each of ``vertices`` (int32 [n], on the device: the
         last ones of the sequences, as a rule) under the rules, -1 where they allow
         none: the states, their rows, the head in 4 bits, the rules.  ``logits``
         [n, C] and ``lse`` [n] hold what the words were taken from.  After alloc().
+        A head that quantise() made is rounded anew, in its form, after a backward() and
+        where torch has counted a change of Ws; after any other change (a fused optimiser
+        without a backward(), ``Ws.data``, replays of a captured step) call quantise().
         Holds the vertices and rules of its last call: wait (ctx.sync()) before others."""
         n, C, dev = int(vertices.shape[0]), int(self.Ws.shape[1]), self.dev
         if self.quant is None:
             self.quantise()
+        made, Ws, count = self.rounded
+        if made is self.quant and (Ws is not self.Ws or count != self._head_now()[1]):
+            self.quantise(made.group, made.shift)
         if getattr(self, "best", None) is None or self.best.shape[0] != n:
             self.ctx.sync()   # an earlier call may still be using what is replaced
             self.rows = torch.empty(n, self.wl.H, dtype=torch.float32, device=dev)

@@ -1,0 +1,74 @@
+"""When runner.LmBatch rounds its head to 4 bits again (CPU only: the calls are
+replaced by ones that record their arguments)."""
+import torch
+
+from paper_1712_04048_amd import binding as B
+from test_lm_next import _float32_by_default, made  # noqa: F401
+
+LAST = torch.tensor([2, 9, 14], dtype=torch.int32)
+
+
+def _packs(seen):
+    return [s[1] for s in seen if s[0] == "quant_pack"]
+
+
+def test_a_changed_head_is_rounded_again_where_it_is(made):
+    """After weights that torch has changed, and after a step's gradients, whatever
+    changes the weights then: into the same memory, in the same form, without a wait."""
+    b, seen = made()
+    b.quantise(64, True)
+    b.next_words(LAST)
+    first, waits = b.quant, b.ctx.synced
+
+    def renewed(times):
+        b.next_words(LAST)
+        b.next_words(LAST)
+        packs = _packs(seen)
+        assert len(packs) == times and packs[-1][2] is b.Ws
+        assert packs[-1][1].data is first.data and (b.quant.group, b.quant.shift) == (64, True)
+        assert b.ctx.synced == waits
+
+    renewed(1)
+    b.Ws.add_(1.0)
+    renewed(2)
+    with torch.no_grad():
+        b.Ws.view(-1)[3] = 7.0
+    renewed(3)
+    b.forward()
+    renewed(3)
+    b.backward()
+    renewed(4)
+    b.Ws = b.Ws.clone()
+    renewed(5)
+    b.quantise(64, True)
+    renewed(6)
+
+
+def test_a_head_whose_changes_torch_does_not_count(made):
+    """Weights made in inference mode have no count of their changes: a step's
+    gradients and quantise() renew them."""
+    b, seen = made()
+    with torch.inference_mode():
+        b.Ws = b.Ws.clone()
+    b.next_words(LAST)
+    b.next_words(LAST)
+    assert len(_packs(seen)) == 1
+    b.backward()
+    b.next_words(LAST)
+    assert len(_packs(seen)) == 2
+
+
+def test_a_head_of_the_program_s_own_stays(made):
+    """Packed weights that the program has put there (from a file, say) are not written."""
+    b, seen = made()
+    b.quantise(64)
+    own = B.QuantWeights(torch.full_like(b.quant.data, 9), 64, 9, 64)
+    for b.quant in (own, own):
+        b.backward()
+        b.Ws.add_(1.0)
+        b.next_words(LAST)
+    assert len(_packs(seen)) == 1 and b.quant is own
+    b.quantise(64)
+    assert len(_packs(seen)) == 2 and b.quant is not own and _packs(seen)[-1][1].data is not own.data
+    b.next_words(LAST)
+    assert len(_packs(seen)) == 2
