@@ -223,14 +223,14 @@ class LmBatch(Batch):
         same form (so a captured next_words finds them there)."""
         H, C = self.Ws.shape
         (Ws, count), q = self._head_now(), self.quant
-        mine = q is not None and q is self.rounded[0]
-        if not mine or (q.H, q.C, q.group, q.shift) != (H, C, group, bool(shift)):
-            if q is not None:
-                self.ctx.sync()   # an earlier call may still be reading what is replaced
+        if q is None or q is not self.rounded[0] or (q.H, q.C, q.group, q.shift) != (H, C, group, bool(shift)):
             data = torch.empty(B.quant_bytes(H, C, group, shift), dtype=torch.uint8, device=self.dev)
-            q = self.quant = B.QuantWeights(data, H, C, group, bool(shift))
+            q = B.QuantWeights(data, H, C, group, bool(shift))
         B.quant_pack(self.ctx, q, Ws)
-        self.rounded = (q, Ws, count)
+        if self.quant is not None and q is not self.quant:
+            self.ctx.sync()   # an earlier call may still be reading what is replaced
+        # a form that is refused has left all as it was
+        self.quant, self.rounded = q, (q, Ws, count)
 
     def next_words(self, vertices: torch.Tensor, rules: Optional[B.LogitRules] = None) -> torch.Tensor:
         """The likeliest word at each of ``vertices`` (int32 [n], on the device: the

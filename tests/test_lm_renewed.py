@@ -72,3 +72,24 @@ def test_a_head_of_the_program_s_own_stays(made):
     assert len(_packs(seen)) == 2 and b.quant is not own and _packs(seen)[-1][1].data is not own.data
     b.next_words(LAST)
     assert len(_packs(seen)) == 2
+
+
+def test_a_form_that_is_refused_leaves_the_head(made, monkeypatch):
+    b, seen = made()
+    b.quantise(64)
+    first = b.quant
+
+    def refuse(*a):
+        raise B.CavsError(B.ERR_ARG, "refused")
+    with monkeypatch.context() as m:
+        m.setattr(B, "quant_pack", refuse)
+        for form in ((48, False), (64, True)):
+            try:
+                b.quantise(*form)
+            except B.CavsError:
+                pass
+            else:
+                raise AssertionError(form)
+            assert b.quant is first
+    b.next_words(LAST)
+    assert len(_packs(seen)) == 1
