@@ -237,6 +237,8 @@ class LmBatch(Batch):
         last ones of the sequences, as a rule) under the rules, -1 where they allow
         none: the states, their rows, the head in 4 bits, the rules.  ``logits``
         [n, C] and ``lse`` [n] hold what the words were taken from.  After alloc().
+        All three are the batch's own and the next call of as many rows writes them
+        again: copy what is to be kept.
         A head that quantise() made is rounded anew, in its form, after a backward() and
         where torch has counted a change of Ws; after any other change (a fused optimiser
         without a backward(), ``Ws.data``, replays of a captured step) call quantise().

@@ -93,3 +93,11 @@ def test_a_form_that_is_refused_leaves_the_head(made, monkeypatch):
             assert b.quant is first
     b.next_words(LAST)
     assert len(_packs(seen)) == 1
+
+
+def test_what_is_returned_lasts_until_the_next_call(made):
+    """As next_words says: one buffer for all calls of as many rows."""
+    b, seen = made()
+    first = b.next_words(LAST)
+    held = (b.logits, b.lse)
+    assert b.next_words(LAST) is first and (b.logits, b.lse) == held
