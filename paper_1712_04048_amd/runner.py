@@ -242,7 +242,9 @@ class LmBatch(Batch):
         A head that quantise() made is rounded anew, in its form, after a backward() and
         where torch has counted a change of Ws; after any other change (a fused optimiser
         without a backward(), ``Ws.data``, replays of a captured step) call quantise().
-        Holds the vertices and rules of its last call: wait (ctx.sync()) before others."""
+        Holds the vertices and rules of its last call: wait (ctx.sync()) before others.
+        A call captured into a graph uses this batch's buffers: after a call of another
+        number of rows, a head of another form or alloc(), capture it again."""
         n, C, dev = int(vertices.shape[0]), int(self.Ws.shape[1]), self.dev
         if self.quant is None:
             self.quantise()
