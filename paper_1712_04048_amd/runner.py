@@ -183,7 +183,10 @@ class LmBatch(Batch):
         if self.max_norm is not None:
             self.norm = torch.empty(1, dtype=torch.float32, device=dev)
             self.ws_clip = torch.empty(B.clip_workspace_bytes(), **u8)
-            self.clip = B.GradList([g for k, g in self.grads.items() if k != "dX"])
+            self.clip = B.GradList(self._clipped())
+
+    def _clipped(self) -> list:
+        return [g for k, g in self.grads.items() if k != "dX" and g is not None]
 
     def forward(self):
         B.embed(self.ctx, self.emb, self.words, self.X)
@@ -198,6 +201,9 @@ class LmBatch(Batch):
         super().backward()
         B.embed_grad(self.ctx, self.emb, self.words, self.grads["dX"], self.grads["dE"], self.ws_emb)
         if self.max_norm is not None:
+            now = self._clipped()
+            if len(now) != len(self.clip.grads) or any(a is not b for a, b in zip(now, self.clip.grads)):
+                self.clip = B.GradList(now)   # the program has replaced some
             B.clip_grads(self.ctx, self.clip, self.max_norm, self.norm, self.ws_clip)
 
     def _states(self):

@@ -101,3 +101,18 @@ def test_what_is_returned_lasts_until_the_next_call(made):
     first = b.next_words(LAST)
     held = (b.logits, b.lse)
     assert b.next_words(LAST) is first and (b.logits, b.lse) == held
+
+
+def test_the_gradients_that_are_written_are_clipped(made):
+    """Those that the program has put into ``grads`` after alloc() too; none that it left out."""
+    b, seen = made(max_norm=1.0)
+    b.backward()
+    listed = b.clip
+    b.backward()
+    assert b.clip is listed
+    b.grads["dWs"] = torch.empty_like(b.grads["dWs"])
+    b.grads["dU"] = None
+    b.backward()
+    name, args, _ = seen[-1]
+    assert name == "clip_grads" and args[1] is b.clip and len(args[1].grads) == 5
+    assert {id(g) for g in args[1].grads} == {id(g) for k, g in b.grads.items() if k not in ("dX", "dU")}
