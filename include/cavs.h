@@ -492,11 +492,12 @@ cavs_status cavs_quant_pack(cavs_ctx* ctx, const cavs_quant* q, int32_t w_type, 
 cavs_status cavs_quant_unpack(cavs_ctx* ctx, const cavs_quant* q, int32_t w_type, void* W);
 
 /* y [n, C] = x [n, H] What + bias (bias [C] or NULL), n <= 2^20, made for the few
-   rows of a decoding step.  x is not rounded (an fp32 x by 2^-24 of it at most);
-   products are exact, sums fp32, y is rounded once.  Of the 128 columns from a
-   multiple of 128 on, values below 2^-32 of a row's largest, and all below 2^-112,
-   keep fewer bits; values of 2^115 and more may give infinities where y has none.
-   A row of x that is not finite gives infinities or NaN in that row alone. */
+   rows of a decoding step.  Products are exact, sums fp32, y is rounded once.  Of x,
+   a bf16 value is off by at most 2^-39 of the largest finite value that its row has
+   in the 128 columns from a multiple of 128 on (none from 2^-31 of that one on), an
+   fp32 value by that or by 2^-23 of itself, whichever is more.  Values of 2^115 and
+   more may give infinities where y has none.  A row of x that is not finite gives
+   infinities or NaN in that row alone. */
 cavs_status cavs_quant_product(cavs_ctx* ctx, const cavs_quant* q, int32_t x_type, const void* x,
                                int32_t n, const float* bias, int32_t y_type, void* y);
 

@@ -220,10 +220,12 @@ __device__ __forceinline__ h8 halves(uint32_t w, const QuantBits& k) {
 //   sum x What = sum over groups of s (sum x (q - 8)) + m X.
 // x is scaled by a power of two 2^up for each row and block of 128 columns, so that
 // the block's largest finite value lies in 2^14 .. 2^15: a half then holds what a bf16
-// has (values 2^-32 of the block's largest and less lose bits, which is less than an
-// fp32 sum keeps of them); an fp32 x is the sum of two halves, 2^-24 of it away at
-// most, or 2^-39 of the block's largest.  Products of halves and codes are exact,
-// their sums are fp32.
+// has, but that values below 2^-31 of the block's largest are off by up to half a
+// half's smallest step, 2^-25, which is 2^-39 of the largest (less than an fp32 sum
+// keeps of them).  An fp32 x is the sum of two halves: what the first leaves is at most
+// 2^12 steps of x's last bit and the second holds 11 bits of it, so that one step,
+// 2^-23 of x, may be lost, or the same 2^-39 of the largest where that is more (below
+// some 2^-16 of it).  Products of halves and codes are exact, their sums are fp32.
 //   LDS: xh [KC][parts][4 b][4 j][rows] of 16 bytes, xs [KC][16] = 2^-up,
 //   with shifts xg [KC][groups][16] = X.
 
@@ -264,7 +266,7 @@ __device__ __forceinline__ void quant_put(const float (&v)[8], int o, int r, int
     top = max(top, (uint32_t)__shfl_xor((int)top, d, 16));
     if (SHIFT && d * 8 < G) sum += __shfl_xor(sum, d, 16);
   }
-  // a block of values below 2^-112 keeps fewer bits
+  // 2^126 at most: values below 2^-112 are whole steps of 2^-149, which are halves then
   const int e = max((int)(top >> 23) - 127, -112), up = top ? 14 - e : 0;
   uint32_t hi[4], lo[4];
 #pragma unroll

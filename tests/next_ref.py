@@ -5,8 +5,8 @@ u = 2^-24 is fp32's half step; a rounding to bf16 is off by at most 2^-8 of the
 value (torch.finfo(torch.bfloat16).eps / 2).
 
 * The 4-bit product: x, scaled so that its block's largest value is at least 2^14, is
-  a half, or the sum of two, 2^-24 of it away at most, or half of a half's smallest step
-  (2^-24): 2^-39 of the block's largest value.  A product of a half and a code is exact;
+  a half, or the sum of two, 2^-23 of it (2 u) away at most, or half of a half's smallest
+  step (2^-24): 2^-39 of the block's largest value.  A product of a half and a code is exact;
   of H terms each passes at most H additions in fp32 and two multiplications (the group's
   scale; the powers of two are exact), and with a shift the same again, of |m x|:
   (2 H + 16) u of the sum of the terms' magnitudes, as for any fp32 product.
