@@ -423,8 +423,10 @@ cavs_status cavs_vocab_grad(cavs_ctx* ctx, const cavs_vocab* v, float* loss, flo
  * gradients scaled so that it stays below a limit,
  *   norm = |scale| sqrt(sum of all g^2),   out = scale min(1, max_norm / norm) g
  * with squares and sums in fp64 and one rounding of each product to fp32 and of
- * each output to its type; the same bits from run to run.  A norm that is not
- * finite (a gradient is not) clips nothing: out = scale g, and norm says so.
+ * each output to its type; the same bits from run to run.  A gradient that is not
+ * finite makes norm infinite or NaN, and nothing is clipped: out = scale g.  Finite
+ * gradients are clipped whatever their norm: one that fp32 cannot hold is written as
+ * infinity, and they are scaled by its value in fp64 all the same.
  * ------------------------------------------------------------------------- */
 typedef struct {
   const void* g;            /* [n] gradient, aligned to its elements */

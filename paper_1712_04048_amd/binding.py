@@ -597,7 +597,9 @@ def clip_workspace_bytes() -> int:
 def clip_grads(ctx: Context, grads: GradList, max_norm: float, norm: torch.Tensor, ws: torch.Tensor,
                scale: float = 1.0) -> None:
     """cavs_clip_grads (asynchronous): norm [1] of all gradients times scale, and
-    the gradients times scale, and times max_norm / norm where that is below 1."""
+    the gradients times scale, and times max_norm / norm where that is below 1: also
+    where float32 holds the norm only as infinity.  A gradient that is not finite leaves
+    all of them unclipped."""
     dev = ctx.torch_device
     if not isinstance(grads, GradList):
         raise CavsError(ERR_ARG, "grads: a GradList is required")

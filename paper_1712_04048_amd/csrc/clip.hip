@@ -215,7 +215,8 @@ __device__ __forceinline__ void clip_scale(const T* g, O* out, long long from, l
 // read it for the norm, so that what was read last is found in its cache (12 million
 // fp32 gradients in both launches: 30.2 us with runs on any XCD, 28.2 on their own,
 // 26.8 from their ends on; 111 million bf16 ones 111.8, 111.6 and 108.3).  A norm that
-// is not finite clips nothing.
+// is not finite in fp64, as a gradient's infinity or NaN makes it, clips nothing; one
+// that only fp32 cannot hold does.
 template <bool FAR>
 __global__ void __launch_bounds__(kThreads) k_clip_scale(const ClipEntry* table, int count, uint32_t total, int slots_n,
                                                          const double* slots, float scale, float max_norm,
