@@ -509,10 +509,12 @@ cavs_status cavs_quant_product(cavs_ctx* ctx, const cavs_quant* q, int32_t x_typ
  *                        v -= frequency k
  *   v += bias_c;  v += sum of the row's extra of c (in the list's order)
  *   v = -inf where the row's mask has c's bit clear;  v /= temp
- * Every array may be NULL: its step is left out (with all three penalties NULL, or
- * L = 0, past is not read).  Words -1 are none; a word or mask row out of range
- * counts as -1, and the next cavs_sync or cavs_timing_read returns
- * CAVS_ERR_RANGE.  repeat and temp should be above 0: they are not checked. */
+ * A step is left out where its arrays are NULL, extra's where K = 0.  Refused:
+ * repeat, presence or frequency without past, unless L = 0; K > 0 without extra_word or
+ * extra; mask_row without mask; mask with M = 0, or without mask_row and M neither 1
+ * nor n.  past is not read where there is no penalty.  Words -1 are none; a word or
+ * mask row out of range counts as -1, and the next cavs_sync or cavs_timing_read
+ * returns CAVS_ERR_RANGE.  repeat and temp should be above 0: they are not checked. */
 typedef struct {
   int32_t z_type, out_type; /* CAVS_T_* */
   int32_t n, C;             /* rows, words; at most 2^20 each */
@@ -540,7 +542,7 @@ size_t cavs_adjust_workspace_bytes(int32_t n, int32_t C);
    NULL) the first of each row's largest v, not NaN, or -1 where no v is above
    -inf; lse [n] (or NULL) ln sum_c exp(v_c), so that v - lse is the word's log
    probability: -inf for a row without words, NaN with one.  best and lse are of
-   the v before out is rounded. */
+   the v before out is rounded.  All three NULL are refused, unless n = 0. */
 cavs_status cavs_adjust_logits(cavs_ctx* ctx, const cavs_rules* rules, const void* z, void* out,
                                int32_t* best, float* lse, void* ws, size_t ws_bytes);
 
