@@ -20,6 +20,11 @@ constexpr int kThreads = 512;
 constexpr int kChunk = kThreads * 8;   // elements that a workgroup takes at a time
 constexpr int kSet = 160;        // gradients whose list is an argument of a launch
 constexpr int kTable = 4096;     // gradients of a table in the workspace
+// Elements that a launch writes from which on they go past the caches: fewer fit into
+// them beside what the next step reads (norm and scaling together, stores into the
+// caches and past them: 12 million in fp32 31.3 us and 26.9, 111 million in bf16 132
+// and 108).  Elements, not chunks: a tensor of any size has one at least.
+constexpr long long kFar = 8 << 20;
 
 // Gradients of a launch; end[k]: chunks up to and with the k-th's.
 struct ClipSet {
@@ -70,8 +75,7 @@ __device__ __forceinline__ float one_float(float v) { return v; }
 __device__ __forceinline__ float one_float(u16 v) { return __uint_as_float((uint32_t)v << 16); }
 
 // FAR: past the caches, which then keep what is read next (the gradients themselves,
-// for the pass that scales them: 111 million bf16 gradients 134 us with ordinary
-// stores, 111 past the caches).
+// for the pass that scales them); from kFar on, where the figures are.
 template <bool FAR, class V>
 __device__ __forceinline__ void put(V* p, V v) {
   if constexpr (FAR) __builtin_nontemporal_store(v, p);
@@ -255,13 +259,15 @@ __global__ void __launch_bounds__(kThreads) k_clip_scale(const ClipEntry* table,
 
 struct ClipFill {
   ClipSet set;
-  uint32_t total;   // its chunks
+  uint32_t total;      // its chunks
+  long long written;   // elements of the outputs
 };
 // The next set of gradients from `at` on; returns where the one after it begins.
 int clip_fill(const cavs_grad* grads, int count, int at, ClipFill& f) {
   ClipSet& a = f.set;
   a.count = 0;
   f.total = 0;
+  f.written = 0;
   std::fill(std::begin(a.gbf), std::end(a.gbf), 0u);
   std::fill(std::begin(a.obf), std::end(a.obf), 0u);
   for (; at < count && a.count < kSet; ++at) {
@@ -272,6 +278,7 @@ int clip_fill(const cavs_grad* grads, int count, int at, ClipFill& f) {
     a.out[k] = g.out;
     a.n[k] = (uint32_t)g.n;
     f.total += (uint32_t)((g.n + kChunk - 1) / kChunk);
+    if (g.out) f.written += g.n;
     a.end[k] = f.total;
     if (g.g_type == CAVS_T_BF16) a.gbf[k >> 5] |= 1u << (k & 31);
     if (g.out_type == CAVS_T_BF16) a.obf[k >> 5] |= 1u << (k & 31);
@@ -306,14 +313,20 @@ cavs_status clip_run(cavs_ctx* ctx, const cavs_grad* grads, int count, float sca
   double* slots = (double*)ws;
   ClipEntry* table = (ClipEntry*)(slots + kSlots);
   ClipFill f;
-  // gradients that share a table, and their chunks
+  // gradients that share a table, their chunks, and elements of their outputs
   struct Round {
     int entries;
     uint32_t chunks;
+    long long written;
+    void add(const ClipFill& f) {
+      entries += f.set.count;
+      chunks += f.total;
+      written += f.written;
+    }
   };
   auto fits = [&](const Round& r) { return r.entries + f.set.count <= kTable && r.chunks + (uint64_t)f.total < 1u << 31; };
   int written = 0;
-  Round first{0, 0};
+  Round first{};
   bool open = true;   // the first round takes this set
   int second = count;
   for (int at = 0; at < count;) {
@@ -328,26 +341,21 @@ cavs_status clip_run(cavs_ctx* ctx, const cavs_grad* grads, int count, float sca
     CAVS_LAUNCH("k_clip_norm", k_clip_norm, dim3(blocks), dim3(kThreads), 0, ctx->stream, f.set, f.total, written,
                 first.chunks, slots, open ? table + first.entries : nullptr);
     written = std::max(written, blocks);
-    if (open) {
-      first.entries += f.set.count;
-      first.chunks += f.total;
-    }
+    if (open) first.add(f);
   }
   auto scaled = [&](const Round& r, float* to) {
-    // from 2048 chunks, 8 million elements, on past the caches: fewer fit into them
-    // beside what the next step reads (12 million in fp32 31.3 us and 26.9, 111 million
-    // in bf16 132 and 108, norm and scaling together)
-    CAVS_LAUNCH("k_clip_scale", r.chunks >= 2048 ? k_clip_scale<true> : k_clip_scale<false>,
+    const bool far = r.written >= kFar;
+    CAVS_LAUNCH(far ? "k_clip_scale<far>" : "k_clip_scale", far ? k_clip_scale<true> : k_clip_scale<false>,
                 dim3(std::max(1u, std::min<uint32_t>(r.chunks, kSlots))), dim3(kThreads), 0, ctx->stream,
                 (const ClipEntry*)table, r.entries, r.chunks, written, (const double*)slots, scale, max_norm, to);
   };
   bool any = false;
   for (int i = 0; i < count; ++i) any |= grads[i].out && grads[i].n > 0;
-  if (!any) first = Round{0, 0};
+  if (!any) first = Round{};
   scaled(first, norm);
   // what the table could not hold, a table at a time
   for (int at = second; any && at < count;) {
-    Round r{0, 0};
+    Round r{};
     while (at < count) {
       const int from = at;
       at = clip_fill(grads, count, at, f);
@@ -358,8 +366,7 @@ cavs_status clip_run(cavs_ctx* ctx, const cavs_grad* grads, int count, float sca
       }
       CAVS_LAUNCH("k_clip_norm", k_clip_norm, dim3(1), dim3(kThreads), 0, ctx->stream, f.set, f.total, 0, r.chunks,
                   (double*)nullptr, table + r.entries);
-      r.entries += f.set.count;
-      r.chunks += f.total;
+      r.add(f);
     }
     scaled(r, nullptr);
   }
