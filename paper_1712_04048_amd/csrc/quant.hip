@@ -320,7 +320,11 @@ __device__ __forceinline__ void quant_stage(const X* __restrict__ x, int H, int 
 // waited for them (16 x 128 000 x 2048: 43 us, 37 so).
 // Bound by memory, the codes once: 16 x 128 000 x 2048 in 36 us (143 MB, 4.0 TB/s), of
 // which reading the codes alone takes 28; 4 x 50 001 x 1024 in 10 (30 MB); below some
-// 10 MB by latency (1 x 10 000 x 512 in 4).
+// 10 MB by latency (1 x 10 000 x 512 in 4.5).  fp32 rows have two halves a value: 42 us
+// and 13.  Two forms are far from the codes' bytes: more than 16 rows, whose groups each
+// make halves of the codes (64 x 32 000 x 2048 in 31 us, fp32 36, 42 MB), and rows that
+// are not in LDS whole, which are staged anew for every group of tiles (16 x 32 000 x
+// 4096 fp32 in 31 us, 70 MB; bf16, which fits, 25).
 struct QuantJob {
   QuantNet q;
   const void* x;
