@@ -465,7 +465,8 @@ cavs_status cavs_clip_grads(cavs_ctx* ctx, const cavs_grad* grads, int32_t count
  * from 0 (the lower of two alike); with them s = (highest - lowest) / 15 and m =
  * (highest + lowest + s) / 2.  Both are rounded to fp32 and that to bf16 before q is taken; where
  * s = 0, as in a group of zeros or, with shifts, of one value, q = 8; a group with a weight
- * that is not finite has s = NaN, m = 0, q = 8.
+ * that is not finite has s = NaN, m = 0, q = 8.  Weights of 2^127 and more may come out
+ * as infinities, by the roundings of s and m.
  *
  * `data` is cavs_quant_bytes(q) bytes, aligned to 16, that cavs_quant_pack writes
  * and a program may keep in files.  With T = ceil(C / 16) and KB = ceil(H / 128):

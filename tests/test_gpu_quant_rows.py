@@ -1,5 +1,6 @@
 """How exactly the 4-bit product takes its rows, on the GPU: each word has one weight
-that is not 0, so that y is x as the product takes it, times that weight."""
+that is not 0, so that y is x as the product takes it, times that weight.  And the
+largest weights."""
 import pytest
 import torch
 
@@ -43,3 +44,23 @@ def test_one_weight_a_word(ctx, n, group, dtype):
             if dtype == BF16:
                 kept = row.abs() >= 2.0 ** -31 * top
                 assert torch.equal(mine[kept], row[kept]), (i, at)
+
+
+@pytest.mark.parametrize("shift", [False, True])
+def test_weights_at_the_end_of_fp32(ctx, shift):
+    """Below 2^127 they stay finite; the largest floats come out as s and m say, which
+    are infinities."""
+    big = torch.finfo(F32).max
+    under = 2.0 ** 127 * (1 - 2.0 ** -24)
+    W = torch.zeros(32, 5)
+    W[:, 0], W[:, 1], W[:, 2] = under, big, torch.linspace(0.9 * under, under, 32)
+    W[::2, 3], W[1::2, 3] = under, -under
+    W[:, 4] = (torch.linspace(-1, 1, 32).double() * big).float()
+    W = W.cuda()
+    q = _packed(ctx, W, 32, shift)
+    want = R.weights(*R.quantise(W, 32, shift), 32).float()
+    back = torch.zeros_like(W)
+    B.quant_unpack(ctx, q, back)
+    ctx.sync()
+    assert torch.equal(back, want)
+    assert torch.isfinite(back[:, [0, 2, 3]]).all() and torch.isinf(back[:, 1]).all()
