@@ -226,7 +226,8 @@ class LmBatch(Batch):
     def quantise(self, group: int = 128, shift: bool = False):
         """The head in 4 bits, which next_words scores with (cavs_quant_pack): the
         weights as they are now, into the memory of the last call where that had the
-        same form (so a captured next_words finds them there)."""
+        same form (so a captured next_words finds them there).  Whatever else reads
+        ``quant`` gets them too: let its calls on other streams end first."""
         H, C = self.Ws.shape
         (Ws, count), q = self._head_now(), self.quant
         if q is None or q is not self.rounded[0] or (q.H, q.C, q.group, q.shift) != (H, C, group, bool(shift)):
